@@ -11,7 +11,9 @@
  *                     sampling, returning the accepted length and the correction token;
  *   hawk_tree_accept  the same for a candidate tree with several candidates per depth.
  *   hawk_spec_cache_*, hawk_pool_*  the cache of vertical predictions and the sampling pool that feed it;
- *   hawk_head_proj_cfg, hawk_*_accept_guided  the head with the guidance combine in its epilogue.
+ *   hawk_head_proj_cfg, hawk_*_accept_guided  the head with the guidance combine in its epilogue;
+ *   hawk_qk_norm_rope, hawk_rope_append, hawk_paged_attn  what surrounds the attention when the cache is paged:
+ *                     norm and rotation of the heads, writing the new rows, attention of a chunk of them.
  *
  * Conventions common to all entry points
  *   - Every pointer is a DEVICE pointer owned by the caller unless the comment says "host".  The
@@ -57,6 +59,9 @@ typedef enum {
 #define HAWK_DEV_NONFINITE 4  /* a NaN or +inf logit was treated as -inf                        */
 #define HAWK_DEV_BAD_PREFIX 8 /* a prefix length lay outside [0, L_cap - K] and was clamped     */
 #define HAWK_DEV_BAD_TREE 16  /* a child range or draft-row index of the tree was out of range    */
+#define HAWK_DEV_BAD_ROWS 64  /* row_begin does not cut the new rows into streams as the call says; the stream was skipped */
+#define HAWK_DEV_BAD_PAGE 128 /* a page id lay outside [0, n_pages)                             */
+#define HAWK_DEV_BAD_POSITION 256 /* a rotation position lay outside [0, n_positions) and was clamped */
 #define HAWK_DEV_BOUNDS 32    /* libraries built with -DHAWK_DEBUG only: an index lay outside its array, the access was skipped */
 
 const char *hawk_status_string(hawk_status status);
@@ -421,6 +426,152 @@ typedef struct {
 } hawk_step_host_args;
 
 hawk_status hawk_verify_step_host(const hawk_step_host_args *args, hawk_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Heads, pages and chunks: the calls around a PAGED key/value cache.
+ *
+ * The paper's target model runs its attention on rotated (and, for some models, normalised) query and
+ * key heads over a KV cache (App. C mentions the cache; Sec. 5 the model); it gives none of these steps.
+ * The calls below are the textbook operations on the cache layout that serving engines use.
+ *
+ * Batch layout shared by hawk_rope_append and hawk_paged_attn.  S streams bring new rows of unequal
+ * number, packed one stream after the other:
+ *   row_begin    int32 [S+1], device, non-decreasing, within [0, T]: stream s owns rows
+ *                row_begin[s] .. row_begin[s+1]-1 of the T rows; n_s = their number (0: the stream is
+ *                idle).  Rows of no stream (padding in front or behind) are neither read into a
+ *                result nor written.
+ *   kv_len       int32 [S], device: keys of the stream INCLUDING its n_s new rows; new row i is cache row
+ *                kv_len[s] - n_s + i.  Entries of idle streams are ignored.
+ *   block_table  int32 [S][table_width], device: entry j is the page that holds cache rows
+ *                j * page_size .. (j+1) * page_size - 1.  Entries past the last used page may hold anything.
+ *   k_pages, v_pages  16-bit, element (page, head, row, d) at page * page_stride + head * head_stride +
+ *                row * row_stride + d (strides in elements): [n_pages][H_kv][page_size][D], the same with
+ *                rows before heads, keys and values in one buffer are all expressible.  A dense cache
+ *                [S][H_kv][L_cap][D] is the paged one with page_size = L_cap and block_table[s][0] = s.
+ * dtype is HAWK_BF16 or HAWK_F16 and holds for every 16-bit tensor of the call.  All 16-bit bases are
+ * 16-byte aligned and all strides multiples of 8 elements (16 bytes); D is 64 or 128.
+ * ---------------------------------------------------------------------------------------------- */
+#define HAWK_BF16 0
+#define HAWK_F16 1
+
+#define HAWK_NORM_NONE 0
+#define HAWK_NORM_RMS 1
+#define HAWK_NORM_LAYER 2
+
+/* ------------------------------------------------------------------------------------------------
+ * hawk_qk_norm_rope - norm of every query and key head, then the position rotation, in one pass.
+ *
+ * Operation, per row t and head h of q (and likewise of k), with x = q[t][h][0..D-1] in fp32:
+ *   HAWK_NORM_RMS    x <- x / sqrt(mean(x^2) + eps) * weight
+ *   HAWK_NORM_LAYER  x <- (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight + bias
+ *   HAWK_NORM_NONE   x as it is
+ * then with c_i = cos_sin[position[t]][i], s_i = cos_sin[position[t]][rot_dim/2 + i], i < rot_dim/2, each
+ * pair (a, b) of elements becomes (a*c_i - b*s_i, b*c_i + a*s_i); the pair is (x[i], x[i + rot_dim/2]), or
+ * (x[2i], x[2i+1]) with `interleaved`.  Elements from rot_dim on are not rotated.  Everything is fp32
+ * up to ONE rounding to the output type.  The table is the caller's: one axis (angle = position * base^(-2i/rot_dim)),
+ * or an image's raster (half the angles by row, half by column), and nodes of a candidate tree at the same depth
+ * simply share a position.
+ *
+ *   q, k         16-bit [T][H][D], [T][H_kv][D] at row and head strides (elements), so that both may be parts of
+ *                one projection's output.  H or H_kv may be 0 (that tensor is absent).
+ *   q_out, k_out the same shapes, own strides; may be q and k themselves (same strides), else must not overlap them
+ *   q_weight, k_weight, q_bias, k_bias   16-bit [D], or with per_head [H][D] / [H_kv][D]; a bias may be NULL
+ *                (none); weights are required by a norm of that tensor, ignored with HAWK_NORM_NONE
+ *   position     int32 [T]
+ *   cos_sin      fp32 [n_positions][rot_dim], 16-byte aligned
+ * Supported: D in {64, 128}; rot_dim a multiple of 16, 0 <= rot_dim <= D (0: no rotation, position and
+ * cos_sin are not read).  A position outside [0, n_positions) is clamped and flagged HAWK_DEV_BAD_POSITION.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, PARAM (eps not a finite number >= 0, unknown dtype or norm), CUDA.
+ * T == 0 returns HAWK_OK without a launch.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct hawk_qk_rope_args {
+    int dtype, T, H, H_kv, D;
+    int norm, per_head, rot_dim, n_positions, interleaved;
+    float eps;
+    const void *q, *k;
+    void *q_out, *k_out;
+    long long q_row_stride, q_head_stride, k_row_stride, k_head_stride;
+    long long q_out_row_stride, q_out_head_stride, k_out_row_stride, k_out_head_stride;
+    const void *q_weight, *k_weight, *q_bias, *k_bias;
+    const int32_t *position;
+    const float *cos_sin;
+} hawk_qk_rope_args;
+
+hawk_status hawk_qk_norm_rope(const hawk_qk_rope_args *args, int32_t *dev_status, hawk_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hawk_rope_append - the new rows' keys and values into the paged cache, normalised and rotated on the way.
+ *
+ * Operation: k goes through hawk_qk_norm_rope's operation and lands in k_pages, v is copied to v_pages, at
+ * the cache row the batch layout above gives each new row; q (H > 0) goes through the same operation
+ * into q_out.  Rows of no stream are skipped in all three.  qk.k_out and its strides are ignored.
+ *   v   16-bit [T][H_kv][D] at its own strides
+ * page_size may be any positive number here.  Two rows sent to the same place of the same page (streams that
+ * share a page they both write) leave either.
+ * A cache row outside [0, table_width * page_size) skips the row's k and v and is flagged HAWK_DEV_BAD_PREFIX, a page id
+ * outside [0, n_pages) the same with HAWK_DEV_BAD_PAGE; q_out is written all the same.
+ * Errors as hawk_qk_norm_rope.  T == 0 or S == 0 returns HAWK_OK without a launch.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct hawk_rope_append_args {
+    hawk_qk_rope_args qk;
+    const void *v;
+    long long v_row_stride, v_head_stride;
+    void *k_pages, *v_pages;
+    long long k_page_stride, k_page_head_stride, k_page_row_stride;
+    long long v_page_stride, v_page_head_stride, v_page_row_stride;
+    int n_pages, page_size, S, table_width;
+    const int32_t *block_table, *row_begin, *kv_len;
+} hawk_rope_append_args;
+
+hawk_status hawk_rope_append(const hawk_rope_append_args *args, int32_t *dev_status, hawk_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hawk_paged_attn - attention of a chunk of new rows over the paged cache.
+ *
+ * Operation: for new row i of stream s (its own key already in the cache), query head h, kv head g = h / (H/H_kv),
+ * with p = kv_len[s] - n_s cache rows in front of the chunk:
+ *     visible keys   j <= p + i                                       (anc_mask NULL: chain)
+ *                    j < p, and j = p + m, m < n_s, iff bit m of anc_mask[i] is set   (anc_mask: tree)
+ *     out[row][h*D:(h+1)*D] = sum_j softmax(sm_scale * <q[row][h], k_j>)_j * v_j
+ * A row that sees no key (p + i < 0; an empty mask without a prefix) gives zeros.  n_s = 1 is a decode step, up
+ * to 64 rows a verify step (hawk_verify_attn, hawk_verify_attn_tree), thousands a chunk of a prompt; one call may mix
+ * them.  Scores, maxima, sums and accumulators are fp32; the probabilities are rounded to the 16-bit type for the
+ * second product, the result once.
+ * Cache rows from kv_len[s] on are never used (they may hold anything, NaN included).  Rows below kv_len[s] must be
+ * finite: a NaN or infinity among a stream's own rows may reach rows of that stream that do not see it.
+ *
+ *   q          16-bit [T][H][D] at row and head strides
+ *   out        16-bit [T][H*D], dense
+ *   anc_mask   uint64 [max_new], device, or NULL; row i of every stream uses entry i.  max_new <= 64 with it.
+ *   max_new    upper bound of n_s known on the host; a stream with more rows is skipped, HAWK_DEV_BAD_ROWS
+ *   max_kv     upper bound of kv_len of the streams that are not idle, <= table_width * page_size (sizes the launch
+ *              and the workspace); a kv_len outside [0, max_kv] is clamped, HAWK_DEV_BAD_PREFIX
+ *   workspace  at least hawk_paged_attn_workspace_bytes(...) bytes, 16-byte aligned, may be NULL when that is 0;
+ *              no initialisation.  Calls that may overlap on the GPU need one each.
+ * A page id outside [0, n_pages) reads as zeros and is flagged HAWK_DEV_BAD_PAGE.
+ * Supported: D in {64, 128}; page_size a multiple of 8; S <= 4096; H a multiple of H_kv, H/H_kv <= 128.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, PARAM, CUDA.  S == 0, T == 0 or max_new == 0 returns HAWK_OK
+ * without a launch.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct hawk_paged_attn_args {
+    int dtype, S, T, max_new, max_kv, H, H_kv, D;
+    int n_pages, page_size, table_width;
+    float sm_scale;
+    const void *q;
+    long long q_row_stride, q_head_stride;
+    const void *k_pages, *v_pages;
+    long long k_page_stride, k_page_head_stride, k_page_row_stride;
+    long long v_page_stride, v_page_head_stride, v_page_row_stride;
+    const int32_t *block_table, *row_begin, *kv_len;
+    const uint64_t *anc_mask;
+    void *out;
+    void *workspace;
+    size_t workspace_bytes;
+} hawk_paged_attn_args;
+
+size_t hawk_paged_attn_workspace_bytes(int S, int T, int max_new, int H, int H_kv, int D, int max_kv);
+
+hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t *dev_status, hawk_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -16,6 +16,7 @@ _BINDING_NAMES = (
     "spec_cache_slots", "spec_cache_slot", "spec_cache_new", "spec_cache_clear", "spec_cache_put",
     "pool_build", "pool_sample", "pool_sample_workspace_bytes",
     "head_proj_cfg", "cfg_accept_guided", "tree_accept_guided",
+    "qk_norm_rope", "rope_append", "paged_attn", "paged_attn_workspace_bytes",
 )
 
 

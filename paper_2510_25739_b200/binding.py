@@ -18,6 +18,7 @@ _LIB_PATH = _PKG / "libhawk_verify.so"
 _lib: Optional[ctypes.CDLL] = None
 
 DEV_TIMEOUT, DEV_BAD_DRAFT, DEV_NONFINITE, DEV_BAD_PREFIX, DEV_BAD_TREE, DEV_BOUNDS = 1, 2, 4, 8, 16, 32
+DEV_BAD_ROWS, DEV_BAD_PAGE, DEV_BAD_POSITION = 64, 128, 256
 
 EXPORTS = (
     "hawk_status_string", "hawk_version",
@@ -30,6 +31,7 @@ EXPORTS = (
     "hawk_spec_cache_slots", "hawk_spec_cache_slot", "hawk_spec_cache_clear", "hawk_spec_cache_put",
     "hawk_pool_build", "hawk_pool_sample_workspace_bytes", "hawk_pool_sample",
     "hawk_head_proj_cfg", "hawk_cfg_accept_guided", "hawk_tree_accept_guided",
+    "hawk_qk_norm_rope", "hawk_rope_append", "hawk_paged_attn_workspace_bytes", "hawk_paged_attn",
 )
 
 
@@ -49,6 +51,38 @@ def _step_fields():
 class StepHostArgs(ctypes.Structure):
     """Mirror of hawk_step_host_args (include/hawk.h)."""
     _fields_ = _step_fields()
+
+
+class QkRopeArgs(ctypes.Structure):
+    """Mirror of hawk_qk_rope_args (include/hawk.h)."""
+    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "T", "H", "H_kv", "D", "norm", "per_head", "rot_dim", "n_positions",
+                                             "interleaved")]
+                + [("eps", ctypes.c_float)]
+                + [(n, ctypes.c_void_p) for n in ("q", "k", "q_out", "k_out")]
+                + [(f"{t}_{w}_stride", ctypes.c_longlong) for t in ("q", "k", "q_out", "k_out") for w in ("row", "head")]
+                + [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "q_bias", "k_bias", "position", "cos_sin")])
+
+
+_PAGE_STRIDES = [(f"{t}_{w}_stride", ctypes.c_longlong) for t in "kv" for w in ("page", "page_head", "page_row")]
+
+
+class RopeAppendArgs(ctypes.Structure):
+    """Mirror of hawk_rope_append_args (include/hawk.h)."""
+    _fields_ = ([("qk", QkRopeArgs), ("v", ctypes.c_void_p), ("v_row_stride", ctypes.c_longlong),
+                 ("v_head_stride", ctypes.c_longlong), ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p)]
+                + _PAGE_STRIDES + [(n, ctypes.c_int) for n in ("n_pages", "page_size", "S", "table_width")]
+                + [(n, ctypes.c_void_p) for n in ("block_table", "row_begin", "kv_len")])
+
+
+class PagedAttnArgs(ctypes.Structure):
+    """Mirror of hawk_paged_attn_args (include/hawk.h)."""
+    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "S", "T", "max_new", "max_kv", "H", "H_kv", "D", "n_pages", "page_size",
+                                             "table_width")]
+                + [("sm_scale", ctypes.c_float), ("q", ctypes.c_void_p), ("q_row_stride", ctypes.c_longlong),
+                   ("q_head_stride", ctypes.c_longlong), ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p)]
+                + _PAGE_STRIDES
+                + [(n, ctypes.c_void_p) for n in ("block_table", "row_begin", "kv_len", "anc_mask", "out", "workspace")]
+                + [("workspace_bytes", ctypes.c_size_t)])
 
 
 class HawkError(RuntimeError):
@@ -139,6 +173,11 @@ def _open(path: Path) -> ctypes.CDLL:
     lib.hawk_pool_sample_workspace_bytes.argtypes = [i32, i32]
     lib.hawk_pool_sample.restype = i32
     lib.hawk_pool_sample.argtypes = [vp] * 4 + [i32] * 6 + [vp, sz, vp, vp]
+    for name, args in (("hawk_qk_norm_rope", QkRopeArgs), ("hawk_rope_append", RopeAppendArgs), ("hawk_paged_attn", PagedAttnArgs)):
+        getattr(lib, name).restype = i32
+        getattr(lib, name).argtypes = [ctypes.POINTER(args), vp, vp]
+    lib.hawk_paged_attn_workspace_bytes.restype = sz
+    lib.hawk_paged_attn_workspace_bytes.argtypes = [i32] * 7
     lib.hawk_verify_step_host.restype = i32
     lib.hawk_verify_step_host.argtypes = [ctypes.POINTER(StepHostArgs), vp]
     return lib
@@ -510,6 +549,196 @@ def pool_sample(pool_q: torch.Tensor, u: torch.Tensor, node_q: torch.Tensor, v_b
     if rc != 0:
         raise HawkError(rc, "hawk_pool_sample")
     return node_token
+
+
+_DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1}
+_NORM_CODES = {"none": 0, "rms": 1, "layer": 2}
+
+
+def _heads(t: torch.Tensor, name: str, like: torch.Tensor, shape):
+    """(pointer, row stride, head stride) of a [rows, heads, D] tensor whose last dimension is dense."""
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name}: expected {like.dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != like.device:
+        raise ValueError(f"{name}: must be on {like.device}")
+    a, b, c = t.stride()
+    if c != 1:
+        raise ValueError(f"{name}: the head dimension must be contiguous")
+    return t.data_ptr(), a, b
+
+
+def _dense(t: Optional[torch.Tensor], name: str, dtype, shape, device):
+    """Pointer of a contiguous tensor, None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name}: must be on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    return t.data_ptr()
+
+
+def _call(name: str, args: ctypes.Structure, dev_status: Optional[torch.Tensor], device) -> None:
+    """Runs an entry point on `device` and its current stream."""
+    fn = getattr(load_library(), name)
+    status = _dense(dev_status, "dev_status", torch.int32, (1,), device)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            rc = fn(ctypes.byref(args), status, torch.cuda.current_stream().cuda_stream)
+    else:
+        rc = fn(ctypes.byref(args), status, torch.cuda.current_stream().cuda_stream)
+    if rc != 0:
+        raise HawkError(rc, name)
+
+
+def _cuda_16bit(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a CUDA tensor")
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: expected torch.bfloat16 or torch.float16, got {t.dtype}")
+    return code
+
+
+def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, like: torch.Tensor, H_kv: int, D: int):
+    """Page count, page size, pointers and strides (page, head, row) of the two [n_pages, H_kv, page_size, D] tensors."""
+    n_pages, page_size = k_pages.shape[0], k_pages.shape[2]
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if t.dtype != like.dtype:
+            raise TypeError(f"{name}: expected {like.dtype}, got {t.dtype}")
+        if t.shape != (n_pages, H_kv, page_size, D):
+            raise ValueError(f"{name}: expected shape {(n_pages, H_kv, page_size, D)}, got {tuple(t.shape)}")
+        if t.device != like.device:
+            raise ValueError(f"{name}: must be on {like.device}")
+        if t.stride(3) != 1:
+            raise ValueError(f"{name}: the head dimension must be contiguous")
+    return n_pages, page_size, k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride()[:3] + v_pages.stride()[:3]
+
+
+def _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved, q_out, k_out, dense_k):
+    """QkRopeArgs and the output tensors (allocated where none was given)."""
+    x = k if q is None else q
+    code = _cuda_16bit(x, "k" if q is None else "q")
+    dev, dt = x.device, x.dtype
+    T, _, D = x.shape
+    if norm not in _NORM_CODES:
+        raise ValueError(f"norm: expected one of {tuple(_NORM_CODES)}, got {norm!r}")
+    H = H_kv = n_pos = rot = per_head = 0
+    qp = qop = kp = kop = (None, 0, 0)
+    if q is not None:
+        H = q.shape[1]
+        qp = _heads(q, "q", x, (T, H, D))
+        if q_out is None:
+            q_out = torch.empty((T, H, D), dtype=dt, device=dev)
+        qop = _heads(q_out, "q_out", x, (T, H, D))
+    if k is not None:
+        H_kv = k.shape[1]
+        kp = _heads(k, "k", x, (T, H_kv, D))
+        if dense_k:
+            if k_out is None:
+                k_out = torch.empty((T, H_kv, D), dtype=dt, device=dev)
+            kop = _heads(k_out, "k_out", x, (T, H_kv, D))
+    if norm != "none":
+        first = next((w for w in (q_weight, k_weight) if w is not None), None)
+        per_head = int(first is not None and first.dim() == 2)
+        qs, ks = ((H, D), (H_kv, D)) if per_head else ((D,), (D,))
+        weights = (_dense(q_weight, "q_weight", dt, qs, dev), _dense(k_weight, "k_weight", dt, ks, dev),
+                   _dense(q_bias, "q_bias", dt, qs, dev), _dense(k_bias, "k_bias", dt, ks, dev))
+    else:
+        weights = (None, None, None, None)
+    if cos_sin is not None:
+        n_pos, rot = cos_sin.shape
+        cs = _dense(cos_sin, "cos_sin", torch.float32, (n_pos, rot), dev)
+        pos = _dense(position, "position", torch.int32, (T,), dev)
+    else:
+        cs = pos = None
+    return QkRopeArgs(code, T, H, H_kv, D, _NORM_CODES[norm], per_head, rot, n_pos, bool(interleaved), eps, qp[0], kp[0], qop[0], kop[0],
+                      qp[1], qp[2], kp[1], kp[2], qop[1], qop[2], kop[1], kop[2], *weights, pos, cs), q_out, k_out, x
+
+
+def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], position: Optional[torch.Tensor],
+                 cos_sin: Optional[torch.Tensor], norm: str = "none", eps: float = 1e-6,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                 q_bias: Optional[torch.Tensor] = None, k_bias: Optional[torch.Tensor] = None, interleaved: bool = False,
+                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                 dev_status: Optional[torch.Tensor] = None):
+    """Norm of every head ("none", "rms", "layer"), then the position rotation: q [T,H,D], k [T,H_kv,D] (bf16 or fp16, any
+    row and head strides) -> (q_out, k_out).  cos_sin fp32 [positions, rot_dim] holds cosines, then sines, of each position;
+    position int32 [T]; None for both: no rotation.  Weights and biases are [D], or [heads, D] one for each head."""
+    if q is None and k is None:
+        raise ValueError("q, k: one of them is needed")
+    args, q_out, k_out, x = _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved,
+                                       q_out, k_out, True)
+    _call("hawk_qk_norm_rope", args, dev_status, x.device)
+    return q_out, k_out
+
+
+def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, position: Optional[torch.Tensor],
+                cos_sin: Optional[torch.Tensor], k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor,
+                row_begin: torch.Tensor, kv_len: torch.Tensor, norm: str = "none", eps: float = 1e-6,
+                q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                q_bias: Optional[torch.Tensor] = None, k_bias: Optional[torch.Tensor] = None, interleaved: bool = False,
+                q_out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """New rows k, v [T,H_kv,D] into k_pages, v_pages [n_pages,H_kv,page_size,D] (any page, head and row strides), k normalised
+    and rotated as by qk_norm_rope; q [T,H,D] goes the same way into q_out, which is returned.  Stream s owns rows
+    row_begin[s] .. row_begin[s+1]-1; kv_len [S] counts its keys with the new ones; block_table [S, pages a stream]."""
+    args, q_out, _, x = _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved, q_out,
+                                   None, False)
+    dev = x.device
+    T, H_kv, D = k.shape
+    vp = _heads(v, "v", x, (T, H_kv, D))
+    n_pages, page_size, kpp, vpp, strides = _pages(k_pages, v_pages, x, H_kv, D)
+    S, width = block_table.shape
+    full = RopeAppendArgs(args, *vp, kpp, vpp, *strides, n_pages, page_size, S, width,
+                          _dense(block_table, "block_table", torch.int32, (S, width), dev),
+                          _dense(row_begin, "row_begin", torch.int32, (S + 1,), dev),
+                          _dense(kv_len, "kv_len", torch.int32, (S,), dev))
+    _call("hawk_rope_append", full, dev_status, dev)
+    return q_out
+
+
+def paged_attn_workspace_bytes(S: int, T: int, max_new: int, H: int, H_kv: int, D: int, max_kv: int) -> int:
+    return int(load_library().hawk_paged_attn_workspace_bytes(S, T, max_new, H, H_kv, D, max_kv))
+
+
+def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor, row_begin: torch.Tensor,
+               kv_len: torch.Tensor, max_new: int, max_kv: int, sm_scale: float, anc_mask: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new rows q [T,H,D] over the paged cache that already holds their keys (rope_append) -> out [T,H*D].
+    max_new and max_kv bound the rows a stream brings and its keys.  With anc_mask (int64 tensor holding the uint64 masks,
+    [max_new]) the rows of a stream are nodes of a candidate tree.  Rows of no stream are left as they are in `out`."""
+    code = _cuda_16bit(q, "q")
+    dev = q.device
+    T, H, D = q.shape
+    H_kv = k_pages.shape[1]
+    qp = _heads(q, "q", q, (T, H, D))
+    n_pages, page_size, kpp, vpp, strides = _pages(k_pages, v_pages, q, H_kv, D)
+    S, width = block_table.shape
+    if out is None:
+        out = torch.empty((T, H * D), dtype=q.dtype, device=dev)
+    if workspace is None:
+        need = load_library().hawk_paged_attn_workspace_bytes(S, T, max_new, H, H_kv, D, max_kv)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace: must be contiguous and on {dev}")
+    args = PagedAttnArgs(code, S, T, max_new, max_kv, H, H_kv, D, n_pages, page_size, width, sm_scale, *qp, kpp, vpp, *strides,
+                         _dense(block_table, "block_table", torch.int32, (S, width), dev),
+                         _dense(row_begin, "row_begin", torch.int32, (S + 1,), dev),
+                         _dense(kv_len, "kv_len", torch.int32, (S,), dev),
+                         _dense(anc_mask, "anc_mask", torch.int64, (max_new,), dev),
+                         _dense(out, "out", q.dtype, (T, H * D), dev),
+                         None if workspace is None else workspace.data_ptr(),
+                         0 if workspace is None else workspace.numel() * workspace.element_size())
+    _call("hawk_paged_attn", args, dev_status, dev)
+    return out
 
 
 def verify_step_host(args: StepHostArgs) -> None:

@@ -54,6 +54,21 @@ bool encode_bf16_rows_sw128(CUtensorMap *map, const void *base, uint64_t rows, u
     return r == CUDA_SUCCESS;
 }
 
+bool encode_16bit_4d_sw128(CUtensorMap *map, const void *base, bool bf16, const uint64_t (&dims)[4],
+                           const uint64_t (&strides)[3], uint32_t b1, uint32_t b2, uint32_t b3)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t d[4] = {dims[0], dims[1], dims[2], dims[3]};
+    cuuint64_t st[3] = {strides[0], strides[1], strides[2]};
+    cuuint32_t box[4] = {64, b1, b2, b3};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    CUresult r = fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                    const_cast<void *>(base), d, st, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
 bool is_sm100(int *sm_count)
 {
     int dev = 0;

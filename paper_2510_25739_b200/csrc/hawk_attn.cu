@@ -154,13 +154,6 @@ __device__ __forceinline__ bool key_visible(int rel, uint64_t m)
 // Mask of position `pos` of a plain chain: block rows 0 .. pos.
 __device__ __forceinline__ uint64_t chain_mask(int pos) { return pos >= 63 ? ~0ull : (2ull << pos) - 1ull; }
 
-__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
-{
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-
 // NQT = number of 8-query column tiles of an item: rows_per_item / 8 (1..4 at D = 64, 1..3 at D = 128).
 template <int D, int NQT, int kWarps, int kStages>
 __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1) attn_kernel(const __grid_constant__ CUtensorMap map_k,
@@ -588,34 +581,6 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1) at
         }
     }
 }
-
-// Division of a 31-bit unsigned number by a divisor fixed at launch: one multiply-high and a shift
-// (division by invariant integers, Granlund and Montgomery): mul = ceil(2^(31 + ceil(log2 d)) / d),
-// n / d = umulhi(n, mul) >> (ceil(log2 d) - 1) for 0 <= n < 2^31.  The host fills it in.
-struct FastDiv {
-    uint32_t d, mul, shr;
-    __host__ void set(uint32_t div)
-    {
-        d = div;
-        if (div <= 1) {
-            mul = 0;
-            shr = 0;
-            return;
-        }
-        uint32_t lg = 0;
-        while ((1u << lg) < div) ++lg;  // ceil(log2 div), 1..31
-        const unsigned long long pw = 1ull << (31 + lg);
-        mul = static_cast<uint32_t>((pw + div - 1) / div);
-        shr = lg - 1;
-    }
-    __device__ __forceinline__ uint32_t div(uint32_t n) const { return d <= 1 ? n : __umulhi(n, mul) >> shr; }
-    __device__ __forceinline__ uint32_t divmod(uint32_t n, uint32_t &rem) const
-    {
-        const uint32_t q = div(n);
-        rem = n - q * d;
-        return q;
-    }
-};
 
 // Divisors of the merge kernel's index arithmetic.
 struct MergeDivs {

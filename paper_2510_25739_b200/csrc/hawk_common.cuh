@@ -5,6 +5,7 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -161,6 +162,29 @@ __device__ __forceinline__ void tma_load_2d_hint(void *smem_dst, const CUtensorM
         : "memory");
 }
 
+// 4-D tiled load: {x, y, z, w} from the contiguous dimension outwards; x as above, the others unrestricted.
+__device__ __forceinline__ void tma_load_4d(void *smem_dst, const CUtensorMap *map, int x, int y, int z, int w,
+                                            uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w),
+          "r"(smem_u32(bar))
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load_4d_hint(void *smem_dst, const CUtensorMap *map, int x, int y, int z, int w,
+                                                 uint64_t *bar, uint64_t policy)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+        "[%0], [%1, {%2, %3, %4, %5}], [%6], %7;"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w),
+          "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
+
 __device__ __forceinline__ uint64_t l2_policy_evict_first()
 {
     uint64_t p;
@@ -199,10 +223,26 @@ __device__ __forceinline__ void mma_bf16_16816(float (&d)[4], const uint32_t (&a
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t *>(&v);
+}
+
+// 8x8 block of 16-bit elements, one row per group of four lanes, transposed across the warp.
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 
 __device__ __forceinline__ float fast_exp2(float x)
@@ -418,6 +458,69 @@ __device__ __forceinline__ uint64_t umma_desc_k_major_sw128(uint32_t smem_addr)
     return d;
 }
 
+// D[tmem] (+)= A[tmem] * B[smem]: A is 128 lanes x 16 elements, two 16-bit elements a column; issued by ONE thread.
+__device__ __forceinline__ void umma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc,
+                                            uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// 32 lanes x 32 columns of 32 bits, registers to tensor memory: thread t of the warp writes lane (base_lane + t).
+__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_wait()
+{
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// Shared-memory matrix descriptor of an MN-major 16-bit tile: rows along K hold 64 elements (128 bytes) of the MN
+// dimension, 128-byte swizzle as above; groups of 8 K-rows are 1024 bytes apart, the next 64 MN elements follow
+// `mn_stride` bytes later.  A step of 16 along K adds 2048 bytes to the start.
+__device__ __forceinline__ uint64_t umma_desc_mn_major_sw128(uint32_t smem_addr, uint32_t mn_stride)
+{
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>((mn_stride >> 4) & 0x3FFFu) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+
+// Instruction descriptor of kind::f16, fp32 accumulator, A K-major: both operands bf16 (format 1) or both fp16 (format 0),
+// B K-major or MN-major.
+__host__ __device__ constexpr uint32_t umma_idesc_f16kind(int m, int n, bool bf16, bool b_mn_major)
+{
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_mn_major ? 1u << 16 : 0u) |
+           (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+
 // Instruction descriptor of kind::f16 with bf16 A and B (both K-major), fp32 accumulator.
 __host__ __device__ constexpr uint32_t umma_idesc_bf16_f32(int m, int n)
 {
@@ -427,6 +530,35 @@ __host__ __device__ constexpr uint32_t umma_idesc_bf16_f32(int m, int n)
            | (0u << 15) | (0u << 16) // A, B K-major
            | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
+
+// ---------------------------------------------------------------------------------- index helpers
+// Division of a 31-bit unsigned number by a divisor fixed at launch: one multiply-high and a shift
+// (division by invariant integers, Granlund and Montgomery): mul = ceil(2^(31 + ceil(log2 d)) / d),
+// n / d = umulhi(n, mul) >> (ceil(log2 d) - 1) for 0 <= n < 2^31.  The host fills it in.
+struct FastDiv {
+    uint32_t d, mul, shr;
+    __host__ void set(uint32_t div)
+    {
+        d = div;
+        if (div <= 1) {
+            mul = 0;
+            shr = 0;
+            return;
+        }
+        uint32_t lg = 0;
+        while ((1u << lg) < div) ++lg;  // ceil(log2 div), 1..31
+        const unsigned long long pw = 1ull << (31 + lg);
+        mul = static_cast<uint32_t>((pw + div - 1) / div);
+        shr = lg - 1;
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return d <= 1 ? n : __umulhi(n, mul) >> shr; }
+    __device__ __forceinline__ uint32_t divmod(uint32_t n, uint32_t &rem) const
+    {
+        const uint32_t q = div(n);
+        rem = n - q * d;
+        return q;
+    }
+};
 
 // ---------------------------------------------------------------------------------- block helpers
 __device__ __forceinline__ float warp_max(float v)
@@ -471,6 +603,11 @@ struct NvtxRange {
 // so the library links against the CUDA runtime only.  Returns false if the driver refuses.
 bool encode_bf16_rows_sw128(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows,
                             bool promote_l2_256);
+
+// Encodes a 4-D map of 16-bit elements {cols, d1, d2, d3} with the given strides (in bytes) of the outer three
+// dimensions and a box of {64, b1, b2, b3}, 128-byte swizzle.  False if the driver refuses.
+bool encode_16bit_4d_sw128(CUtensorMap *map, const void *base, bool bf16, const uint64_t (&dims)[4],
+                           const uint64_t (&strides)[3], uint32_t b1, uint32_t b2, uint32_t b3);
 
 bool is_sm100(int *sm_count);
 
