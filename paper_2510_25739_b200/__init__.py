@@ -23,5 +23,6 @@ _BINDING_NAMES = (
 def __getattr__(name):
     if name in _BINDING_NAMES:
         from . import binding
-        return getattr(binding, name)
+        value = globals()[name] = getattr(binding, name)  # later look-ups find it without this function
+        return value
     raise AttributeError(name)

@@ -555,111 +555,125 @@ _DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1}
 _NORM_CODES = {"none": 0, "rms": 1, "layer": 2}
 
 
-def _heads(t: torch.Tensor, name: str, like: torch.Tensor, shape):
-    """(pointer, row stride, head stride) of a [rows, heads, D] tensor whose last dimension is dense."""
-    if t.dtype != like.dtype:
-        raise TypeError(f"{name}: expected {like.dtype}, got {t.dtype}")
-    if t.shape != shape:
+def _refuse(t: torch.Tensor, name: str, dtype, shape, index: int, dense: bool) -> None:
+    """Says what is wrong with a tensor that a call's own quick test did not take."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device != like.device:
-        raise ValueError(f"{name}: must be on {like.device}")
-    a, b, c = t.stride()
-    if c != 1:
-        raise ValueError(f"{name}: the head dimension must be contiguous")
-    return t.data_ptr(), a, b
+    if t.get_device() != index:
+        raise ValueError(f"{name}: must be on cuda:{index}, is on {t.device}")
+    raise ValueError(f"{name}: must be contiguous" if dense else f"{name}: the head dimension must be contiguous")
 
 
-def _dense(t: Optional[torch.Tensor], name: str, dtype, shape, device):
+# The three calls below run once a layer on tensors of a few kilobytes, so what they cost on the host counts: a tensor
+# is looked at once, in one expression, and only a refusal takes the time to say why.
+def _heads(t: torch.Tensor, name: str, dtype, shape, index: int):
+    """(pointer, row stride, head stride) of a [rows, heads, D] tensor whose last dimension is dense."""
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or st[2] != 1:
+        _refuse(t, name, dtype, shape, index, False)
+    return t.data_ptr(), st[0], st[1]
+
+
+def _dense(t: Optional[torch.Tensor], name: str, dtype, shape, index: int):
     """Pointer of a contiguous tensor, None for None."""
     if t is None:
         return None
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{name}: must be on {device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: must be contiguous")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        _refuse(t, name, dtype, shape, index, True)
     return t.data_ptr()
 
 
-def _call(name: str, args: ctypes.Structure, dev_status: Optional[torch.Tensor], device) -> None:
-    """Runs an entry point on `device` and its current stream."""
-    fn = getattr(load_library(), name)
-    status = _dense(dev_status, "dev_status", torch.int32, (1,), device)
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            rc = fn(ctypes.byref(args), status, torch.cuda.current_stream().cuda_stream)
+def _call(name: str, args: ctypes.Structure, dev_status: Optional[torch.Tensor], index: int) -> None:
+    """Runs an entry point on GPU `index` and its current stream."""
+    fn = getattr(_lib or load_library(), name)
+    status = None if dev_status is None else _dense(dev_status, "dev_status", torch.int32, (1,), index)
+    stream = torch._C._cuda_getCurrentRawStream(index)  # (a Stream object costs 3 us)
+    if index == torch.cuda.current_device():
+        rc = fn(ctypes.byref(args), status, stream)
     else:
-        rc = fn(ctypes.byref(args), status, torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(index):
+            rc = fn(ctypes.byref(args), status, stream)
     if rc != 0:
         raise HawkError(rc, name)
 
 
-def _cuda_16bit(t: torch.Tensor, name: str) -> int:
-    if not t.is_cuda:
+def _cuda_16bit(t: torch.Tensor, name: str):
+    """(dtype code, GPU index) of the tensor that decides both for a call."""
+    index = t.get_device()
+    if index < 0:
         raise ValueError(f"{name}: must be a CUDA tensor")
     code = _DTYPE_CODES.get(t.dtype)
     if code is None:
         raise TypeError(f"{name}: expected torch.bfloat16 or torch.float16, got {t.dtype}")
-    return code
+    return code, index
 
 
-def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, like: torch.Tensor, H_kv: int, D: int):
+def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, dtype, H_kv: int, D: int, index: int):
     """Page count, page size, pointers and strides (page, head, row) of the two [n_pages, H_kv, page_size, D] tensors."""
-    n_pages, page_size = k_pages.shape[0], k_pages.shape[2]
-    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-        if t.dtype != like.dtype:
-            raise TypeError(f"{name}: expected {like.dtype}, got {t.dtype}")
-        if t.shape != (n_pages, H_kv, page_size, D):
-            raise ValueError(f"{name}: expected shape {(n_pages, H_kv, page_size, D)}, got {tuple(t.shape)}")
-        if t.device != like.device:
-            raise ValueError(f"{name}: must be on {like.device}")
-        if t.stride(3) != 1:
-            raise ValueError(f"{name}: the head dimension must be contiguous")
-    return n_pages, page_size, k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride()[:3] + v_pages.stride()[:3]
+    shape = k_pages.shape
+    if len(shape) != 4:
+        raise ValueError(f"k_pages: expected [n_pages, H_kv, page_size, D], got {tuple(shape)}")
+    n_pages, _, page_size, _ = shape
+    ks, vs = k_pages.stride(), v_pages.stride()
+    want = (n_pages, H_kv, page_size, D)
+    if k_pages.dtype is not dtype or shape != want or k_pages.get_device() != index or ks[3] != 1:
+        _refuse(k_pages, "k_pages", dtype, want, index, False)
+    if v_pages.dtype is not dtype or v_pages.shape != want or v_pages.get_device() != index or vs[3] != 1:
+        _refuse(v_pages, "v_pages", dtype, want, index, False)
+    return n_pages, page_size, (k_pages.data_ptr(), v_pages.data_ptr(), *ks[:3], *vs[:3])
+
+
+_ABSENT = (None, 0, 0)
 
 
 def _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved, q_out, k_out, dense_k):
-    """QkRopeArgs and the output tensors (allocated where none was given)."""
+    """QkRopeArgs, the output tensors (allocated where none was given), the GPU and (T, D)."""
     x = k if q is None else q
-    code = _cuda_16bit(x, "k" if q is None else "q")
-    dev, dt = x.device, x.dtype
+    code, index = _cuda_16bit(x, "k" if q is None else "q")
+    dt = x.dtype
     T, _, D = x.shape
-    if norm not in _NORM_CODES:
+    kind = _NORM_CODES.get(norm)
+    if kind is None:
         raise ValueError(f"norm: expected one of {tuple(_NORM_CODES)}, got {norm!r}")
     H = H_kv = n_pos = rot = per_head = 0
-    qp = qop = kp = kop = (None, 0, 0)
+    qp = qop = kp = kop = _ABSENT
     if q is not None:
-        H = q.shape[1]
-        qp = _heads(q, "q", x, (T, H, D))
+        shape = q.shape
+        H = shape[1]
+        qp = _heads(q, "q", dt, shape, index)
         if q_out is None:
-            q_out = torch.empty((T, H, D), dtype=dt, device=dev)
-        qop = _heads(q_out, "q_out", x, (T, H, D))
+            q_out = torch.empty(shape, dtype=dt, device=x.device)
+        qop = _heads(q_out, "q_out", dt, shape, index)
     if k is not None:
         H_kv = k.shape[1]
-        kp = _heads(k, "k", x, (T, H_kv, D))
+        shape = (T, H_kv, D)
+        kp = _heads(k, "k", dt, shape, index)
         if dense_k:
             if k_out is None:
-                k_out = torch.empty((T, H_kv, D), dtype=dt, device=dev)
-            kop = _heads(k_out, "k_out", x, (T, H_kv, D))
-    if norm != "none":
-        first = next((w for w in (q_weight, k_weight) if w is not None), None)
-        per_head = int(first is not None and first.dim() == 2)
+                k_out = torch.empty(shape, dtype=dt, device=x.device)
+            kop = _heads(k_out, "k_out", dt, shape, index)
+    wq = wk = bq = bk = cs = pos = None
+    if kind:
+        first = k_weight if q_weight is None else q_weight
+        per_head = 0 if first is None else first.dim() - 1
         qs, ks = ((H, D), (H_kv, D)) if per_head else ((D,), (D,))
-        weights = (_dense(q_weight, "q_weight", dt, qs, dev), _dense(k_weight, "k_weight", dt, ks, dev),
-                   _dense(q_bias, "q_bias", dt, qs, dev), _dense(k_bias, "k_bias", dt, ks, dev))
-    else:
-        weights = (None, None, None, None)
+        wq = _dense(q_weight, "q_weight", dt, qs, index)
+        wk = _dense(k_weight, "k_weight", dt, ks, index)
+        if q_bias is not None:
+            bq = _dense(q_bias, "q_bias", dt, qs, index)
+        if k_bias is not None:
+            bk = _dense(k_bias, "k_bias", dt, ks, index)
     if cos_sin is not None:
-        n_pos, rot = cos_sin.shape
-        cs = _dense(cos_sin, "cos_sin", torch.float32, (n_pos, rot), dev)
-        pos = _dense(position, "position", torch.int32, (T,), dev)
-    else:
-        cs = pos = None
-    return QkRopeArgs(code, T, H, H_kv, D, _NORM_CODES[norm], per_head, rot, n_pos, bool(interleaved), eps, qp[0], kp[0], qop[0], kop[0],
-                      qp[1], qp[2], kp[1], kp[2], qop[1], qop[2], kop[1], kop[2], *weights, pos, cs), q_out, k_out, x
+        if position is None:
+            raise ValueError("position: needed with cos_sin")
+        shape = cos_sin.shape
+        n_pos, rot = shape
+        cs = _dense(cos_sin, "cos_sin", torch.float32, shape, index)
+        pos = _dense(position, "position", torch.int32, (T,), index)
+    return QkRopeArgs(code, T, H, H_kv, D, kind, per_head, rot, n_pos, 1 if interleaved else 0, eps, qp[0], kp[0], qop[0], kop[0],
+                      qp[1], qp[2], kp[1], kp[2], qop[1], qop[2], kop[1], kop[2], wq, wk, bq, bk, pos, cs), q_out, k_out, index, dt, T, D
 
 
 def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], position: Optional[torch.Tensor],
@@ -673,9 +687,9 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], position:
     position int32 [T]; None for both: no rotation.  Weights and biases are [D], or [heads, D] one for each head."""
     if q is None and k is None:
         raise ValueError("q, k: one of them is needed")
-    args, q_out, k_out, x = _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved,
-                                       q_out, k_out, True)
-    _call("hawk_qk_norm_rope", args, dev_status, x.device)
+    args, q_out, k_out, index, _, _, _ = _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias,
+                                                    interleaved, q_out, k_out, True)
+    _call("hawk_qk_norm_rope", args, dev_status, index)
     return q_out, k_out
 
 
@@ -688,18 +702,18 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos
     """New rows k, v [T,H_kv,D] into k_pages, v_pages [n_pages,H_kv,page_size,D] (any page, head and row strides), k normalised
     and rotated as by qk_norm_rope; q [T,H,D] goes the same way into q_out, which is returned.  Stream s owns rows
     row_begin[s] .. row_begin[s+1]-1; kv_len [S] counts its keys with the new ones; block_table [S, pages a stream]."""
-    args, q_out, _, x = _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved, q_out,
-                                   None, False)
-    dev = x.device
-    T, H_kv, D = k.shape
-    vp = _heads(v, "v", x, (T, H_kv, D))
-    n_pages, page_size, kpp, vpp, strides = _pages(k_pages, v_pages, x, H_kv, D)
-    S, width = block_table.shape
-    full = RopeAppendArgs(args, *vp, kpp, vpp, *strides, n_pages, page_size, S, width,
-                          _dense(block_table, "block_table", torch.int32, (S, width), dev),
-                          _dense(row_begin, "row_begin", torch.int32, (S + 1,), dev),
-                          _dense(kv_len, "kv_len", torch.int32, (S,), dev))
-    _call("hawk_rope_append", full, dev_status, dev)
+    args, q_out, _, index, dt, T, D = _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias,
+                                                 interleaved, q_out, None, False)
+    H_kv = args.H_kv
+    vp = _heads(v, "v", dt, (T, H_kv, D), index)
+    n_pages, page_size, pages = _pages(k_pages, v_pages, dt, H_kv, D, index)
+    shape = block_table.shape
+    S, width = shape
+    full = RopeAppendArgs(args, *vp, *pages, n_pages, page_size, S, width,
+                          _dense(block_table, "block_table", torch.int32, shape, index),
+                          _dense(row_begin, "row_begin", torch.int32, (S + 1,), index),
+                          _dense(kv_len, "kv_len", torch.int32, (S,), index))
+    _call("hawk_rope_append", full, dev_status, index)
     return q_out
 
 
@@ -714,30 +728,33 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, bl
     """Attention of the new rows q [T,H,D] over the paged cache that already holds their keys (rope_append) -> out [T,H*D].
     max_new and max_kv bound the rows a stream brings and its keys.  With anc_mask (int64 tensor holding the uint64 masks,
     [max_new]) the rows of a stream are nodes of a candidate tree.  Rows of no stream are left as they are in `out`."""
-    code = _cuda_16bit(q, "q")
-    dev = q.device
-    T, H, D = q.shape
+    code, index = _cuda_16bit(q, "q")
+    dt = q.dtype
+    shape = q.shape
+    T, H, D = shape
+    qp = _heads(q, "q", dt, shape, index)
     H_kv = k_pages.shape[1]
-    qp = _heads(q, "q", q, (T, H, D))
-    n_pages, page_size, kpp, vpp, strides = _pages(k_pages, v_pages, q, H_kv, D)
-    S, width = block_table.shape
+    n_pages, page_size, pages = _pages(k_pages, v_pages, dt, H_kv, D, index)
+    shape = block_table.shape
+    S, width = shape
     if out is None:
-        out = torch.empty((T, H * D), dtype=q.dtype, device=dev)
+        out = torch.empty((T, H * D), dtype=dt, device=q.device)
+    ws, ws_bytes = None, 0
     if workspace is None:
-        need = load_library().hawk_paged_attn_workspace_bytes(S, T, max_new, H, H_kv, D, max_kv)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    elif workspace.device != dev or not workspace.is_contiguous():
-        raise ValueError(f"workspace: must be contiguous and on {dev}")
-    args = PagedAttnArgs(code, S, T, max_new, max_kv, H, H_kv, D, n_pages, page_size, width, sm_scale, *qp, kpp, vpp, *strides,
-                         _dense(block_table, "block_table", torch.int32, (S, width), dev),
-                         _dense(row_begin, "row_begin", torch.int32, (S + 1,), dev),
-                         _dense(kv_len, "kv_len", torch.int32, (S,), dev),
-                         _dense(anc_mask, "anc_mask", torch.int64, (max_new,), dev),
-                         _dense(out, "out", q.dtype, (T, H * D), dev),
-                         None if workspace is None else workspace.data_ptr(),
-                         0 if workspace is None else workspace.numel() * workspace.element_size())
-    _call("hawk_paged_attn", args, dev_status, dev)
+        ws_bytes = (_lib or load_library()).hawk_paged_attn_workspace_bytes(S, T, max_new, H, H_kv, D, max_kv)
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            ws = workspace.data_ptr()
+    else:
+        ws = _dense(workspace, "workspace", workspace.dtype, workspace.shape, index)
+        ws_bytes = workspace.numel() * workspace.element_size()
+    args = PagedAttnArgs(code, S, T, max_new, max_kv, H, H_kv, D, n_pages, page_size, width, sm_scale, *qp, *pages,
+                         _dense(block_table, "block_table", torch.int32, shape, index),
+                         _dense(row_begin, "row_begin", torch.int32, (S + 1,), index),
+                         _dense(kv_len, "kv_len", torch.int32, (S,), index),
+                         _dense(anc_mask, "anc_mask", torch.int64, (max_new,), index),
+                         _dense(out, "out", dt, (T, H * D), index), ws, ws_bytes)
+    _call("hawk_paged_attn", args, dev_status, index)
     return out
 
 
