@@ -21,18 +21,19 @@ namespace {
 
 using namespace hawk;
 
-// Launch shapes (WARPS pipelines per block, STAGES tiles deep, 8 KB a stage):
-//   shares: 8 x 3, one block per SM; items may be cut, the merge kernel follows.
-//   whole : 3 x 8, one warp per item: few short items, nothing to merge.
-//   group : 4 x 2, three blocks per SM, one item per block, its four warps merge in shared memory.
-constexpr int kWarpsShares = 8, kStagesShares = 3;
-constexpr int kWarpsWhole = 3, kStagesWhole = 8;
-constexpr int kWarpsGroup = 4, kStagesGroup = 2;
-constexpr int kWholeMaxTiles = 6;    // longest item that one warp takes alone
+// Launch shapes (WARPS pipelines per block, STAGES tiles deep, 8 KB a stage).
+//   shares: one block per SM, every warp an equal share of the list; items may be cut, the merge kernel follows.  Items
+//           of one 8-row column tile leave registers for 12 warps of 2 stages, wider ones for 8 of 3.
+//   group : one item per block, split evenly over its warps, which merge in shared memory.  8 warps of 3 stages and one
+//           block per SM, or (one column tile) 4 of 2 and three blocks per SM.
+// group needs no second kernel and no partial results in memory, so it is taken whenever the items fit the GPU at once
+// and are not so few and long that most SMs would idle (plan_rows has the rule and what both sides measured).
+__host__ __device__ constexpr int shares_warps(int nqt) { return nqt == 1 ? 12 : 8; }
+__host__ __device__ constexpr int shares_stages(int nqt) { return nqt == 1 ? 2 : 3; }
 constexpr int kMinShareTiles = 2;    // shorter shares would only add partial results to merge
+constexpr float kLazy = 8.f;         // log2 units by which a score may exceed the softmax shift
 constexpr int kStageBytes = 8192;
 constexpr int kMaxStreams = 4096;    // the prefix sum is held in shared memory
-constexpr int kWorkersMax = hawk_host::kPagedSms * kWarpsShares;
 constexpr int kRecordInts = 8;       // start tile, tiles of the item, first row, rows, kv head, row chunk, total tiles, workers
 
 template <int D>
@@ -51,11 +52,11 @@ constexpr size_t rows_smem(int warps, int stages, int S)
            (static_cast<size_t>(S) + 1) * sizeof(int);
 }
 
-// Position in the list of tiles: stream, item of the stream (kv head, row chunk), tile of the item.
+// Position in the list of tiles: stream, kv head, row chunk, tile of that item.
 struct Cursor {
-    int s, it, tile;
-    int r0, n, kv, nt, items;  // of the stream
-    int left;                  // tiles left in the share, this one included
+    int s, hk, chunk, tile;
+    int r0, n, kv, nt, chunks;  // of the stream
+    int left;                   // tiles left in the share, this one included
 };
 
 template <int D>
@@ -78,20 +79,20 @@ __device__ __forceinline__ void enter_stream(Cursor &c, const PagedParams &P, in
     c.n = st.n;
     c.kv = st.kv;
     c.nt = tiles_of<D>(st.kv);
-    c.items = items_of<D, RPI>(P, st);
+    c.chunks = (st.n * P.group + RPI - 1) / RPI;
 }
 
 __device__ __forceinline__ long long share_begin(long long g, long long T, int W) { return g * T / W; }
 
-template <typename T16, int D, int NQT, int kWarps, int kStages>
-__global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
+template <typename T16, int D, int NQT, int kWarps, int kStages, bool kGroup>
+__global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
     paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                       const PagedParams P)
 {
     using C = Tile<D>;
     using E = Elem<T16>;
     constexpr int TK = C::kKeys, KB = TK / 16, DB = D / 16, RPI = NQT * 8;
-    constexpr bool kShares = kWarps == kWarpsShares, kGroup = kWarps == kWarpsGroup;
+    constexpr bool kShares = !kGroup;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kWarps * kStages * kStageBytes);
@@ -110,7 +111,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
     }
     grid_dependency_wait();
 
-    // ---- prefix sum over the streams: of their tiles (shares) or of their items (whole, group)
+    // ---- prefix sum over the streams: of their tiles (shares) or of their items (group)
     int flags = 0;
     int running = 0;
     for (int base = 0; base < P.S; base += kWarps * 32) {
@@ -155,12 +156,12 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
             len = static_cast<int>(share_begin(w + 1, total, W)) - f;
         }
     } else {
-        w = f = kGroup ? static_cast<int>(blockIdx.x) : warp * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+        w = f = static_cast<int>(blockIdx.x);
         len = w < total ? 1 : 0;
     }
     Cursor cc;
-    cc.s = cc.it = cc.tile = cc.left = cc.r0 = cc.n = cc.kv = cc.items = 0;
-    cc.nt = 1;
+    cc.s = cc.hk = cc.chunk = cc.tile = cc.left = cc.r0 = cc.n = cc.kv = 0;
+    cc.nt = cc.chunks = 1;
     if (len > 0) {
         int lo = 0, hi = P.S;  // prefix[lo] <= f < prefix[hi]
         while (hi - lo > 1) {
@@ -170,26 +171,23 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
         }
         cc.s = lo;
         enter_stream<D, RPI>(cc, P, flags);
-        const int loc = f - prefix[lo];
+        int item = f - prefix[lo];
         if (kShares) {
-            cc.it = loc / cc.nt;
-            cc.tile = loc - cc.it * cc.nt;
+            const int loc = item;
+            item = loc / cc.nt;
+            cc.tile = loc - item * cc.nt;
             cc.left = len;
         } else {
-            cc.it = loc;
-            if (kGroup) {
-                cc.tile = static_cast<int>(static_cast<long long>(cc.nt) * warp / kWarps);
-                cc.left = static_cast<int>(static_cast<long long>(cc.nt) * (warp + 1) / kWarps) - cc.tile;
-            } else {
-                cc.left = cc.nt;
-            }
+            cc.tile = static_cast<int>(static_cast<long long>(cc.nt) * warp / kWarps);
+            cc.left = static_cast<int>(static_cast<long long>(cc.nt) * (warp + 1) / kWarps) - cc.tile;
         }
+        cc.hk = item / cc.chunks;
+        cc.chunk = item - cc.hk * cc.chunks;
     }
     if (kShares && lane == 0) {
         int32_t *rec = P.records + static_cast<size_t>(w) * kRecordInts;
-        const int chunks = max(1, (cc.n * P.group + RPI - 1) / RPI);
         *reinterpret_cast<int4 *>(rec) = make_int4(cc.tile, cc.nt, cc.r0, cc.n);
-        *reinterpret_cast<int4 *>(rec + 4) = make_int4(cc.it / chunks, cc.it % chunks, total, W);
+        *reinterpret_cast<int4 *>(rec + 4) = make_int4(cc.hk, cc.chunk, total, W);
     }
     if (!kGroup && cc.left == 0) return;
     const Cursor head = cc;  // group shape: the block's item
@@ -205,11 +203,14 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
         ++c.tile;
         if (c.tile == c.nt && c.left > 0) {
             c.tile = 0;
-            if (++c.it == c.items) {
-                c.it = 0;
-                do ++c.s;
-                while (prefix[c.s + 1] == prefix[c.s]);  // (ends: tiles are left)
-                enter_stream<D, RPI>(c, P, flags);
+            if (++c.chunk == c.chunks) {
+                c.chunk = 0;
+                if (++c.hk == P.H_kv) {
+                    c.hk = 0;
+                    do ++c.s;
+                    while (prefix[c.s + 1] == prefix[c.s]);  // (ends: tiles are left)
+                    enter_stream<D, RPI>(c, P, flags);
+                }
             }
         }
     };
@@ -241,33 +242,39 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
         }
         return __shfl_sync(0xffffffffu, pg_cur, pg - pg_base);
     };
-    const int boxes = TK / P.box_rows;
+    int box_pg = 0, box_row = 0;  // page index and row in it of the next box
+    if (cc.left > 0) {
+        uint32_t row;
+        box_pg = static_cast<int>(P.div_page.divmod(static_cast<uint32_t>(cc.tile) * TK, row));
+        box_row = static_cast<int>(row);
+    }
     bool first_issue = true;
     auto issue = [&](const Cursor &c, int st) {
-        const int chunks = (c.n * P.group + RPI - 1) / RPI;
-        const int hk = c.it / chunks;
-        const int key0 = c.tile * TK;
-        const int live = max(0, min(boxes, (c.kv - key0 + P.box_rows - 1) / P.box_rows));
+        if (c.tile == 0) box_pg = box_row = 0;
+        const int bytes_box = P.box_rows * 128;
+        const int live = max(0, min(TK, c.kv - c.tile * TK) + P.box_rows - 1) & -P.box_rows;  // rows of the boxes to load
         uint8_t *kd = ring + st * kStageBytes;
         uint8_t *vd = kd + C::kHalves * C::kSubBytes;
         if (lane == 0) {
             // (test builds only: the first tile of the first share is armed for more bytes than arrive)
             const bool stall = kTestStallBytes != 0 && blockIdx.x == 0 && warp == 0 && first_issue;
-            mbar_arrive_expect_tx(&full_bar[st], live * P.box_rows * 128 * 2 * C::kHalves + (stall ? kTestStallBytes : 0u));
+            mbar_arrive_expect_tx(&full_bar[st], live * 128 * 2 * C::kHalves + (stall ? kTestStallBytes : 0u));
         }
         first_issue = false;
-        for (int b = 0; b < live; ++b) {
-            uint32_t row;
-            const int pg = static_cast<int>(P.div_page.divmod(static_cast<uint32_t>(key0 + b * P.box_rows), row));
-            const int id = page_of(c, pg);
+        for (int off = 0; off < live * 128; off += bytes_box) {
+            const int id = page_of(c, box_pg);
             if (id < 0 || id >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;  // (outside the tensor map: zeros)
             if (lane == 0) {
 #pragma unroll
                 for (int hf = 0; hf < C::kHalves; ++hf) {
-                    const int off = hf * C::kSubBytes + b * P.box_rows * 128;
-                    paged_load(kd + off, &map_k, P.k_rows_inner, hf, static_cast<int>(row), hk, id, &full_bar[st], policy);
-                    paged_load(vd + off, &map_v, P.v_rows_inner, hf, static_cast<int>(row), hk, id, &full_bar[st], policy);
+                    paged_load(kd + hf * C::kSubBytes + off, &map_k, P.k_rows_inner, hf, box_row, c.hk, id, &full_bar[st], policy);
+                    paged_load(vd + hf * C::kSubBytes + off, &map_v, P.v_rows_inner, hf, box_row, c.hk, id, &full_bar[st], policy);
                 }
+            }
+            box_row += P.box_rows;
+            if (box_row >= P.page_size) {
+                box_row = 0;
+                ++box_pg;
             }
         }
     };
@@ -351,7 +358,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
         // group shape: the ring is free by now (every copy issued has been consumed) and takes the partial
         float *ps = kGroup ? reinterpret_cast<float *>(ring)
                            : P.part + (static_cast<size_t>(w) * 2 + (seg_first ? 0 : 1)) * RPI * (D + 2);
-        static_assert(RPI * (D + 2) * 4 <= kStagesGroup * kStageBytes, "a partial fits the ring");
+        static_assert(!kGroup || RPI * (D + 2) * 4 <= kStages * kStageBytes, "a partial fits the ring");
         if (kGroup && lane == 0) has_part[warp] = 1;
 #pragma unroll
         for (int nq = 0; nq < NQT; ++nq)
@@ -378,9 +385,8 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
         if (!open) {
             // ---- a new segment: this item's queries, empty state
             open = true;
-            const int chunks = (cc.n * P.group + RPI - 1) / RPI;
-            hk = cc.it / chunks;
-            row0 = (cc.it - hk * chunks) * RPI;
+            hk = cc.hk;
+            row0 = cc.chunk * RPI;
             nrows = min(RPI, cc.n * P.group - row0);
             seg_r0 = cc.r0;
             seg_tile = cc.tile;
@@ -446,46 +452,56 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
                     }
                 }
         }
-        // ---- running softmax per row, base 2
+        // ---- running softmax per row, base 2.  The shift m may be any number as long as o, the sum and p share it; it
+        // is renewed only when a score exceeds it by more than kLazy, so that almost every tile goes without the
+        // reduction across lanes and without touching o (p stays below 2^kLazy: far inside fp16, bf16 and fp32)
+        bool grows = false;
+        float mx[NQT][2];
+#pragma unroll
+        for (int nq = 0; nq < NQT; ++nq) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float m = -CUDART_INF_F;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) m = fmaxf(m, fmaxf(sc[nq][kb][c], sc[nq][kb][2 + c]));
+                mx[nq][c] = m * P.scale_log2;
+                grows |= mx[nq][c] > mrun[nq][c] + kLazy;
+            }
+        }
+        if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+            for (int nq = 0; nq < NQT; ++nq)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float m = mx[nq][c];
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    m = fmaxf(m, mrun[nq][c]);
+                    const float a = fast_exp2(mrun[nq][c] - (m == -CUDART_INF_F ? 0.f : m));
+                    mrun[nq][c] = m;
+                    lrun[nq][c] *= a;
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        ot[nq][db][c] *= a;
+                        ot[nq][db][2 + c] *= a;
+                    }
+                }
+        }
         uint32_t pb[NQT][KB][2];
 #pragma unroll
         for (int nq = 0; nq < NQT; ++nq) {
-            float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                mx0 = fmaxf(mx0, fmaxf(sc[nq][kb][0], sc[nq][kb][2]));
-                mx1 = fmaxf(mx1, fmaxf(sc[nq][kb][1], sc[nq][kb][3]));
-            }
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) {
-                mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
-                mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
-            }
-            const float mn0 = fmaxf(mrun[nq][0], mx0 * P.scale_log2), mn1 = fmaxf(mrun[nq][1], mx1 * P.scale_log2);
-            const float mu0 = mn0 == -CUDART_INF_F ? 0.f : mn0, mu1 = mn1 == -CUDART_INF_F ? 0.f : mn1;
-            const float a0 = fast_exp2(mrun[nq][0] - mu0), a1 = fast_exp2(mrun[nq][1] - mu1);
-            mrun[nq][0] = mn0;
-            mrun[nq][1] = mn1;
-            float s0 = 0.f, s1 = 0.f;
+            const float mu0 = mrun[nq][0] == -CUDART_INF_F ? 0.f : mrun[nq][0];
+            const float mu1 = mrun[nq][1] == -CUDART_INF_F ? 0.f : mrun[nq][1];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const float p0 = fast_exp2(fmaf(sc[nq][kb][0], P.scale_log2, -mu0));
                 const float p1 = fast_exp2(fmaf(sc[nq][kb][1], P.scale_log2, -mu1));
                 const float p2 = fast_exp2(fmaf(sc[nq][kb][2], P.scale_log2, -mu0));
                 const float p3 = fast_exp2(fmaf(sc[nq][kb][3], P.scale_log2, -mu1));
-                s0 += p0 + p2;
-                s1 += p1 + p3;
+                lrun[nq][0] += p0 + p2;
+                lrun[nq][1] += p1 + p3;
                 pb[nq][kb][0] = movmatrix_trans(E::pack(p0, p1));
                 pb[nq][kb][1] = movmatrix_trans(E::pack(p2, p3));
-            }
-            lrun[nq][0] = lrun[nq][0] * a0 + s0;
-            lrun[nq][1] = lrun[nq][1] * a1 + s1;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                ot[nq][db][0] *= a0;
-                ot[nq][db][1] *= a1;
-                ot[nq][db][2] *= a0;
-                ot[nq][db][3] *= a1;
             }
         }
         // ---- O^T += V^T P^T; values behind the last key hold anything (or are an earlier tile's): zeroed, 0 * NaN is NaN
@@ -546,10 +562,9 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
     if constexpr (kGroup) {
         // ---- the four warps' partial results of the block's item, folded in share order from shared memory
         __syncthreads();
-        if (head.items == 0) return;
+        if (head.n == 0) return;
         constexpr int PER = D / 32;
-        const int chunks = (head.n * P.group + RPI - 1) / RPI;
-        const int kvh = head.it / chunks, c_row0 = (head.it - kvh * chunks) * RPI;
+        const int kvh = head.hk, c_row0 = head.chunk * RPI;
         const int rows = min(RPI, head.n * P.group - c_row0);
         for (int r = warp; r < rows; r += kWarps) {
             float acc[PER];
@@ -577,68 +592,160 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == kWarpsGroup ? 3 : 1)
     }
 }
 
-// Merges the items that were cut: one warp per (worker, row).  Worker g stands for the item its share starts inside of, if
-// its predecessor's share holds that item's first tile; the item's contributions are the predecessor's last segment and
-// the first segments of g, g + 1, ... until its tiles are used up.  Everything comes from the records.
+// Merges the items that were cut.  Worker g stands for the item its share starts inside of, if its predecessor's share
+// holds that item's first tile; contribution 0 is the predecessor's last segment, contribution c the first segment of
+// worker g + c - 1, until the item's tiles are used up.  Everything comes from the records.
+// A block looks at 8 neighbouring workers and deals its 8 warps out to those among them that stand for an item: one warp
+// each when all do (items shorter than a share: two contributions), all 8 on one item when it is the only one (an item
+// spread over dozens of shares), joined in shared memory.  A warp takes 8 rows (4 at D = 128: registers), its lanes across the head dimension, and has
+// two contributions' loads under way at a time.  (One warp per worker and row instead, 1775 to 3549 blocks most of which
+// only looked at a record, took 5 us at 8 rows an item and 8 us at 24.)
+constexpr int kMergeWorkers = 8;
+__host__ __device__ constexpr int merge_rows(int D) { return D == 64 ? 8 : 4; }
+
 template <typename T16, int D, int RPI>
-__global__ void __launch_bounds__(256) paged_merge_kernel(const PagedParams P)
+__global__ void __launch_bounds__(256, 3) paged_merge_kernel(const PagedParams P)
 {
     using E = Elem<T16>;
-    constexpr int PER = D / 32;
+    constexpr int PER = D / 32, RW = merge_rows(D);
+    __shared__ float joined[8][RW * (D + 2)];
     allow_dependent_launch();
-    const int wid = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
-    const int g = wid / RPI + 1, r = wid % RPI;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g0 = blockIdx.x * kMergeWorkers + 1, r0g = blockIdx.y * RW;  // first worker, first row of the item
     grid_dependency_wait();
-    if (g >= kWorkersMax) return;
-    const int4 a = *reinterpret_cast<const int4 *>(P.records + static_cast<size_t>(g) * kRecordInts);
-    const int4 b = *reinterpret_cast<const int4 *>(P.records + static_cast<size_t>(g) * kRecordInts + 4);
-    const int tile = a.x, nt = a.y, r0 = a.z, n = a.w, hk = b.x, row0 = b.y * RPI, total = b.z, W = b.w;
-    if (g >= W || tile == 0 || r >= min(RPI, n * P.group - row0)) return;
-    const int sb = static_cast<int>(share_begin(g, total, W));
-    const int before = sb - static_cast<int>(share_begin(g - 1, total, W));
-    if (tile > before) return;  // an earlier boundary of the same item merges it
+    // lane i < 8 looks at worker g0 + i
+    const int mine = g0 + (lane & 7);
+    int4 a = make_int4(0, 1, 0, 0), b = make_int4(0, 0, 0, 1);
+    if (mine < hawk_host::kPagedSms * shares_warps(RPI / 8)) {
+        a = *reinterpret_cast<const int4 *>(P.records + static_cast<size_t>(mine) * kRecordInts);
+        b = *reinterpret_cast<const int4 *>(P.records + static_cast<size_t>(mine) * kRecordInts + 4);
+    }
+    const int total = b.z, W = b.w;
+    const int sb = static_cast<int>(share_begin(mine, total, W));
+    const int before = sb - static_cast<int>(share_begin(mine - 1, total, W));
+    const bool stands = lane < 8 && mine < W && a.x > 0 && a.x <= before;
+    const unsigned act = __ballot_sync(0xffffffffu, stands);
+    const int n_act = __popc(act);
+    if (n_act == 0) return;
+    const int wpi = n_act == 1 ? 8 : n_act == 2 ? 4 : n_act <= 4 ? 2 : 1;  // warps per item
+    const int idx = warp / wpi, sub = warp - idx * wpi;
+    const bool work = idx < n_act;
+    const int src = work ? __fns(act, 0, idx + 1) : 0;
+    const int tile = __shfl_sync(0xffffffffu, a.x, src), nt = __shfl_sync(0xffffffffu, a.y, src);
+    const int first_row = __shfl_sync(0xffffffffu, a.z, src), n = __shfl_sync(0xffffffffu, a.w, src);
+    const int hk = __shfl_sync(0xffffffffu, b.x, src), row0 = __shfl_sync(0xffffffffu, b.y, src) * RPI + r0g;
+    const int sb_g = __shfl_sync(0xffffffffu, sb, src), before_g = __shfl_sync(0xffffffffu, before, src);
+    const int all = __shfl_sync(0xffffffffu, total, src), workers = __shfl_sync(0xffffffffu, W, src);
+    const int g = g0 + src, end = sb_g - tile + nt;  // one past the item's last tile in the list
+    const int rows = work ? min(RW, min(RPI, n * P.group - (row0 - r0g)) - r0g) : 0;
 
-    float acc[PER];
+    float acc[RW][PER], mm[RW], ll[RW];
 #pragma unroll
-    for (int c = 0; c < PER; ++c) acc[c] = 0.f;
-    float mm = -CUDART_INF_F, ll = 0.f;
-    auto fold = [&](int slot) {
-        const float *ps = P.part + static_cast<size_t>(slot) * RPI * (D + 2);
-        const float2 m_l = *reinterpret_cast<const float2 *>(ps + RPI * D + 2 * r);
-        float v[PER];
-        if constexpr (PER == 2) {
-            const float2 x = *reinterpret_cast<const float2 *>(ps + r * D + lane * PER);
-            v[0] = x.x;
-            v[1] = x.y;
-        } else {
-            const float4 x = *reinterpret_cast<const float4 *>(ps + r * D + lane * PER);
-            v[0] = x.x;
-            v[1] = x.y;
-            v[PER - 2] = x.z;
-            v[PER - 1] = x.w;
-        }
-        const float mn = fmaxf(mm, m_l.x);
-        const float mu = mn == -CUDART_INF_F ? 0.f : mn;
-        const float f_old = fast_exp2(mm - mu), f_new = fast_exp2(m_l.x - mu);
-        mm = mn;
-        ll = ll * f_old + m_l.y * f_new;
+    for (int r = 0; r < RW; ++r) {
+        mm[r] = -CUDART_INF_F;
+        ll[r] = 0.f;
 #pragma unroll
-        for (int c = 0; c < PER; ++c) acc[c] = acc[c] * f_old + v[c] * f_new;
+        for (int c = 0; c < PER; ++c) acc[r][c] = 0.f;
+    }
+    auto exists = [&](int c) {
+        if (c == 0) return true;
+        const int gg = g + c - 1;
+        return gg < workers && static_cast<int>(share_begin(gg, all, workers)) < end;
     };
-    fold((g - 1) * 2 + (tile == before ? 0 : 1));
-    const int end = sb - tile + nt;  // one past the item's last tile in the list
-    for (int gg = g; gg < W && static_cast<int>(share_begin(gg, total, W)) < end; ++gg) fold(gg * 2);
-    const float inv = ll == 0.f ? 0.f : 1.f / ll;
-    uint32_t hd;
-    const uint32_t pos = P.div_group.divmod(static_cast<uint32_t>(row0 + r), hd);
-    T16 *dst = static_cast<T16 *>(P.out) + ((r0 + static_cast<long long>(pos)) * P.H + hk * P.group + static_cast<int>(hd)) * D +
-               lane * PER;
+    auto slot_of = [&](int c) {
+        const int slot = c == 0 ? (g - 1) * 2 + (tile == before_g ? 0 : 1) : (g + c - 1) * 2;
+        return P.part + static_cast<size_t>(slot) * RPI * (D + 2);
+    };
+    struct Piece {
+        float2 ml;  // lane r: of row r
+        float v[RW][PER];
+    };
+    auto fetch = [&](Piece &p, const float *ps) {
+        p.ml = make_float2(-CUDART_INF_F, 0.f);
+        if (lane < rows) p.ml = *reinterpret_cast<const float2 *>(ps + RPI * D + 2 * (r0g + lane));
 #pragma unroll
-    for (int c = 0; c < PER; c += 2) *reinterpret_cast<uint32_t *>(dst + c) = E::pack(acc[c] * inv, acc[c + 1] * inv);
+        for (int r = 0; r < RW; ++r) {
+            if (r < rows) {
+                const float *pr = ps + (r0g + r) * D + lane * PER;
+                if constexpr (PER == 2) {
+                    const float2 x = *reinterpret_cast<const float2 *>(pr);
+                    p.v[r][0] = x.x;
+                    p.v[r][1] = x.y;
+                } else {
+                    const float4 x = *reinterpret_cast<const float4 *>(pr);
+                    p.v[r][0] = x.x;
+                    p.v[r][1] = x.y;
+                    p.v[r][PER - 2] = x.z;
+                    p.v[r][PER - 1] = x.w;
+                }
+            }
+        }
+    };
+    auto fold_row = [&](int r, float m, float l, const float (&v)[PER]) {
+        const float mn = fmaxf(mm[r], m);
+        const float mu = mn == -CUDART_INF_F ? 0.f : mn;
+        const float f_old = fast_exp2(mm[r] - mu), f_new = fast_exp2(m - mu);
+        mm[r] = mn;
+        ll[r] = ll[r] * f_old + l * f_new;
+#pragma unroll
+        for (int c = 0; c < PER; ++c) acc[r][c] = acc[r][c] * f_old + v[c] * f_new;
+    };
+    auto fold = [&](const Piece &p) {
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+            const float m = __shfl_sync(0xffffffffu, p.ml.x, r), l = __shfl_sync(0xffffffffu, p.ml.y, r);
+            if (r < rows) fold_row(r, m, l, p.v[r]);
+        }
+    };
+    if (rows > 0) {
+        for (int c = sub; exists(c); c += 2 * wpi) {
+            Piece p0, p1;
+            const bool two = exists(c + wpi);
+            fetch(p0, slot_of(c));
+            if (two) fetch(p1, slot_of(c + wpi));
+            fold(p0);
+            if (two) fold(p1);
+        }
+    }
+    if (wpi > 1) {  // (block-uniform)
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+#pragma unroll
+            for (int c = 0; c < PER; ++c) joined[warp][r * D + lane * PER + c] = acc[r][c];
+            if (lane == 0) {
+                joined[warp][RW * D + 2 * r] = mm[r];
+                joined[warp][RW * D + 2 * r + 1] = ll[r];
+            }
+        }
+        __syncthreads();
+        if (sub > 0) return;
+        for (int o = 1; o < wpi; ++o) {
+            const float *j = joined[warp + o];
+#pragma unroll
+            for (int r = 0; r < RW; ++r) {
+                float v[PER];
+#pragma unroll
+                for (int c = 0; c < PER; ++c) v[c] = j[r * D + lane * PER + c];
+                fold_row(r, j[RW * D + 2 * r], j[RW * D + 2 * r + 1], v);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < RW; ++r) {
+        if (r >= rows) break;
+        const float inv = ll[r] == 0.f ? 0.f : 1.f / ll[r];
+        uint32_t hd;
+        const uint32_t pos = P.div_group.divmod(static_cast<uint32_t>(row0 + r), hd);
+        T16 *dst = static_cast<T16 *>(P.out) +
+                   ((first_row + static_cast<long long>(pos)) * P.H + hk * P.group + static_cast<int>(hd)) * D + lane * PER;
+#pragma unroll
+        for (int c = 0; c < PER; c += 2)
+            *reinterpret_cast<uint32_t *>(dst + c) = E::pack(acc[r][c] * inv, acc[r][c + 1] * inv);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- host side
-enum Shape { kShapeShares, kShapeWhole, kShapeGroup };
+enum Shape { kShapeShares, kShapeGroup4, kShapeGroup8 };
 
 struct RowsPlan {
     Shape shape;
@@ -656,12 +763,15 @@ RowsPlan plan_rows(int S, int rows, int H_kv, int D, int max_kv)
     const int tiles = max_kv < 1 ? 1 : (max_kv + tk - 1) / tk;
     p.shape = kShapeShares;
     p.grid = hawk_host::kPagedSms;
-    if (items <= hawk_host::kPagedSms * kWarpsWhole && tiles <= kWholeMaxTiles) {
-        p.shape = kShapeWhole;
-        p.grid = static_cast<int>(items < hawk_host::kPagedSms ? items : hawk_host::kPagedSms);
-    } else if (p.rpi <= 8 && items <= 3 * hawk_host::kPagedSms && 2 * items >= 3 * hawk_host::kPagedSms) {
-        // few items of one 8-row column tile, at least 222 and all resident at once
-        p.shape = kShapeGroup;
+    // at most one item per SM, a block each.  Shares spread the same tiles over all SMs but pay some 4 us for partial results
+    // and their merge: with 80 items of 8 rows at D = 64 blocks take 13.9 / 22.8 / 40.2 us at 65 / 129 / 257 tiles an item, shares
+    // 16.7 / 23.3 / 36.7; with 32 items the two cross at 65 tiles, with 144 they never do (97 against 103 us at 513)
+    if (items <= hawk_host::kPagedSms && (items >= 120 || tiles <= 40 + items)) {
+        p.shape = kShapeGroup8;
+        p.grid = static_cast<int>(items);
+    } else if (p.rpi <= 8 && items > hawk_host::kPagedSms && items <= 3 * hawk_host::kPagedSms) {
+        // (320 items of 36 tiles: 17.9 us against 22.8 as shares; 400 of 257: 131 against 142)
+        p.shape = kShapeGroup4;
         p.grid = static_cast<int>(items);
     }
     return p;
@@ -670,10 +780,10 @@ RowsPlan plan_rows(int S, int rows, int H_kv, int D, int max_kv)
 size_t rows_workspace_bytes(const RowsPlan &p, int D)
 {
     if (p.shape != kShapeShares) return 0;
-    return static_cast<size_t>(kWorkersMax) * (kRecordInts * sizeof(int32_t) + 2ull * p.rpi * (D + 2) * sizeof(float));
+    return static_cast<size_t>(hawk_host::kPagedSms) * shares_warps(p.rpi / 8) * (kRecordInts * sizeof(int32_t) + 2ull * p.rpi * (D + 2) * sizeof(float));
 }
 
-template <typename T16, int D, int NQT, int WARPS, int STAGES>
+template <typename T16, int D, int NQT, int WARPS, int STAGES, bool GROUP>
 cudaError_t launch_shape(const CUtensorMap &mk, const CUtensorMap &mv, const PagedParams &P, int grid, cudaStream_t st)
 {
     const size_t smem = rows_smem(WARPS, STAGES, P.S);
@@ -683,26 +793,29 @@ cudaError_t launch_shape(const CUtensorMap &mk, const CUtensorMap &mv, const Pag
     if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
     static std::atomic<unsigned long long> attr_done{0};  // one bit per device
     if (!((attr_done.load(std::memory_order_relaxed) >> device) & 1ull)) {
-        const size_t most = rows_smem(WARPS, STAGES, WARPS == kWarpsShares ? kMaxStreams : hawk_host::kPagedSms * 3);
-        e = cudaFuncSetAttribute(paged_rows_kernel<T16, D, NQT, WARPS, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 static_cast<int>(most));
+        // (group: no more streams than items)
+        const size_t most = rows_smem(WARPS, STAGES, GROUP ? hawk_host::kPagedSms * 3 : kMaxStreams);
+        e = cudaFuncSetAttribute(paged_rows_kernel<T16, D, NQT, WARPS, STAGES, GROUP>,
+                                 cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
         if (e != cudaSuccess) return e;
         attr_done.fetch_or(1ull << device, std::memory_order_relaxed);
     }
-    return hawk_host::launch_dependent(paged_rows_kernel<T16, D, NQT, WARPS, STAGES>, dim3(grid), dim3(WARPS * 32), smem, st,
-                                       mk, mv, P);
+    return hawk_host::launch_dependent(paged_rows_kernel<T16, D, NQT, WARPS, STAGES, GROUP>, dim3(grid), dim3(WARPS * 32), smem,
+                                       st, mk, mv, P);
 }
 
 template <typename T16, int D, int NQT>
 cudaError_t launch_rows(const CUtensorMap &mk, const CUtensorMap &mv, const PagedParams &P, const RowsPlan &p, cudaStream_t st)
 {
-    if (p.shape == kShapeWhole) return launch_shape<T16, D, NQT, kWarpsWhole, kStagesWhole>(mk, mv, P, p.grid, st);
+    if (p.shape == kShapeGroup8) return launch_shape<T16, D, NQT, 8, 3, true>(mk, mv, P, p.grid, st);
     if constexpr (NQT == 1)
-        if (p.shape == kShapeGroup) return launch_shape<T16, D, NQT, kWarpsGroup, kStagesGroup>(mk, mv, P, p.grid, st);
-    cudaError_t e = launch_shape<T16, D, NQT, kWarpsShares, kStagesShares>(mk, mv, P, p.grid, st);
+        if (p.shape == kShapeGroup4) return launch_shape<T16, D, NQT, 4, 2, true>(mk, mv, P, p.grid, st);
+    constexpr int kW = shares_warps(NQT);
+    cudaError_t e = launch_shape<T16, D, NQT, kW, shares_stages(NQT), false>(mk, mv, P, p.grid, st);
     if (e != cudaSuccess) return e;
-    const unsigned warps = (kWorkersMax - 1) * NQT * 8;
-    return hawk_host::launch_dependent(paged_merge_kernel<T16, D, NQT * 8>, dim3((warps + 7) / 8), dim3(256), 0, st, P);
+    const unsigned boundaries = hawk_host::kPagedSms * kW - 1;
+    return hawk_host::launch_dependent(paged_merge_kernel<T16, D, NQT * 8>,
+                                       dim3((boundaries + kMergeWorkers - 1) / kMergeWorkers, NQT * 8 / merge_rows(D)), dim3(256), 0, st, P);
 }
 
 template <typename T16, int D>
@@ -818,7 +931,7 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     P.block_table = a.block_table;
     P.anc_mask = a.anc_mask;
     P.records = static_cast<int32_t *>(a.workspace);
-    P.part = reinterpret_cast<float *>(P.records + static_cast<size_t>(kWorkersMax) * kRecordInts);
+    P.part = reinterpret_cast<float *>(P.records + static_cast<size_t>(hawk_host::kPagedSms) * shares_warps(plan.rpi / 8) * kRecordInts);
     P.q_row_stride = a.q_row_stride;
     P.q_head_stride = a.q_head_stride;
     P.S = a.S;
