@@ -2,18 +2,27 @@
 // cores, keys and values streamed page by page.
 //
 // A block owns one (stream, kv head, pair of 128-row query tiles).  The rows of a tile are (position, head of the group)
-// pairs with the head running fastest, so grouped-query heads share every key and value tile.  Two query tiles a block
-// halve the key/value bytes each flop asks of L2 and give the tensor pipe something to do while the other tile's
-// scores are in softmax.  Warps:
-//   0-3, 4-7  softmax of tile 0 and of tile 1: one query row a thread (row maxima and sums need no shuffles)
+// pairs with the head running fastest, so grouped-query heads share every key and value tile.  Two accumulation slots a
+// block give the tensor pipe something to do while the other slot's scores are in softmax, and a pair of query tiles
+// halves the key/value bytes each flop asks of L2.  Where only one query tile has rows, both slots work on it, the even key
+// tiles in slot 0 and the odd ones in slot 1, and are joined at the end.  Warps:
+//   0-3, 4-7  softmax of slot 0 and of slot 1: one query row a thread (row maxima and sums need no shuffles)
 //   8         issues every tcgen05.mma:  S_t = Q_t K^T (both operands in shared memory), O_t += P_t V (P_t in tensor
 //             memory, V in shared memory read along its rows)
-//   9         loads: Q once, then K and V tiles of 128 keys into a ring, as boxes that stay inside a page
+//   9         loads: Q once, then K and V tiles of 128 keys into a ring, as boxes that stay inside a page, a box a lane
 // Tensor memory: S_0, S_1 (128 columns each; P_t overwrites the first half of S_t in 16 bits), O_0, O_1 (D columns each).
-// Order of the products: S_0(0) S_1(0) | P_0(i)V S_0(i+1) P_1(i)V S_1(i+1) | ..., so one tile's softmax runs under the
-// other tile's two products, and when S_t(i) is complete so is O_t up to tile i-1: the softmax warps rescale O_t in
+// Order of the products: S_0(0) S_1(0) | P_0(i)V S_0(i+1) P_1(i)V S_1(i+1) | ..., so one slot's softmax runs under the
+// other slot's two products, and when S_t(i) is complete so is O_t up to tile i-1: the softmax warps rescale O_t in
 // place without any other handshake.  They do so only when a row's maximum has grown by more than 2^8 since the last
 // time (any shift keeps the softmax exact as long as O and the sum use the same one; 2^8 leaves fp16 and fp32 ample room).
+// P is handed over in two halves, so that P V starts on the first 64 keys while the others are in the exponential.
+// At D = 64 the exponentials bound the loop (128 x 128 of them a tile against 512 cycles of products): every fourth pair
+// is computed on the FMA pipe instead, 2^x = 2^n 2^f with n the nearest integer and a degree-4 polynomial for 2^f on
+// [-1/2, 1/2] (least squares on Chebyshev points, relative error 2.6e-6); 4 x 2048 rows over 8192 keys, 32 heads sharing 8: 726 to
+// 702 us.  At D = 128 it gains nothing (790 against 794).
+// Measured there: 1217 TFLOP/s at D = 128, 0.73 of the measured burst peak.  What it took: MMAs issued under a predicate with
+// descriptors stepped by their low word (980 to 790 us; see umma_f16_ss_if).  Two score buffers of 64 keys a slot, so that the next
+// scores never wait for P V, came to 916 us: products of 64 columns read Q from shared memory twice as often.
 // Few blocks: the key range is split too, each split leaves (o, max, sum) in fp32 and a second kernel joins them.
 #include <atomic>
 
@@ -24,7 +33,8 @@ namespace {
 using namespace hawk;
 
 constexpr int kBM = 128, kBN = 128;
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;        // three warpgroups; the third has one warp for the products and one for the loads
+constexpr int kRegsSoftmax = 216, kRegsOther = 72;  // of the 168 a thread that the block starts with (2 x 216 + 72 = 3 x 168)
 constexpr int kMaxSplits = 16;
 constexpr int kMinSplitKeys = 512;  // shorter key ranges cost more in partial results than they gain in blocks
 
@@ -42,7 +52,7 @@ struct TileCfg {
     static constexpr int kHalfBytes = 128 * 128;           // [128 rows][64 columns]
     static constexpr int kTileBytes = kHalves * kHalfBytes;
     static constexpr int kStages = D == 128 ? 5 : 10;
-    static constexpr size_t kSmem = 1024 + static_cast<size_t>(2 + kStages) * kTileBytes + 512;
+    static constexpr size_t kSmem = 1024 + static_cast<size_t>(2 + kStages) * kTileBytes + 512 + 1024 /* max, sum of slot 1's rows */;
 };
 
 // What the block works on.
@@ -50,9 +60,10 @@ struct TileJob {
     int s, hk, split;
     int r0, n, kv;
     int tok0;            // first position of the block's first query tile
-    int nt[2];           // key tiles of each query tile, counted from tile `begin`
+    int nt[2];           // key tiles of each slot
+    int tiles;           // key tiles of the block, counted from tile `begin`
     int begin;           // first key tile of the split
-    bool any;
+    bool single;         // one query tile, its key tiles dealt out to the two slots
 };
 
 // Pairs of query tiles of a stream that belongs to this kernel.
@@ -123,8 +134,64 @@ __device__ __forceinline__ bool find_job(const TileParams &P, bool with_split, i
     const int stop = static_cast<int>(static_cast<long long>(all) * (job.split + 1) / P.n_split);
 #pragma unroll
     for (int t = 0; t < 2; ++t) job.nt[t] = max(0, min(end[t], stop) - job.begin);
-    job.any = job.nt[0] > 0 || job.nt[1] > 0;
+    job.tiles = max(job.nt[0], job.nt[1]);
+    job.single = job.tok0 + P.tok >= st.n;
+    if (job.single) {
+        job.nt[0] = (job.tiles + 1) / 2;
+        job.nt[1] = job.tiles / 2;
+    }
     return true;
+}
+
+// Pairs of fp32 numbers in one 64-bit register: one instruction for two operations.
+__device__ __forceinline__ uint64_t pack2(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// 2^x of two numbers on the FMA pipe, -126 <= x < 127 (smaller ones give 2^-126).
+__device__ __forceinline__ float2 exp2_fma(uint64_t x2)
+{
+    float2 x = unpack2(x2);
+    x.x = fmaxf(x.x, -126.f);
+    x.y = fmaxf(x.y, -126.f);
+    const uint64_t v = pack2(x.x, x.y);
+    constexpr float kRound = 12582912.f;  // 1.5 * 2^23: adding it leaves the nearest integer in the low mantissa bits
+    const uint64_t n = add2(v, pack2(kRound, kRound));
+    const uint64_t f = add2(v, fma2(n, pack2(-1.f, -1.f), pack2(kRound, kRound)));  // x - nearest integer
+    uint64_t p = fma2(pack2(0.0095701f, 0.0095701f), f, pack2(0.05591786f, 0.05591786f));
+    p = fma2(p, f, pack2(0.24024745f, 0.24024745f));
+    p = fma2(p, f, pack2(0.69312181f, 0.69312181f));
+    p = fma2(p, f, pack2(0.99999926f, 0.99999926f));
+    const float2 pf = unpack2(p), nf = unpack2(n);
+    return make_float2(__int_as_float(__float_as_int(pf.x) + (__float_as_int(nf.x) << 23)),
+                       __int_as_float(__float_as_int(pf.y) + (__float_as_int(nf.y) << 23)));
+}
+
+// mbar_wait of a whole warp: true for all its lanes or for none, so that the warp stays together when a wait gives up.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
 
 template <typename T16, int D>
@@ -136,11 +203,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     using E = Elem<T16>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t *q_smem = smem;                              // two query tiles
+    uint8_t *q_smem = smem;                              // two query tiles; at the end slot 1's O of a single tile
     uint8_t *ring = smem + 2 * C::kTileBytes;            // K and V tiles in turn
-    uint64_t *bars = reinterpret_cast<uint64_t *>(ring + C::kStages * C::kTileBytes);
+    float2 *ml_smem = reinterpret_cast<float2 *>(ring + C::kStages * C::kTileBytes);  // [128]
+    uint64_t *bars = reinterpret_cast<uint64_t *>(ml_smem + 128);
     uint64_t *full = bars, *empty = bars + C::kStages;
-    uint64_t *q_full = bars + 2 * C::kStages, *s_full = q_full + 1, *p_ready = q_full + 3, *o_done = q_full + 5, *drain = q_full + 7;
+    uint64_t *q_full = bars + 2 * C::kStages, *s_full = q_full + 1, *p_ready = q_full + 3, *o_done = q_full + 7, *drain = q_full + 9;
     uint32_t *tmem_ptr = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_ptr + 1);
     int *sums = reinterpret_cast<int *>(tmem_ptr + 2);   // [20]
@@ -154,7 +222,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(q_full, 1);
         for (int t = 0; t < 2; ++t) {
             mbar_init(&s_full[t], 1);
-            mbar_init(&p_ready[t], 4);
+            mbar_init(&p_ready[2 * t], 4);
+            mbar_init(&p_ready[2 * t + 1], 4);
             mbar_init(&o_done[t], 1);
         }
         mbar_init(drain, 1);
@@ -179,173 +248,209 @@ __global__ void __launch_bounds__(kThreads, 1)
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
-    const uint32_t tmem = *tmem_ptr;
-    const int nt_max = max(job.nt[0], job.nt[1]);
+    constexpr uint32_t tmem = 0;  // all 512 columns are the block's: its tensor memory starts at lane 0, column 0
     const int pfx = job.kv - job.n;
+    // K tiles run this many ahead of V tiles in the ring: slot 1 of a single query tile starts on key tile 1
+    const int ahead = job.single ? 2 : 1;
 
-    if (warp == 9) {
-        // ------------------------------------------------------------------ loads
-        bool ok = true;
-        int issued = 0;  // ring stages armed
-        if (job.any) {
-            const uint64_t keep = l2_policy_evict_last();
-            if (lane == 0) {
-                const uint32_t bytes = (job.nt[0] > 0 ? 1 : 0) + (job.nt[1] > 0 ? 1 : 0);
-                mbar_arrive_expect_tx(q_full, bytes * C::kHalves * P.q_rows * 128);
-                for (int t = 0; t < 2; ++t)
-                    if (job.nt[t] > 0)
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+        if (warp == 9) {
+            // -------------------------------------------------------------- loads
+            bool ok = true;
+            int issued = 0;  // ring stages armed
+            if (job.tiles > 0) {
+                const uint64_t keep = l2_policy_evict_last();
+                const int q_tiles = job.single ? 1 : 2;
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(q_full, q_tiles * C::kHalves * P.q_rows * 128);
+                    for (int t = 0; t < q_tiles; ++t)
                         for (int hf = 0; hf < C::kHalves; ++hf)
                             tma_load_4d(q_smem + t * C::kTileBytes + hf * C::kHalfBytes, &map_q, hf * 64, job.hk * P.c.group,
                                         job.r0 + job.tok0 + t * P.tok, 0, q_full);
-            }
-            const int need = static_cast<int>(P.c.div_page.div(static_cast<uint32_t>(job.kv + P.c.page_size - 1)));
-            const int32_t *tb = P.c.block_table + static_cast<size_t>(job.s) * P.c.table_width;
-            const int boxes = kBN / P.c.box_rows;
-            int base = -64, cur = 0, nxt = 0;  // page ids base + lane and base + 32 + lane
-            auto fetch = [&](int b) { return b + lane < need ? tb[b + lane] : 0; };
-            for (int i = 0; i < nt_max && ok; ++i) {
-                const int key0 = (job.begin + i) * kBN;
-                const int live = min(boxes, (job.kv - key0 + P.c.box_rows - 1) / P.c.box_rows);
-                for (int kind = 0; kind < 2 && ok; ++kind) {  // K, then V
-                    const int st = issued % C::kStages;
-                    const uint32_t round = issued / C::kStages;
-                    if (round > 0) ok = mbar_wait(&empty[st], (round - 1) & 1u, abort_flag);
-                    if (!ok) break;
-                    uint8_t *dst = ring + st * C::kTileBytes;
+                }
+                // lane l loads 64-column half l % halves of box l / halves of every tile (at most 32 of them: boxes have
+                // 8 rows or more); its page id is fetched one tile ahead
+                const int hf = lane % C::kHalves;
+                const int box_key = lane / C::kHalves * P.c.box_rows;
+                const int32_t *tb = P.c.block_table + static_cast<size_t>(job.s) * P.c.table_width;
+                auto key_of = [&](int i) { return (job.begin + i) * kBN + box_key; };
+                auto has_box = [&](int i) { return i < job.tiles && box_key < kBN && key_of(i) < job.kv; };
+                auto page_id = [&](int i) {
+                    return has_box(i) ? tb[P.c.div_page.div(static_cast<uint32_t>(key_of(i)))] : 0;
+                };
+                int id[4] = {page_id(0), page_id(1), page_id(2), 0};  // of tiles j, j + 1, j + 2 (and the one on its way)
+                auto load = [&](int i, bool values, int pg) {
+                    const int st = issued % C::kStages, round = issued / C::kStages;
+                    if (round > 0) ok = ok && warp_wait(&empty[st], (round - 1) & 1u, abort_flag);
+                    if (!ok) return;
+                    const int rows = min(kBN, (job.kv - (job.begin + i) * kBN + P.c.box_rows - 1) & -P.c.box_rows);
                     if (lane == 0) {
                         const bool stall = kTestStallBytes != 0 && blockIdx.x == 0 && issued == 0;
-                        mbar_arrive_expect_tx(&full[st], live * P.c.box_rows * 128 * C::kHalves + (stall ? kTestStallBytes : 0u));
+                        mbar_arrive_expect_tx(&full[st], rows * 128 * C::kHalves + (stall ? kTestStallBytes : 0u));
                     }
-                    ++issued;
-                    for (int b = 0; b < live; ++b) {
-                        uint32_t row;
-                        const int pg = static_cast<int>(P.c.div_page.divmod(static_cast<uint32_t>(key0 + b * P.c.box_rows), row));
-                        if (pg < base || pg >= base + 32) {
-                            if (pg >= base + 32 && pg < base + 64) {
-                                cur = nxt;
-                                base += 32;
-                            } else {
-                                base = pg & ~31;
-                                cur = fetch(base);
-                            }
-                            nxt = fetch(base + 32);
-                        }
-                        const int id = __shfl_sync(0xffffffffu, cur, pg - base);
-                        if (id < 0 || id >= P.c.n_pages) flags |= HAWK_DEV_BAD_PAGE;  // (outside the tensor map: zeros)
-                        if (lane == 0)
-                            for (int hf = 0; hf < C::kHalves; ++hf)
-                                paged_load(dst + hf * C::kHalfBytes + b * P.c.box_rows * 128, kind ? &map_v : &map_k,
-                                           kind ? P.c.v_rows_inner : P.c.k_rows_inner, hf, static_cast<int>(row), job.hk, id,
-                                           &full[st], keep);
-                    }
-                    // K's boxes of this tile come again for V: the table window may have moved on, which `base` notices
-                }
-            }
-            if (!ok || *abort_flag) {
-                // let what is in flight land (bounded) before the block retires
-                *abort_flag = 1;
-                mbar_wait(q_full, 0, nullptr);
-                for (int i = max(0, issued - C::kStages); i < issued; ++i)
-                    mbar_wait(&full[i % C::kStages], (i / C::kStages) & 1u, nullptr);
-                flags |= HAWK_DEV_TIMEOUT;
-            }
-        }
-        if (flags && lane == 0 && P.c.dev_status) atomicOr(P.c.dev_status, flags);
-    } else if (warp == 8) {
-        // ------------------------------------------------------------------ products
-        constexpr uint32_t idesc_s = umma_idesc_f16kind(kBM, kBN, E::kBf16, false);
-        constexpr uint32_t idesc_o = umma_idesc_f16kind(kBM, D, E::kBf16, true);
-        const uint32_t q_addr = smem_u32(q_smem), ring_addr = smem_u32(ring);
-        bool ok = true;
-        auto wait_full = [&](int load) {  // load 2i: K tile i, 2i + 1: V tile i
-            ok = ok && mbar_wait(&full[load % C::kStages], (load / C::kStages) & 1u, abort_flag);
-        };
-        auto scores = [&](int t, int i) {
-            const uint32_t a = q_addr + t * C::kTileBytes, b = ring_addr + ((2 * i) % C::kStages) * C::kTileBytes;
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t off = (kk >> 2) * C::kHalfBytes + (kk & 3) * 32;
-                umma_bf16(tmem + t * kBN, umma_desc_k_major_sw128(a + off), umma_desc_k_major_sw128(b + off), idesc_s, kk > 0);
-            }
-            umma_commit(&s_full[t]);
-        };
-        auto values = [&](int t, int i) {
-            const uint32_t b = ring_addr + ((2 * i + 1) % C::kStages) * C::kTileBytes;
-#pragma unroll
-            for (int kk = 0; kk < kBN / 16; ++kk)
-                umma_f16_ts(tmem + 256 + t * D, tmem + t * kBN + kk * 8,
-                            umma_desc_mn_major_sw128(b + kk * 2048, C::kHalfBytes), idesc_o, i > 0 || kk > 0);
-            if (i + 1 == job.nt[t]) umma_commit(&o_done[t]);
-        };
-        if (job.any) {
-            ok = mbar_wait(q_full, 0, abort_flag);
-            wait_full(0);
-            if (ok && lane == 0) {
-                tcgen05_fence_after();
-                for (int t = 0; t < 2; ++t)
-                    if (job.nt[t] > 0) scores(t, 0);
-                umma_commit(&empty[0]);
-            }
-            for (int i = 0; i < nt_max && ok; ++i) {
-                wait_full(2 * i + 1);
-                const int vst = (2 * i + 1) % C::kStages;
-                const int left = job.kv - (job.begin + i) * kBN;  // keys of the tile that exist
-                if (ok && left < kBN) {
-                    // values behind the last key hold anything: zero them (0 * NaN is NaN)
-                    uint8_t *v = ring + vst * C::kTileBytes;
-                    for (int x = left * 8 + lane; x < kBN * 8; x += 32)
-                        for (int hf = 0; hf < C::kHalves; ++hf)
-                            *reinterpret_cast<uint4 *>(v + hf * C::kHalfBytes + x * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    fence_proxy_async();
                     __syncwarp();
-                }
-                for (int t = 0; t < 2 && ok; ++t) {
-                    if (i < job.nt[t]) {
-                        ok = mbar_wait(&p_ready[t], i & 1u, abort_flag);
-                        if (ok && lane == 0) {
-                            tcgen05_fence_after();
-                            values(t, i);
-                        }
+                    ++issued;
+                    if (has_box(i)) {
+                        if (pg < 0 || pg >= P.c.n_pages) flags |= HAWK_DEV_BAD_PAGE;  // (outside the tensor map: zeros)
+                        uint32_t row;
+                        P.c.div_page.divmod(static_cast<uint32_t>(key_of(i)), row);
+                        paged_load(ring + st * C::kTileBytes + hf * C::kHalfBytes + box_key * 128, values ? &map_v : &map_k,
+                                   values ? P.c.v_rows_inner : P.c.k_rows_inner, hf, static_cast<int>(row), job.hk, pg, &full[st],
+                                   keep);
                     }
-                    if (i + 1 < job.nt[t]) {
-                        wait_full(2 * i + 2);
-                        if (ok && lane == 0) scores(t, i + 1);
+                    __syncwarp();
+                };
+                load(0, false, id[0]);
+                if (ahead == 2 && job.tiles > 1 && ok) load(1, false, id[1]);
+                for (int j = 0; j < job.tiles && ok; ++j) {
+                    id[3] = page_id(j + 3);
+                    load(j, true, id[0]);
+                    if (ok && j + ahead < job.tiles) load(j + ahead, false, ahead == 2 ? id[2] : id[1]);
+                    id[0] = id[1];
+                    id[1] = id[2];
+                    id[2] = id[3];
+                }
+                if (!ok || *abort_flag) {
+                    // let what is in flight land (bounded) before the block retires
+                    *abort_flag = 1;
+                    warp_wait(q_full, 0, nullptr);
+                    for (int i = max(0, issued - C::kStages); i < issued; ++i)
+                        warp_wait(&full[i % C::kStages], (i / C::kStages) & 1u, nullptr);
+                    flags |= HAWK_DEV_TIMEOUT;
+                }
+            }
+            if (flags && P.c.dev_status) atomicOr(P.c.dev_status, flags);
+        } else if (warp == 8 && job.tiles > 0) {
+            // -------------------------------------------------------------- products
+            constexpr uint32_t idesc_s = umma_idesc_f16kind(kBM, kBN, E::kBf16, false);
+            constexpr uint32_t idesc_o = umma_idesc_f16kind(kBM, D, E::kBf16, true);
+            const uint32_t lead = elect_one();
+            // broadcasts: what the loop runs on is warp-uniform for the compiler too (uniform registers, no divergence)
+            const int nt0 = __shfl_sync(0xffffffffu, job.nt[0], 0), nt1 = __shfl_sync(0xffffffffu, job.nt[1], 0);
+            const int tiles = __shfl_sync(0xffffffffu, job.tiles, 0);
+            const int all_keys = __shfl_sync(0xffffffffu, job.kv - job.begin * kBN, 0);  // keys from the block's first tile on
+            const bool single = __shfl_sync(0xffffffffu, static_cast<int>(job.single), 0) != 0;
+            const uint64_t qd = umma_desc_k_major_sw128(smem_u32(q_smem)), kd = umma_desc_k_major_sw128(smem_u32(ring)),
+                           vd = umma_desc_mn_major_sw128(smem_u32(ring), C::kHalfBytes);
+            const uint32_t q_lo = static_cast<uint32_t>(qd), k_lo = static_cast<uint32_t>(kd), v_lo = static_cast<uint32_t>(vd);
+            const uint32_t qk_hi = static_cast<uint32_t>(qd >> 32), v_hi = static_cast<uint32_t>(vd >> 32);
+            bool ok = warp_wait(q_full, 0, abort_flag);
+            int taken = 0;
+            auto acquire = [&]() {  // the next tile of the ring
+                const int st = taken % C::kStages;
+                ok = ok && warp_wait(&full[st], (taken / C::kStages) & 1u, abort_flag);
+                ++taken;
+                return st;
+            };
+            auto release = [&](int st) {
+                if (ok) umma_commit_if(lead, &empty[st]);
+            };
+            auto scores = [&](int t, int st) {
+                if (!ok) return;
+                const uint32_t a = q_lo + ((single ? 0 : t * C::kTileBytes) >> 4);
+                const uint32_t b = k_lo + ((st * C::kTileBytes) >> 4);
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    constexpr int kHalf16 = C::kHalfBytes >> 4;
+                    const uint32_t off = (kk >> 2) * kHalf16 + (kk & 3) * 2;
+                    umma_f16_ss_if(lead, tmem + t * kBN, a + off, qk_hi, b + off, qk_hi, idesc_s, kk > 0);
+                }
+                umma_commit_if(lead, &s_full[t]);
+            };
+            auto values = [&](int t, int i, int st) {
+                const uint32_t b = v_lo + ((st * C::kTileBytes) >> 4);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    ok = ok && warp_wait(&p_ready[2 * t + half], i & 1u, abort_flag);
+                    if (!ok) return;
+                    tcgen05_fence_after();
+#pragma unroll
+                    for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+                        umma_f16_ts_if(lead, tmem + 256 + t * D, tmem + t * kBN + kk * 8, b + kk * 128, v_hi, idesc_o, i > 0 || kk > 0);
+                }
+                if (i + 1 == (t == 0 ? nt0 : nt1)) umma_commit_if(lead, &o_done[t]);
+            };
+            auto clean = [&](int tile, int st) {
+                // values behind the last key hold anything: zero them (0 * NaN is NaN)
+                const int left = all_keys - tile * kBN;  // keys of the tile that exist
+                if (!ok || left >= kBN) return;
+                uint8_t *v = ring + st * C::kTileBytes;
+                for (int x = left * 8 + lane; x < kBN * 8; x += 32)
+                    for (int hf = 0; hf < C::kHalves; ++hf)
+                        *reinterpret_cast<uint4 *>(v + hf * C::kHalfBytes + x * 16) = make_uint4(0u, 0u, 0u, 0u);
+                fence_proxy_async();
+                __syncwarp();
+            };
+            if (single) {
+                int st = acquire();
+                scores(0, st);
+                release(st);
+                if (tiles > 1) {
+                    st = acquire();
+                    scores(1, st);
+                    release(st);
+                }
+                for (int j = 0; j < tiles && ok; ++j) {
+                    const int t = j & 1, v = acquire();
+                    clean(j, v);
+                    values(t, j >> 1, v);
+                    release(v);
+                    if (j + 2 < tiles) {
+                        const int k = acquire();
+                        scores(t, k);
+                        release(k);
                     }
                 }
-                if (ok && lane == 0) {
-                    umma_commit(&empty[vst]);
-                    if (i + 1 < nt_max) umma_commit(&empty[(2 * i + 2) % C::kStages]);
+            } else {
+                int k = acquire();
+                if (nt0 > 0) scores(0, k);
+                if (nt1 > 0) scores(1, k);
+                release(k);
+                for (int i = 0; i < tiles && ok; ++i) {
+                    const int v = acquire();
+                    clean(i, v);
+                    if (i < nt0) values(0, i, v);
+                    if (i + 1 < tiles) k = acquire();
+                    if (i + 1 < nt0) scores(0, k);
+                    if (i < nt1) values(1, i, v);
+                    release(v);
+                    if (i + 1 < nt1) scores(1, k);
+                    if (i + 1 < tiles) release(k);
                 }
             }
             // every product issued has finished before the block gives its tensor memory back
             __syncwarp();
-            if (lane == 0) umma_commit(drain);
+            umma_commit_if(lead, drain);
             if (!ok) *abort_flag = 1;
-            if (!mbar_wait(drain, 0, nullptr)) ok = false;
+            if (!warp_wait(drain, 0, nullptr)) ok = false;
             if (!ok && lane == 0 && P.c.dev_status) atomicOr(P.c.dev_status, HAWK_DEV_TIMEOUT);
         }
     } else {
-        // ------------------------------------------------------------------ softmax and epilogue of query tile t
+        // ------------------------------------------------------------------ softmax and epilogue of slot t
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int t = warp >> 2;
         const int r = tid & 127;
         const uint32_t lane_off = static_cast<uint32_t>(warp & 3) << 21;  // 32 lanes of tensor memory per warp
         const uint32_t s_addr = tmem + lane_off + t * kBN, o_addr = tmem + lane_off + 256 + t * D;
         uint32_t hd;
-        const int pos = job.tok0 + t * P.tok + static_cast<int>(P.c.div_group.divmod(static_cast<uint32_t>(r), hd));
+        const int pos = job.tok0 + (job.single ? 0 : t * P.tok) + static_cast<int>(P.c.div_group.divmod(static_cast<uint32_t>(r), hd));
         const bool valid = r < P.q_rows && pos < job.n;
         const int limit = min(job.kv, pfx + min(pos, job.n - 1) + 1);  // keys this row sees
+        const int first = job.begin + (job.single ? t : 0), stride = job.single ? 2 : 1;  // key tiles of the slot
+        const uint64_t scale2 = pack2(P.c.scale_log2, P.c.scale_log2);
         float m_run = -CUDART_INF_F, l_run = 0.f;
         const int nt = job.nt[t];
         bool ok = true;
         for (int i = 0; i < nt; ++i) {
-            ok = mbar_wait(&s_full[t], i & 1u, abort_flag);
+            ok = warp_wait(&s_full[t], i & 1u, abort_flag);
             if (!ok) break;
             tcgen05_fence_after();
             uint32_t u[4][32];
 #pragma unroll
             for (int q = 0; q < 4; ++q) tmem_ld_32x32(s_addr + q * 32, u[q]);
             tmem_ld_wait();
-            const int seen = limit - (job.begin + i) * kBN;
+            const int seen = limit - (first + i * stride) * kBN;
             if (seen < kBN) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
@@ -379,72 +484,120 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             const float mu = m_run == -CUDART_INF_F ? 0.f : m_run;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const uint64_t shift2 = pack2(-mu, -mu);
+            uint64_t sum_a = 0, sum_b = 0;  // (two zeros each)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 uint32_t pk[32];
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
-                    const float x0 = __uint_as_float(u[half * 2 + (c >> 4)][(2 * c) & 31]);
-                    const float x1 = __uint_as_float(u[half * 2 + (c >> 4)][(2 * c + 1) & 31]);
-                    const float p0 = fast_exp2(fmaf(x0, P.c.scale_log2, -mu)), p1 = fast_exp2(fmaf(x1, P.c.scale_log2, -mu));
-                    sum[c & 1] += p0;
-                    sum[2 + (c & 1)] += p1;
-                    pk[c] = E::pack(p0, p1);
+                    const int q = half * 2 + (c >> 4), e = (2 * c) & 31;
+                    const uint64_t x2 = fma2(pack2(__uint_as_float(u[q][e]), __uint_as_float(u[q][e + 1])), scale2, shift2);
+                    float2 p;
+                    if (D == 64 && c % 4 == 3) {
+                        p = exp2_fma(x2);
+                    } else {
+                        p = unpack2(x2);
+                        p.x = fast_exp2(p.x);
+                        p.y = fast_exp2(p.y);
+                    }
+                    if (c & 1) sum_b = add2(sum_b, pack2(p.x, p.y));
+                    else sum_a = add2(sum_a, pack2(p.x, p.y));
+                    pk[c] = E::pack(p.x, p.y);
                 }
                 tmem_st_32x32(s_addr + half * 32, pk);
+                tmem_st_wait();
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_ready[2 * t + half]);
             }
-            l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            tmem_st_wait();
-            tcgen05_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_ready[t]);
+            const float2 sums2 = unpack2(add2(sum_a, sum_b));
+            l_run += sums2.x + sums2.y;
         }
-        if (ok && nt > 0) ok = mbar_wait(&o_done[t], 0, abort_flag);
+        if (ok && nt > 0) ok = warp_wait(&o_done[t], 0, abort_flag);
+        if (ok && job.single && job.tiles > 1) ok = warp_wait(&o_done[t ^ 1], 0, abort_flag);  // (Q is free then)
         if (!ok) *abort_flag = 1;
         tcgen05_fence_after();
-        const long long row = job.r0 + static_cast<long long>(pos);
-        const int h = job.hk * P.c.group + static_cast<int>(hd);
-        const long long cell = row * P.c.H + h;
+        if (m_run == -CUDART_INF_F) l_run = 0.f;  // a row that has seen no key
         // the tensor-memory loads below are for whole warps: rows that do not exist take part and store nothing
-        if (P.n_split == 1) {
-            const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-            T16 *dst = static_cast<T16 *>(P.c.out) + (valid ? cell * D : 0);
-#pragma unroll
-            for (int c0 = 0; c0 < D; c0 += 32) {
-                uint32_t o[32];
+        float f_own = 1.f, f_other = 0.f;  // weights of the two slots' O where they are joined
+        auto other_at = [&](int c) {       // 16-byte chunk c of row r of slot 1's O (the chunk index turned by the row: no conflicts)
+            return reinterpret_cast<uint4 *>(q_smem) + r * (D / 4) + (c ^ (r & (D / 4 - 1)));
+        };
+        if (job.single) {
+            if (t == 1) {
+                ml_smem[r] = make_float2(m_run, l_run);
                 if (nt > 0) {
-                    tmem_ld_32x32(o_addr + c0, o);
-                    tmem_ld_wait();
-                }
-                if (valid && ok) {
 #pragma unroll
-                    for (int c = 0; c < 32; c += 8) {
-                        uint32_t w[4];
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        uint32_t o[32];
+                        tmem_ld_32x32(o_addr + c0, o);
+                        tmem_ld_wait();
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            w[k] = nt == 0 || l_run == 0.f ? 0u
-                                                           : E::pack(__uint_as_float(o[c + 2 * k]) * inv,
-                                                                     __uint_as_float(o[c + 2 * k + 1]) * inv);
-                        *reinterpret_cast<uint4 *>(dst + c0 + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int c = 0; c < 32; c += 4) *other_at((c0 + c) / 4) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
                     }
                 }
             }
-        } else {
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (t == 0) {
+                const float2 o = ml_smem[r];
+                const float m = fmaxf(m_run, o.x);
+                const float mu = m == -CUDART_INF_F ? 0.f : m;
+                f_own = l_run == 0.f ? 0.f : fast_exp2(m_run - mu);
+                f_other = o.y == 0.f ? 0.f : fast_exp2(o.x - mu);
+                l_run = l_run * f_own + o.y * f_other;
+                m_run = m;
+            }
+        }
+        if (!job.single || t == 0) {
+            const long long row = job.r0 + static_cast<long long>(pos);
+            const long long cell = row * P.c.H + job.hk * P.c.group + static_cast<int>(hd);
+            const bool join = job.single && job.nt[1] > 0;
+            const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
             const long long cells = static_cast<long long>(P.c.T) * P.c.H, at = job.split * cells + (valid ? cell : 0);
-            float *dst = P.c.part + at * D;
-            if (valid && ok)
+            T16 *dst = static_cast<T16 *>(P.c.out) + (valid ? cell * D : 0);
+            float *part = P.c.part + at * D;
+            if (P.n_split > 1 && valid && ok)
                 *reinterpret_cast<float2 *>(P.c.part + P.n_split * cells * D + at * 2) = make_float2(m_run, l_run);
-            if (nt > 0) {  // (a split without keys has l = 0 and its o is not read)
+            // (a split without keys has sum 0 and its o is not read)
+            if (nt > 0 || P.n_split == 1) {
 #pragma unroll
                 for (int c0 = 0; c0 < D; c0 += 32) {
                     uint32_t o[32];
-                    tmem_ld_32x32(o_addr + c0, o);
-                    tmem_ld_wait();
-                    if (valid && ok) {
+                    if (nt > 0) {
+                        tmem_ld_32x32(o_addr + c0, o);
+                        tmem_ld_wait();
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        float v[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = l_run == 0.f ? 0.f : __uint_as_float(o[c + k]);
+                        if (join) {
+                            const uint4 x = *other_at((c0 + c) / 4);
+                            // (a slot without mass for this row may hold anything)
+                            v[0] = (f_own == 0.f ? 0.f : v[0] * f_own) + (f_other == 0.f ? 0.f : __uint_as_float(x.x) * f_other);
+                            v[1] = (f_own == 0.f ? 0.f : v[1] * f_own) + (f_other == 0.f ? 0.f : __uint_as_float(x.y) * f_other);
+                            v[2] = (f_own == 0.f ? 0.f : v[2] * f_own) + (f_other == 0.f ? 0.f : __uint_as_float(x.z) * f_other);
+                            v[3] = (f_own == 0.f ? 0.f : v[3] * f_own) + (f_other == 0.f ? 0.f : __uint_as_float(x.w) * f_other);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[c + k] = __float_as_uint(v[k]);
+                    }
+                    if (!valid || !ok) continue;
+                    if (P.n_split == 1) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                w[k] = E::pack(__uint_as_float(o[c + 2 * k]) * inv, __uint_as_float(o[c + 2 * k + 1]) * inv);
+                            *reinterpret_cast<uint4 *>(dst + c0 + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    } else {
 #pragma unroll
                         for (int c = 0; c < 32; c += 4)
-                            *reinterpret_cast<uint4 *>(dst + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                            *reinterpret_cast<uint4 *>(part + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
                     }
                 }
             }
@@ -452,10 +605,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     tcgen05_fence_before();
     __syncthreads();
-    if (warp == 8) tmem_dealloc(tmem, 512);
+    if (warp == 8) tmem_dealloc(*tmem_ptr, 512);
 }
 
-// Joins the splits: a block per (pair of query tiles, kv head) as above, a warp per row.
+// Joins the splits: 16 blocks per (pair of query tiles, kv head), a warp per row.
 template <typename T16, int D>
 __global__ void __launch_bounds__(256) paged_tile_merge_kernel(const TileParams P)
 {
@@ -471,7 +624,7 @@ __global__ void __launch_bounds__(256) paged_tile_merge_kernel(const TileParams 
     const long long cells = static_cast<long long>(P.c.T) * P.c.H;
     const float *ml = P.c.part + P.n_split * cells * D;
     const int rows = min(2 * P.tok, job.n - job.tok0) * P.c.group;
-    for (int r = warp; r < rows; r += 8) {
+    for (int r = blockIdx.y * 8 + warp; r < rows; r += 8 * gridDim.y) {
         uint32_t hd;
         const uint32_t pos = P.c.div_group.divmod(static_cast<uint32_t>(r), hd);
         const long long cell = (job.r0 + static_cast<long long>(job.tok0) + pos) * P.c.H + job.hk * P.c.group + static_cast<int>(hd);
@@ -552,7 +705,7 @@ cudaError_t launch(const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorM
     e = hawk_host::launch_dependent(paged_tile_kernel<T16, D>, dim3(base * P.n_split), dim3(kThreads), TileCfg<D>::kSmem, st, mq,
                                     mk, mv, P);
     if (e != cudaSuccess || P.n_split == 1) return e;
-    return hawk_host::launch_dependent(paged_tile_merge_kernel<T16, D>, dim3(base), dim3(256), 0, st, P);
+    return hawk_host::launch_dependent(paged_tile_merge_kernel<T16, D>, dim3(base, 16), dim3(256), 0, st, P);
 }
 
 }  // namespace
