@@ -2,12 +2,15 @@
 
 Every function takes torch CUDA tensors, checks dtype/contiguity/device, and passes raw pointers,
 sizes and the current CUDA stream to the entry point of the same name in libhawk_verify.so.  No
-step of the verify path is computed here, and there is no fallback: a missing library raises.
+step of the verify path is computed here, and there is no fallback: a missing library raises.  The calls around the
+paged cache, which run once a layer, are marshalled the same way by a small extension (csrc/hawk_marshal.cpp).
 """
 from __future__ import annotations
 
 import contextlib
 import ctypes
+import importlib.util
+import sysconfig
 from pathlib import Path
 from typing import Optional
 
@@ -15,7 +18,9 @@ import torch
 
 _PKG = Path(__file__).resolve().parent
 _LIB_PATH = _PKG / "libhawk_verify.so"
+_MARSHAL_PATH = _PKG / ("_hawk_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 _lib: Optional[ctypes.CDLL] = None
+_marshal = None
 
 DEV_TIMEOUT, DEV_BAD_DRAFT, DEV_NONFINITE, DEV_BAD_PREFIX, DEV_BAD_TREE, DEV_BOUNDS = 1, 2, 4, 8, 16, 32
 DEV_BAD_ROWS, DEV_BAD_PAGE, DEV_BAD_POSITION = 64, 128, 256
@@ -53,38 +58,6 @@ class StepHostArgs(ctypes.Structure):
     _fields_ = _step_fields()
 
 
-class QkRopeArgs(ctypes.Structure):
-    """Mirror of hawk_qk_rope_args (include/hawk.h)."""
-    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "T", "H", "H_kv", "D", "norm", "per_head", "rot_dim", "n_positions",
-                                             "interleaved")]
-                + [("eps", ctypes.c_float)]
-                + [(n, ctypes.c_void_p) for n in ("q", "k", "q_out", "k_out")]
-                + [(f"{t}_{w}_stride", ctypes.c_longlong) for t in ("q", "k", "q_out", "k_out") for w in ("row", "head")]
-                + [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "q_bias", "k_bias", "position", "cos_sin")])
-
-
-_PAGE_STRIDES = [(f"{t}_{w}_stride", ctypes.c_longlong) for t in "kv" for w in ("page", "page_head", "page_row")]
-
-
-class RopeAppendArgs(ctypes.Structure):
-    """Mirror of hawk_rope_append_args (include/hawk.h)."""
-    _fields_ = ([("qk", QkRopeArgs), ("v", ctypes.c_void_p), ("v_row_stride", ctypes.c_longlong),
-                 ("v_head_stride", ctypes.c_longlong), ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p)]
-                + _PAGE_STRIDES + [(n, ctypes.c_int) for n in ("n_pages", "page_size", "S", "table_width")]
-                + [(n, ctypes.c_void_p) for n in ("block_table", "row_begin", "kv_len")])
-
-
-class PagedAttnArgs(ctypes.Structure):
-    """Mirror of hawk_paged_attn_args (include/hawk.h)."""
-    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "S", "T", "max_new", "max_kv", "H", "H_kv", "D", "n_pages", "page_size",
-                                             "table_width")]
-                + [("sm_scale", ctypes.c_float), ("q", ctypes.c_void_p), ("q_row_stride", ctypes.c_longlong),
-                   ("q_head_stride", ctypes.c_longlong), ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p)]
-                + _PAGE_STRIDES
-                + [(n, ctypes.c_void_p) for n in ("block_table", "row_begin", "kv_len", "anc_mask", "out", "workspace")]
-                + [("workspace_bytes", ctypes.c_size_t)])
-
-
 class HawkError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -104,8 +77,21 @@ def load_library() -> ctypes.CDLL:
         raise RuntimeError(
             f"{_LIB_PATH} is missing: build it with `python -m paper_2510_25739_b200.build` "
             "(or __graft_entry__.build()); there is no fallback path")
+    _load_marshal()
     _lib = _open(_LIB_PATH)
     return _lib
+
+
+def _load_marshal() -> None:
+    """Loads the extension that marshals the calls around the paged cache (built beside the library); raises if absent."""
+    global _marshal
+    if _marshal is None:
+        if not _MARSHAL_PATH.exists():
+            raise RuntimeError(f"{_MARSHAL_PATH} is missing: build it with `python -m paper_2510_25739_b200.build`")
+        spec = importlib.util.spec_from_file_location("_hawk_marshal", _MARSHAL_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _marshal = module
 
 
 @contextlib.contextmanager
@@ -116,6 +102,7 @@ def alternate_library(path):
     if not Path(path).exists():
         raise RuntimeError(f"{path} is missing")
     saved = _lib
+    _load_marshal()
     _lib = _open(Path(path))
     try:
         yield _lib
@@ -173,13 +160,15 @@ def _open(path: Path) -> ctypes.CDLL:
     lib.hawk_pool_sample_workspace_bytes.argtypes = [i32, i32]
     lib.hawk_pool_sample.restype = i32
     lib.hawk_pool_sample.argtypes = [vp] * 4 + [i32] * 6 + [vp, sz, vp, vp]
-    for name, args in (("hawk_qk_norm_rope", QkRopeArgs), ("hawk_rope_append", RopeAppendArgs), ("hawk_paged_attn", PagedAttnArgs)):
+    for name in ("hawk_qk_norm_rope", "hawk_rope_append", "hawk_paged_attn"):  # (argument struct, status word, stream)
         getattr(lib, name).restype = i32
-        getattr(lib, name).argtypes = [ctypes.POINTER(args), vp, vp]
+        getattr(lib, name).argtypes = [vp, vp, vp]
     lib.hawk_paged_attn_workspace_bytes.restype = sz
     lib.hawk_paged_attn_workspace_bytes.argtypes = [i32] * 7
     lib.hawk_verify_step_host.restype = i32
     lib.hawk_verify_step_host.argtypes = [ctypes.POINTER(StepHostArgs), vp]
+    for name in ("qk_norm_rope", "rope_append", "paged_attn", "paged_attn_workspace_bytes"):  # for the marshalling extension
+        setattr(lib, "address_" + name, ctypes.cast(getattr(lib, "hawk_" + name), vp).value)
     return lib
 
 
@@ -551,131 +540,6 @@ def pool_sample(pool_q: torch.Tensor, u: torch.Tensor, node_q: torch.Tensor, v_b
     return node_token
 
 
-_DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1}
-_NORM_CODES = {"none": 0, "rms": 1, "layer": 2}
-
-
-def _refuse(t: torch.Tensor, name: str, dtype, shape, index: int, dense: bool) -> None:
-    """Says what is wrong with a tensor that a call's own quick test did not take."""
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.get_device() != index:
-        raise ValueError(f"{name}: must be on cuda:{index}, is on {t.device}")
-    raise ValueError(f"{name}: must be contiguous" if dense else f"{name}: the head dimension must be contiguous")
-
-
-# The three calls below run once a layer on tensors of a few kilobytes, so what they cost on the host counts: a tensor
-# is looked at once, in one expression, and only a refusal takes the time to say why.
-def _heads(t: torch.Tensor, name: str, dtype, shape, index: int):
-    """(pointer, row stride, head stride) of a [rows, heads, D] tensor whose last dimension is dense."""
-    st = t.stride()
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or st[2] != 1:
-        _refuse(t, name, dtype, shape, index, False)
-    return t.data_ptr(), st[0], st[1]
-
-
-def _dense(t: Optional[torch.Tensor], name: str, dtype, shape, index: int):
-    """Pointer of a contiguous tensor, None for None."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
-        _refuse(t, name, dtype, shape, index, True)
-    return t.data_ptr()
-
-
-def _call(name: str, args: ctypes.Structure, dev_status: Optional[torch.Tensor], index: int) -> None:
-    """Runs an entry point on GPU `index` and its current stream."""
-    fn = getattr(_lib or load_library(), name)
-    status = None if dev_status is None else _dense(dev_status, "dev_status", torch.int32, (1,), index)
-    stream = torch._C._cuda_getCurrentRawStream(index)  # (a Stream object costs 3 us)
-    if index == torch.cuda.current_device():
-        rc = fn(ctypes.byref(args), status, stream)
-    else:
-        with torch.cuda.device(index):
-            rc = fn(ctypes.byref(args), status, stream)
-    if rc != 0:
-        raise HawkError(rc, name)
-
-
-def _cuda_16bit(t: torch.Tensor, name: str):
-    """(dtype code, GPU index) of the tensor that decides both for a call."""
-    index = t.get_device()
-    if index < 0:
-        raise ValueError(f"{name}: must be a CUDA tensor")
-    code = _DTYPE_CODES.get(t.dtype)
-    if code is None:
-        raise TypeError(f"{name}: expected torch.bfloat16 or torch.float16, got {t.dtype}")
-    return code, index
-
-
-def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, dtype, H_kv: int, D: int, index: int):
-    """Page count, page size, pointers and strides (page, head, row) of the two [n_pages, H_kv, page_size, D] tensors."""
-    shape = k_pages.shape
-    if len(shape) != 4:
-        raise ValueError(f"k_pages: expected [n_pages, H_kv, page_size, D], got {tuple(shape)}")
-    n_pages, _, page_size, _ = shape
-    ks, vs = k_pages.stride(), v_pages.stride()
-    want = (n_pages, H_kv, page_size, D)
-    if k_pages.dtype is not dtype or shape != want or k_pages.get_device() != index or ks[3] != 1:
-        _refuse(k_pages, "k_pages", dtype, want, index, False)
-    if v_pages.dtype is not dtype or v_pages.shape != want or v_pages.get_device() != index or vs[3] != 1:
-        _refuse(v_pages, "v_pages", dtype, want, index, False)
-    return n_pages, page_size, (k_pages.data_ptr(), v_pages.data_ptr(), *ks[:3], *vs[:3])
-
-
-_ABSENT = (None, 0, 0)
-
-
-def _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved, q_out, k_out, dense_k):
-    """QkRopeArgs, the output tensors (allocated where none was given), the GPU and (T, D)."""
-    x = k if q is None else q
-    code, index = _cuda_16bit(x, "k" if q is None else "q")
-    dt = x.dtype
-    T, _, D = x.shape
-    kind = _NORM_CODES.get(norm)
-    if kind is None:
-        raise ValueError(f"norm: expected one of {tuple(_NORM_CODES)}, got {norm!r}")
-    H = H_kv = n_pos = rot = per_head = 0
-    qp = qop = kp = kop = _ABSENT
-    if q is not None:
-        shape = q.shape
-        H = shape[1]
-        qp = _heads(q, "q", dt, shape, index)
-        if q_out is None:
-            q_out = torch.empty(shape, dtype=dt, device=x.device)
-        qop = _heads(q_out, "q_out", dt, shape, index)
-    if k is not None:
-        H_kv = k.shape[1]
-        shape = (T, H_kv, D)
-        kp = _heads(k, "k", dt, shape, index)
-        if dense_k:
-            if k_out is None:
-                k_out = torch.empty(shape, dtype=dt, device=x.device)
-            kop = _heads(k_out, "k_out", dt, shape, index)
-    wq = wk = bq = bk = cs = pos = None
-    if kind:
-        first = k_weight if q_weight is None else q_weight
-        per_head = 0 if first is None else first.dim() - 1
-        qs, ks = ((H, D), (H_kv, D)) if per_head else ((D,), (D,))
-        wq = _dense(q_weight, "q_weight", dt, qs, index)
-        wk = _dense(k_weight, "k_weight", dt, ks, index)
-        if q_bias is not None:
-            bq = _dense(q_bias, "q_bias", dt, qs, index)
-        if k_bias is not None:
-            bk = _dense(k_bias, "k_bias", dt, ks, index)
-    if cos_sin is not None:
-        if position is None:
-            raise ValueError("position: needed with cos_sin")
-        shape = cos_sin.shape
-        n_pos, rot = shape
-        cs = _dense(cos_sin, "cos_sin", torch.float32, shape, index)
-        pos = _dense(position, "position", torch.int32, (T,), index)
-    return QkRopeArgs(code, T, H, H_kv, D, kind, per_head, rot, n_pos, 1 if interleaved else 0, eps, qp[0], kp[0], qop[0], kop[0],
-                      qp[1], qp[2], kp[1], kp[2], qop[1], qop[2], kop[1], kop[2], wq, wk, bq, bk, pos, cs), q_out, k_out, index, dt, T, D
-
-
 def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], position: Optional[torch.Tensor],
                  cos_sin: Optional[torch.Tensor], norm: str = "none", eps: float = 1e-6,
                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
@@ -685,11 +549,11 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], position:
     """Norm of every head ("none", "rms", "layer"), then the position rotation: q [T,H,D], k [T,H_kv,D] (bf16 or fp16, any
     row and head strides) -> (q_out, k_out).  cos_sin fp32 [positions, rot_dim] holds cosines, then sines, of each position;
     position int32 [T]; None for both: no rotation.  Weights and biases are [D], or [heads, D] one for each head."""
-    if q is None and k is None:
-        raise ValueError("q, k: one of them is needed")
-    args, q_out, k_out, index, _, _, _ = _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias,
-                                                    interleaved, q_out, k_out, True)
-    _call("hawk_qk_norm_rope", args, dev_status, index)
+    lib = _lib or load_library()
+    rc, q_out, k_out = _marshal.qk_norm_rope(lib.address_qk_norm_rope, q, k, position, cos_sin, norm, eps, q_weight, k_weight,
+                                             q_bias, k_bias, interleaved, q_out, k_out, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_qk_norm_rope")
     return q_out, k_out
 
 
@@ -702,18 +566,11 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos
     """New rows k, v [T,H_kv,D] into k_pages, v_pages [n_pages,H_kv,page_size,D] (any page, head and row strides), k normalised
     and rotated as by qk_norm_rope; q [T,H,D] goes the same way into q_out, which is returned.  Stream s owns rows
     row_begin[s] .. row_begin[s+1]-1; kv_len [S] counts its keys with the new ones; block_table [S, pages a stream]."""
-    args, q_out, _, index, dt, T, D = _rope_args(q, k, position, cos_sin, norm, eps, q_weight, k_weight, q_bias, k_bias,
-                                                 interleaved, q_out, None, False)
-    H_kv = args.H_kv
-    vp = _heads(v, "v", dt, (T, H_kv, D), index)
-    n_pages, page_size, pages = _pages(k_pages, v_pages, dt, H_kv, D, index)
-    shape = block_table.shape
-    S, width = shape
-    full = RopeAppendArgs(args, *vp, *pages, n_pages, page_size, S, width,
-                          _dense(block_table, "block_table", torch.int32, shape, index),
-                          _dense(row_begin, "row_begin", torch.int32, (S + 1,), index),
-                          _dense(kv_len, "kv_len", torch.int32, (S,), index))
-    _call("hawk_rope_append", full, dev_status, index)
+    lib = _lib or load_library()
+    rc, q_out = _marshal.rope_append(lib.address_rope_append, q, k, position, cos_sin, v, k_pages, v_pages, block_table, row_begin,
+                                     kv_len, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved, q_out, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_rope_append")
     return q_out
 
 
@@ -728,33 +585,11 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, bl
     """Attention of the new rows q [T,H,D] over the paged cache that already holds their keys (rope_append) -> out [T,H*D].
     max_new and max_kv bound the rows a stream brings and its keys.  With anc_mask (int64 tensor holding the uint64 masks,
     [max_new]) the rows of a stream are nodes of a candidate tree.  Rows of no stream are left as they are in `out`."""
-    code, index = _cuda_16bit(q, "q")
-    dt = q.dtype
-    shape = q.shape
-    T, H, D = shape
-    qp = _heads(q, "q", dt, shape, index)
-    H_kv = k_pages.shape[1]
-    n_pages, page_size, pages = _pages(k_pages, v_pages, dt, H_kv, D, index)
-    shape = block_table.shape
-    S, width = shape
-    if out is None:
-        out = torch.empty((T, H * D), dtype=dt, device=q.device)
-    ws, ws_bytes = None, 0
-    if workspace is None:
-        ws_bytes = (_lib or load_library()).hawk_paged_attn_workspace_bytes(S, T, max_new, H, H_kv, D, max_kv)
-        if ws_bytes:
-            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
-            ws = workspace.data_ptr()
-    else:
-        ws = _dense(workspace, "workspace", workspace.dtype, workspace.shape, index)
-        ws_bytes = workspace.numel() * workspace.element_size()
-    args = PagedAttnArgs(code, S, T, max_new, max_kv, H, H_kv, D, n_pages, page_size, width, sm_scale, *qp, *pages,
-                         _dense(block_table, "block_table", torch.int32, shape, index),
-                         _dense(row_begin, "row_begin", torch.int32, (S + 1,), index),
-                         _dense(kv_len, "kv_len", torch.int32, (S,), index),
-                         _dense(anc_mask, "anc_mask", torch.int64, (max_new,), index),
-                         _dense(out, "out", dt, (T, H * D), index), ws, ws_bytes)
-    _call("hawk_paged_attn", args, dev_status, index)
+    lib = _lib or load_library()
+    rc, out = _marshal.paged_attn(lib.address_paged_attn, lib.address_paged_attn_workspace_bytes, q, k_pages, v_pages, block_table,
+                                  row_begin, kv_len, max_new, max_kv, sm_scale, anc_mask, out, workspace, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_paged_attn")
     return out
 
 

@@ -1,7 +1,8 @@
 """Builds the C-ABI shared library (libhawk_verify.so) in-tree with nvcc for sm_100a.
 
 nvcc cross-compiles without a GPU.  The library links the CUDA runtime statically and reaches the
-one driver call it needs (tensor-map encoding) through the runtime's driver entry point.
+one driver call it needs (tensor-map encoding) through the runtime's driver entry point.  A small Python extension (host code) beside
+it marshals the calls that run once a layer.
 """
 from __future__ import annotations
 
@@ -9,6 +10,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
@@ -43,6 +45,8 @@ def build(force: bool = False, verbose: bool = False, lib: Path = LIB, objdir: P
           extra_flags=()) -> Path:
     """Compiles every source to an object of its own (in parallel; only the ones whose source or headers changed)
     and links them into `lib`."""
+    if lib == LIB:
+        build_marshal(force=force)
     objdir = objdir or (PKG / "_build")
     objdir.mkdir(exist_ok=True)
     tag = objdir / "flags.txt"
@@ -83,6 +87,33 @@ def build(force: bool = False, verbose: bool = False, lib: Path = LIB, objdir: P
         raise RuntimeError("nvcc failed linking " + lib.name)
     os.replace(tmp, lib)
     return lib
+
+
+MARSHAL_SOURCE = CSRC / "hawk_marshal.cpp"
+MARSHAL_LIB = PKG / ("_hawk_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
+def build_marshal(force: bool = False) -> Path:
+    """Compiles the Python extension that turns tensors into the argument structs of the calls around the paged cache (host
+    code only; links the torch libraries that the process has loaded anyway)."""
+    newest = max(MARSHAL_SOURCE.stat().st_mtime, (PKG.parent / "include" / "hawk.h").stat().st_mtime)
+    if not force and MARSHAL_LIB.exists() and MARSHAL_LIB.stat().st_mtime >= newest:
+        return MARSHAL_LIB
+    import torch
+    root = Path(torch.__file__).resolve().parent
+    cuda = Path(_nvcc()).resolve().parent.parent
+    tmp = MARSHAL_LIB.with_suffix(f".{os.getpid()}.tmp")
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", sysconfig.get_paths()["include"],
+           "-isystem", str(root / "include"), "-isystem", str(root / "include" / "torch" / "csrc" / "api" / "include"),
+           "-isystem", str(cuda / "include"), str(MARSHAL_SOURCE), "-o", str(tmp), "-L", str(root / "lib"),
+           "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError("g++ failed on " + MARSHAL_SOURCE.name)
+    os.replace(tmp, MARSHAL_LIB)
+    return MARSHAL_LIB
 
 
 STALL_LIB = PKG / "libhawk_verify_stall.so"

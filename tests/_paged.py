@@ -1,4 +1,6 @@
 """Ragged batches over a paged cache for the tests of the calls around it (inputs only, no arithmetic of the method)."""
+import ctypes
+
 import numpy as np
 import torch
 
@@ -89,3 +91,36 @@ def rope_table(positions, rot, grid=0, seed=None):
     else:
         angle = np.outer(at, 10000.0 ** (-np.arange(half) / half))
     return torch.from_numpy(np.concatenate([np.cos(angle), np.sin(angle)], 1).astype(np.float32))
+
+
+# ---- the argument structs of include/hawk.h, for the tests of the C ABI's refusals
+class QkRopeArgs(ctypes.Structure):
+    """Mirror of hawk_qk_rope_args (include/hawk.h)."""
+    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "T", "H", "H_kv", "D", "norm", "per_head", "rot_dim", "n_positions",
+                                             "interleaved")]
+                + [("eps", ctypes.c_float)]
+                + [(n, ctypes.c_void_p) for n in ("q", "k", "q_out", "k_out")]
+                + [(f"{t}_{w}_stride", ctypes.c_longlong) for t in ("q", "k", "q_out", "k_out") for w in ("row", "head")]
+                + [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "q_bias", "k_bias", "position", "cos_sin")])
+
+
+_PAGE_STRIDES = [(f"{t}_{w}_stride", ctypes.c_longlong) for t in "kv" for w in ("page", "page_head", "page_row")]
+
+
+class RopeAppendArgs(ctypes.Structure):
+    """Mirror of hawk_rope_append_args (include/hawk.h)."""
+    _fields_ = ([("qk", QkRopeArgs), ("v", ctypes.c_void_p), ("v_row_stride", ctypes.c_longlong),
+                 ("v_head_stride", ctypes.c_longlong), ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p)]
+                + _PAGE_STRIDES + [(n, ctypes.c_int) for n in ("n_pages", "page_size", "S", "table_width")]
+                + [(n, ctypes.c_void_p) for n in ("block_table", "row_begin", "kv_len")])
+
+
+class PagedAttnArgs(ctypes.Structure):
+    """Mirror of hawk_paged_attn_args (include/hawk.h)."""
+    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "S", "T", "max_new", "max_kv", "H", "H_kv", "D", "n_pages", "page_size",
+                                             "table_width")]
+                + [("sm_scale", ctypes.c_float), ("q", ctypes.c_void_p), ("q_row_stride", ctypes.c_longlong),
+                   ("q_head_stride", ctypes.c_longlong), ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p)]
+                + _PAGE_STRIDES
+                + [(n, ctypes.c_void_p) for n in ("block_table", "row_begin", "kv_len", "anc_mask", "out", "workspace")]
+                + [("workspace_bytes", ctypes.c_size_t)])

@@ -8,6 +8,7 @@ import torch
 
 from oracle import paged
 from paper_2510_25739_b200 import binding, build
+from tests._paged import PagedAttnArgs, QkRopeArgs, RopeAppendArgs
 
 OK, E_NULL, E_SHAPE, E_ALIGN, E_UNSUP, E_WS, E_PARAM, E_CUDA = range(8)
 P, ODD = 0x1000, 0x1004
@@ -20,7 +21,7 @@ def lib():
 
 
 def _qk(**kw):
-    a = binding.QkRopeArgs()
+    a = QkRopeArgs()
     for name, _ in a._fields_:
         if name in ("q", "k", "q_out", "k_out", "q_weight", "k_weight", "q_bias", "k_bias", "position", "cos_sin"):
             setattr(a, name, P)
@@ -49,7 +50,7 @@ def test_norm_rope_refusals(lib):
 
 
 def _append(**kw):
-    a = binding.RopeAppendArgs()
+    a = RopeAppendArgs()
     a.qk = _qk(**kw.pop("qk", {}))
     for name, _ in a._fields_:
         if name in ("v", "k_pages", "v_pages", "block_table", "row_begin", "kv_len"):
@@ -75,7 +76,7 @@ def test_append_refusals(lib):
 
 
 def _attn(**kw):
-    a = binding.PagedAttnArgs()
+    a = PagedAttnArgs()
     for name, _ in a._fields_:
         if name in ("q", "k_pages", "v_pages", "block_table", "row_begin", "kv_len", "out"):
             setattr(a, name, P)
@@ -128,8 +129,8 @@ def test_struct_fields_match_the_header():
     import re
     from pathlib import Path
     text = (Path(__file__).resolve().parent.parent / "include" / "hawk.h").read_text()
-    for struct, cls in (("hawk_qk_rope_args", binding.QkRopeArgs), ("hawk_rope_append_args", binding.RopeAppendArgs),
-                        ("hawk_paged_attn_args", binding.PagedAttnArgs)):
+    for struct, cls in (("hawk_qk_rope_args", QkRopeArgs), ("hawk_rope_append_args", RopeAppendArgs),
+                        ("hawk_paged_attn_args", PagedAttnArgs)):
         body = re.search(r"typedef struct " + struct + r" \{(.*?)\} " + struct + ";", text, re.S).group(1)
         names = []
         for decl in re.sub(r"/\*.*?\*/", "", body, flags=re.S).split(";"):
