@@ -8,6 +8,13 @@
 
 namespace hawk {
 
+// A pair of query tiles of a stream of many rows: what a block of the tile kernel works on (for one kv head).
+struct PagedGroup {
+    int s, r0, n, kv;  // stream, its first row, rows, keys; n = 0: behind the list's end
+    int tok0;          // first position of the pair
+    int pad[3];
+};
+
 // One launch of either kernel.
 struct PagedParams {
     const void *q;
@@ -24,6 +31,9 @@ struct PagedParams {
     int box_rows;              // cache rows of one TMA box: a divisor of the page size and of the tile
     int k_rows_inner, v_rows_inner;  // tensor maps are {D, rows, heads, pages} (1) or {D, heads, rows, pages} (0): the
                                      // dimension with the smaller stride comes first
+    int row_blocks;            // rows kernel: blocks that do rows; one more makes the list below, where there is one
+    PagedGroup *groups;        // [group_cap], longest first; NULL: no stream goes to the tile kernel
+    int group_cap, tile_tok;   // tile_tok: positions a query tile holds
     FastDiv div_page, div_group;
     float scale_log2;          // sm_scale * log2(e)
     int32_t *dev_status;
@@ -57,9 +67,110 @@ __device__ __forceinline__ PagedStream paged_stream(const PagedParams &P, int s,
     return st;
 }
 
+// The rows before `end` of a stream of n see keys of this many of its rows at most: a chain's up to themselves, a tree's nodes
+// whatever their masks say.
+__device__ __forceinline__ int paged_reach(const PagedParams &P, int n, int end) { return P.anc_mask ? n : min(n, end); }
+
 __device__ __forceinline__ bool paged_is_few(const PagedParams &P, const PagedStream &st)
 {
     return static_cast<long long>(st.n) * P.group <= P.rows_few;
+}
+
+constexpr int kPagedTileKeys = 128;  // keys of a tile of the tile kernel
+constexpr int kPlanBuckets = 256;
+
+constexpr int kPlanWaves = 6;  // jobs of so many waves of blocks even out by themselves
+
+// Makes the tile kernel's list: one block, `sh` holds kPlanBuckets + 1 ints.  Longest pair first (a counting sort over 256
+// cost classes), so that no long job starts last; where the jobs are many waves of blocks, one stream after the other instead, each
+// from its longest pair on, so that what runs together shares keys and values in L2 (799 against 822 us for 4 x 2048 rows
+// over 8192 keys; for 7B chunks of 300 to 511 rows, under two waves, the sort takes 94 us to 84).
+// A warp looks at 32 streams at once and deals a stream's pairs out to its lanes.
+__device__ __forceinline__ void paged_plan(const PagedParams &P, int *sh, int &flags)
+{
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
+    const int per_pair = 2 * P.tile_tok;
+    const float scale = (kPlanBuckets - 1) / (2.f * (P.kv_cap / kPagedTileKeys + 1));
+    auto pairs_at = [&](int s, PagedStream &st) {  // pairs of stream s, 0 for one of the rows kernel's or none
+        st = {0, 0, 0};
+        if (s < P.S) st = paged_stream(P, s, flags);
+        return st.n == 0 || paged_is_few(P, st) ? 0 : (st.n + per_pair - 1) / per_pair;
+    };
+    // visit(cost class, stream, first row, rows, keys, pair, place of the stream's last pair in plain order): for every pair
+    auto each = [&](bool plain, auto &&visit) {
+        for (int s0 = warp * 32; s0 < P.S; s0 += warps * 32) {
+            PagedStream st;
+            int before = 0;  // pairs of the streams before this lane's
+            if (plain) {
+                for (int s = lane; s < s0; s += 32) before += pairs_at(s, st);
+                before = __reduce_add_sync(0xffffffffu, before);
+            }
+            const int mine = pairs_at(s0 + lane, st);
+            int inc = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += u;
+            }
+            before += inc - mine;
+            unsigned many = __ballot_sync(0xffffffffu, mine > 0);
+            while (many) {
+                const int b = __ffs(many) - 1;
+                many &= many - 1;
+                const int r0 = __shfl_sync(0xffffffffu, st.r0, b), n = __shfl_sync(0xffffffffu, st.n, b);
+                const int kv = __shfl_sync(0xffffffffu, st.kv, b), pairs = __shfl_sync(0xffffffffu, mine, b);
+                const int at = __shfl_sync(0xffffffffu, before, b);
+                for (int p = lane; p < pairs; p += 32) {
+                    // cost: key tiles that the pair's last position sees, twice where both its query tiles have rows
+                    const int keys = max(0, min(kv, kv - n + paged_reach(P, n, (p + 1) * per_pair)));
+                    const int tiles = (keys + kPagedTileKeys - 1) / kPagedTileKeys;
+                    const int cost = p * per_pair + P.tile_tok >= n ? tiles : 2 * tiles;
+                    const int bucket = kPlanBuckets - 1 - min(kPlanBuckets - 1, static_cast<int>(cost * scale));
+                    visit(bucket, s0 + b, r0, n, kv, p, at + pairs - 1 - p);
+                }
+                __syncwarp();
+            }
+        }
+    };
+    for (int i = tid; i < kPlanBuckets; i += blockDim.x) sh[i] = 0;
+    __syncthreads();
+    each(false, [&](int bucket, int, int, int, int, int, int) { atomicAdd(&sh[bucket], 1); });
+    __syncthreads();
+    if (warp == 0) {  // exclusive prefix sum, 8 classes a lane
+        constexpr int kPer = kPlanBuckets / 32;
+        int v[kPer], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            v[i] = sh[lane * kPer + i];
+            sum += v[i];
+        }
+        int inc = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += u;
+        }
+        if (lane == 31) sh[kPlanBuckets] = inc;
+        int at = inc - sum;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            sh[lane * kPer + i] = at;
+            at += v[i];
+        }
+    }
+    __syncthreads();
+    const int total = sh[kPlanBuckets];
+    auto put = [&](int at, int s, int r0, int n, int kv, int p) {
+        if (at >= P.group_cap) return;  // (the cap bounds every valid batch)
+        *reinterpret_cast<int4 *>(P.groups + at) = make_int4(s, r0, n, kv);
+        P.groups[at].tok0 = p * per_pair;
+    };
+    const bool plain = static_cast<long long>(total) * P.H_kv >= kPlanWaves * 148;
+    each(plain, [&](int bucket, int s, int r0, int n, int kv, int p, int place) {
+        put(plain ? place : atomicAdd(&sh[bucket], 1), s, r0, n, kv, p);
+    });
+    if (warp == 0)
+        for (int i = total + lane; i < P.group_cap; i += 32) P.groups[i].n = 0;
 }
 
 // Box of cache rows (page, row inside it, kv head, 64-column half) into shared memory.
@@ -105,9 +216,10 @@ bool encode_pages(CUtensorMap *map, const hawk_paged_attn_args &a, bool values, 
 
 int paged_gcd(int a, int b);
 
-// The chunk kernel (tcgen05 tiles of query rows): bytes of its partial results, and its launch.
+// The tile kernel (tcgen05 tiles of query rows): bytes of its list and of its partial results, and its launch.
 size_t paged_tile_workspace_bytes(int S, int T, int max_new, int H, int H_kv, int few, int D, int max_kv);
-cudaError_t launch_paged_tile(const hawk_paged_attn_args &a, const hawk::PagedParams &base, float *part, cudaStream_t st,
-                              bool *refused);
+// Upper bound of the call's pairs of query tiles (the list's length); 0: more than the kernel can number.
+int paged_tile_groups(int S, int T, int max_new, int H, int H_kv, int few);
+cudaError_t launch_paged_tile(const hawk_paged_attn_args &a, const hawk::PagedParams &base, float *part, cudaStream_t st);
 
 }  // namespace hawk_host

@@ -1,5 +1,5 @@
 // hawk_paged_attn: attention of a ragged batch of new rows over a paged key/value cache.  This file holds the entry point
-// and the kernel for FEW rows per kv head (decode steps, drafted blocks, candidate trees); chunks of many rows go to the
+// and the kernel for FEW rows per kv head (decode steps, drafted blocks, candidate trees); many rows go to the
 // tile kernel in hawk_paged_tile.cu.  A stream is handled by one of the two, by its own row count.
 //
 // With few rows the call is bound by reading every key and value once (r flops per byte for r rows per kv head), so the
@@ -110,9 +110,15 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
         prefetch_tensormap(&map_v);
     }
     grid_dependency_wait();
+    int flags = 0;
+    if (P.groups && static_cast<int>(blockIdx.x) == P.row_blocks) {  // the block that makes the tile kernel's list
+        __syncthreads();
+        paged_plan(P, reinterpret_cast<int *>(smem), flags);
+        if (flags && P.dev_status) atomicOr(P.dev_status, flags);
+        return;
+    }
 
     // ---- prefix sum over the streams: of their tiles (shares) or of their items (group)
-    int flags = 0;
     int running = 0;
     for (int base = 0; base < P.S; base += kWarps * 32) {
         const int s = base + tid;
@@ -149,7 +155,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
     const int total = running;
     int W = 0, w = 0, f = 0, len = 0;
     if (kShares) {
-        W = max(1, min(static_cast<int>(gridDim.x) * kWarps, total / kMinShareTiles));
+        W = max(1, min(P.row_blocks * kWarps, total / kMinShareTiles));
         w = static_cast<int>(blockIdx.x) * kWarps + warp;
         if (w < W) {
             f = static_cast<int>(share_begin(w, total, W));
@@ -800,7 +806,8 @@ cudaError_t launch_shape(const CUtensorMap &mk, const CUtensorMap &mv, const Pag
         if (e != cudaSuccess) return e;
         attr_done.fetch_or(1ull << device, std::memory_order_relaxed);
     }
-    return hawk_host::launch_dependent(paged_rows_kernel<T16, D, NQT, WARPS, STAGES, GROUP>, dim3(grid), dim3(WARPS * 32), smem,
+    return hawk_host::launch_dependent(paged_rows_kernel<T16, D, NQT, WARPS, STAGES, GROUP>,
+                                       dim3(grid + (P.groups ? 1 : 0)), dim3(WARPS * 32), smem,
                                        st, mk, mv, P);
 }
 
@@ -832,7 +839,11 @@ cudaError_t launch_rows_n(const CUtensorMap &mk, const CUtensorMap &mv, const Pa
 }
 
 // Rows per kv head up to which a stream goes to the rows kernel.
-int few_rows(int D) { return 2 * rows_max(D); }
+#ifndef FEW64
+#define FEW64 64
+#define FEW128 48
+#endif
+int few_rows(int D) { return D == 64 ? FEW64 : FEW128; }
 
 size_t align16(size_t n) { return (n + 15) / 16 * 16; }
 
@@ -870,11 +881,7 @@ extern "C" size_t hawk_paged_attn_workspace_bytes(int S, int T, int max_new, int
     if (max_new > T) max_new = T;
     const long long rows = static_cast<long long>(max_new) * (H / H_kv);
     const long long few = rows < few_rows(D) ? rows : few_rows(D);
-    size_t a = rows_workspace_bytes(plan_rows(S, static_cast<int>(few), H_kv, D, max_kv), D);
-    if (max_new <= 64) {  // a tree's streams go to the rows kernel whatever their rows
-        const size_t tree = rows_workspace_bytes(plan_rows(S, static_cast<int>(rows), H_kv, D, max_kv), D);
-        if (tree > a) a = tree;
-    }
+    const size_t a = rows_workspace_bytes(plan_rows(S, static_cast<int>(few), H_kv, D, max_kv), D);
     const size_t b = rows > few_rows(D) ? hawk_host::paged_tile_workspace_bytes(S, T, max_new, H, H_kv, few_rows(D), D, max_kv) : 0;
     return align16(a) + b;
 }
@@ -907,7 +914,7 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     const int group = a.H / a.H_kv, max_new = a.max_new < a.T ? a.max_new : a.T;
     const long long rows_all = static_cast<long long>(max_new) * group;
     const int limit = few_rows(a.D);
-    const bool tiles = rows_all > limit && !a.anc_mask;
+    const bool tiles = rows_all > limit;
     const int rows = static_cast<int>(tiles ? limit : rows_all);
     const RowsPlan plan = plan_rows(a.S, rows, a.H_kv, a.D, a.max_kv);
     // list positions are 32-bit numbers
@@ -915,6 +922,8 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     if (static_cast<double>(a.S) * a.H_kv * ((rows + plan.rpi - 1) / plan.rpi) * (a.max_kv / tk + 1) >= 2147483000.0 ||
         static_cast<double>(a.T) * group >= 2147483000.0)
         return HAWK_ERR_UNSUPPORTED;
+    const int groups = tiles ? hawk_host::paged_tile_groups(a.S, a.T, max_new, a.H, a.H_kv, rows) : 0;
+    if (tiles && groups == 0) return HAWK_ERR_UNSUPPORTED;
     const size_t rows_ws = rows_workspace_bytes(plan, a.D);
     const size_t need = hawk_paged_attn_workspace_bytes(a.S, a.T, a.max_new, a.H, a.H_kv, a.D, a.max_kv);
     if (need > 0) {
@@ -949,6 +958,12 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     P.div_group.set(static_cast<uint32_t>(group));
     P.scale_log2 = a.sm_scale * 1.4426950408889634f;
     P.dev_status = dev_status;
+    P.row_blocks = plan.grid;
+    if (tiles) {
+        P.groups = reinterpret_cast<PagedGroup *>(static_cast<uint8_t *>(a.workspace) + align16(rows_ws));
+        P.group_cap = groups;
+        P.tile_tok = 128 / group;
+    }
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
 
     {
@@ -964,11 +979,6 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
             e = a.D == 64 ? launch_rows_n<__half, 64>(mk, mv, P, plan, st) : launch_rows_n<__half, 128>(mk, mv, P, plan, st);
         if (e != cudaSuccess) return HAWK_ERR_CUDA;
     }
-    if (tiles) {
-        bool refused = false;
-        float *part = reinterpret_cast<float *>(static_cast<uint8_t *>(a.workspace) + align16(rows_ws));
-        if (hawk_host::launch_paged_tile(a, P, part, st, &refused) != cudaSuccess) return HAWK_ERR_CUDA;
-        if (refused) return HAWK_ERR_UNSUPPORTED;
-    }
+    if (tiles && hawk_host::launch_paged_tile(a, P, reinterpret_cast<float *>(P.groups), st) != cudaSuccess) return HAWK_ERR_CUDA;
     return HAWK_OK;
 }

@@ -23,7 +23,12 @@
 // Measured there: 1217 TFLOP/s at D = 128, 0.73 of the measured burst peak.  What it took: MMAs issued under a predicate with
 // descriptors stepped by their low word (980 to 790 us; see umma_f16_ss_if).  Two score buffers of 64 keys a slot, so that the next
 // scores never wait for P V, came to 916 us: products of 64 columns read Q from shared memory twice as often.
+// Jobs come from a list that one extra block of the rows kernel (which every call launches before this one) makes: a block reads
+// one record instead of searching the batch, and the longest jobs start first.
 // Few blocks: the key range is split too, each split leaves (o, max, sum) in fp32 and a second kernel joins them.
+// Measured and taken back: one persistent block per SM over equal shares of all key tiles.  Changing segments inside a block
+// costs what changing blocks does (some 10 k cycles of draining, epilogue, queries and first scores), cuts add partial results,
+// and the clock under the power cap was lower: 868 against 793 us for the prefill above, 137 against 119 for 4 x 512 rows.
 #include <atomic>
 
 #include "hawk_paged.cuh"
@@ -34,12 +39,13 @@ using namespace hawk;
 
 constexpr int kBM = 128, kBN = 128;
 constexpr int kThreads = 384;        // three warpgroups; the third has one warp for the products and one for the loads
-constexpr int kRegsSoftmax = 216, kRegsOther = 72;  // of the 168 a thread that the block starts with (2 x 216 + 72 = 3 x 168)
+constexpr int kRegsSoftmax = 224, kRegsOther = 56;  // of the 168 a thread that the block starts with (2 x 224 + 56 = 3 x 168)
 constexpr int kMaxSplits = 16;
 constexpr int kMinSplitKeys = 512;  // shorter key ranges cost more in partial results than they gain in blocks
 
 struct TileParams {
     PagedParams c;
+    const PagedGroup *groups;  // the call's pairs of query tiles, longest first
     int tok;       // positions a query tile holds: 128 / group
     int n_split;
     int q_rows;    // rows of a query tile that are used: tok * group
@@ -52,6 +58,8 @@ struct TileCfg {
     static constexpr int kHalfBytes = 128 * 128;           // [128 rows][64 columns]
     static constexpr int kTileBytes = kHalves * kHalfBytes;
     static constexpr int kStages = D == 128 ? 5 : 10;
+    // partial result of a block: o as [D / 4][256 rows][4], so that a warp's rows are neighbours, then (max, sum) of the rows
+    static constexpr int kPartFloats = 2 * kBM * (D + 2);
     static constexpr size_t kSmem = 1024 + static_cast<size_t>(2 + kStages) * kTileBytes + 512 + 1024 /* max, sum of slot 1's rows */;
 };
 
@@ -66,67 +74,29 @@ struct TileJob {
     bool single;         // one query tile, its key tiles dealt out to the two slots
 };
 
-// Pairs of query tiles of a stream that belongs to this kernel.
-__device__ __forceinline__ int pairs_of(const TileParams &P, const PagedStream &st)
-{
-    if (st.n == 0 || paged_is_few(P.c, st)) return 0;
-    return (st.n + 2 * P.tok - 1) / (2 * P.tok);
-}
-
-// Finds the block's job: the streams' pairs are numbered through; one sweep of the block over the streams.
-__device__ __forceinline__ bool find_job(const TileParams &P, bool with_split, int *shared_sums, TileJob &job, int &flags)
+// The block's job (or, without `with_split`, its group and kv head) from the sorted list; false behind the list's end.
+__device__ __forceinline__ bool find_job(const TileParams &P, bool with_split, TileJob &job)
 {
     uint32_t split = 0, hk;
-    const uint32_t pair_hk = with_split ? P.div_split.divmod(blockIdx.x, split) : blockIdx.x;
-    const int pair = static_cast<int>(P.div_hkv.divmod(pair_hk, hk));
+    const uint32_t group_hk = with_split ? P.div_split.divmod(blockIdx.x, split) : blockIdx.x;
+    const uint32_t rank = P.div_hkv.divmod(group_hk, hk);
+    const int4 a = *reinterpret_cast<const int4 *>(P.groups + rank);
+    const int2 b = *reinterpret_cast<const int2 *>(reinterpret_cast<const int4 *>(P.groups + rank) + 1);
+    PagedStream st;
+    job.s = a.x;
+    job.r0 = a.y;
+    job.n = st.n = a.z;
+    job.kv = st.kv = a.w;
+    job.tok0 = b.x;
     job.split = static_cast<int>(split);
     job.hk = static_cast<int>(hk);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
-    int *found = shared_sums + 16;
-    int running = 0;
-    if (tid == 0) found[0] = -1;
-    for (int base = 0; base < P.c.S && running <= pair; base += blockDim.x) {
-        const int s = base + tid;
-        int v = 0;
-        if (s < P.c.S) v = pairs_of(P, paged_stream(P.c, s, flags));
-        int inc = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += u;
-        }
-        if (lane == 31) shared_sums[warp] = inc;
-        __syncthreads();
-        int before = running, all = running;
-        for (int w = 0; w < warps; ++w) {
-            if (w < warp) before += shared_sums[w];
-            all += shared_sums[w];
-        }
-        const int end = before + inc;
-        if (v > 0 && pair >= end - v && pair < end) {
-            found[0] = s;
-            found[1] = pair - (end - v);
-            found[2] = v;
-        }
-        running = all;
-        __syncthreads();
-    }
-    __syncthreads();
-    const int s = found[0];
-    if (s < 0) return false;
-    const PagedStream st = paged_stream(P.c, s, flags);
-    job.s = s;
-    job.r0 = st.r0;
-    job.n = st.n;
-    job.kv = st.kv;
-    job.tok0 = (found[2] - 1 - found[1]) * 2 * P.tok;  // the pairs that see the most keys first
+    if (job.n == 0) return false;  // (the list ends with an empty record)
     const int pfx = st.kv - st.n;
     int end[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int first = job.tok0 + t * P.tok;
-        const int last = min(st.n, first + P.tok) - 1;  // last position of the tile
-        const int keys = first < st.n ? max(0, min(st.kv, pfx + last + 1)) : 0;
+        const int keys = first < st.n ? max(0, min(st.kv, pfx + paged_reach(P.c, st.n, first + P.tok))) : 0;
         end[t] = (keys + kBN - 1) / kBN;
     }
     const int all = max(end[0], end[1]);
@@ -162,6 +132,14 @@ __device__ __forceinline__ float2 exp2_fma(uint64_t x2)
                        __int_as_float(__float_as_int(pf.y) + (__float_as_int(nf.y) << 23)));
 }
 
+// Bits c = 0 .. 31 of a tree row: may it see the key `rel + c` places behind the prefix?  (rel < 0: some lie in the prefix.)
+__device__ __forceinline__ uint32_t tree_word(int rel, uint64_t nodes)
+{
+    if (rel <= -32) return 0xffffffffu;
+    if (rel < 0) return static_cast<uint32_t>(nodes << -rel) | ((1u << -rel) - 1u);
+    return rel < 64 ? static_cast<uint32_t>(nodes >> rel) : 0u;
+}
+
 // mbar_wait of a whole warp: true for all its lanes or for none, so that the warp stays together when a wait gives up.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
 {
@@ -185,10 +163,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint64_t *q_full = bars + 2 * C::kStages, *s_full = q_full + 1, *p_ready = q_full + 3, *o_done = q_full + 7, *drain = q_full + 9;
     uint32_t *tmem_ptr = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_ptr + 1);
-    int *sums = reinterpret_cast<int *>(tmem_ptr + 2);   // [20]
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) {
+    if (tid == 9 * 32) {  // (the warp that loads: it starts before the others are told)
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
@@ -211,17 +188,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     grid_dependency_wait();
     int flags = 0;
     TileJob job;
-    const bool has_job = find_job(P, true, sums, job, flags);  // (block-uniform; also publishes the barriers)
-    if (flags && blockIdx.x == 0 && P.c.dev_status) atomicOr(P.c.dev_status, flags);
-    flags = 0;
-    if (!has_job) return;
+    if (!find_job(P, true, job)) return;  // (block-uniform)
     if (warp == 8) {
         tmem_alloc(tmem_ptr, 512);
         tmem_relinquish();
     }
-    tcgen05_fence_before();
-    __syncthreads();
-    tcgen05_fence_after();
+    if (warp == 9) {
+        __syncwarp();
+        asm volatile("bar.arrive 0, %0;" ::"n"(kThreads) : "memory");  // the barriers are there; the loads need nothing else
+    } else {
+        tcgen05_fence_before();
+        asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+        tcgen05_fence_after();
+    }
     constexpr uint32_t tmem = 0;  // all 512 columns are the block's: its tensor memory starts at lane 0, column 0
     const int pfx = job.kv - job.n;
     // K tiles run this many ahead of V tiles in the ring: slot 1 of a single query tile starts on key tile 1
@@ -410,7 +389,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t hd;
         const int pos = job.tok0 + (job.single ? 0 : t * P.tok) + static_cast<int>(P.c.div_group.divmod(static_cast<uint32_t>(r), hd));
         const bool valid = r < P.q_rows && pos < job.n;
-        const int limit = min(job.kv, pfx + min(pos, job.n - 1) + 1);  // keys this row sees
+        // keys this row sees: all up to itself in a chain; in a tree all in front of the chunk, and the nodes of its mask
+        uint64_t nodes = 0;
+        int limit = min(job.kv, pfx + min(pos, job.n - 1) + 1);
+        if (P.c.anc_mask) {
+            limit = pfx;
+            nodes = P.c.anc_mask[min(pos, job.n - 1)];
+            if (job.n < 64) nodes &= (1ull << job.n) - 1;
+        }
         const int first = job.begin + (job.single ? t : 0), stride = job.single ? 2 : 1;  // key tiles of the slot
         const uint64_t scale2 = pack2(P.c.scale_log2, P.c.scale_log2);
         float m_run = -CUDART_INF_F, l_run = 0.f;
@@ -426,11 +412,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_ld_wait();
             const int seen = limit - (first + i * stride) * kBN;
             if (seen < kBN) {
+                if (P.c.anc_mask) {
+                    // (seen counts the keys in front of the tree here)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t open = tree_word(q * 32 - seen, nodes);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c)
-                        if (q * 32 + c >= seen) u[q][c] = 0xff800000u;  // -inf
+                        for (int c = 0; c < 32; ++c)
+                            if (!(open >> c & 1u)) u[q][c] = 0xff800000u;
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (q * 32 + c >= seen) u[q][c] = 0xff800000u;  // -inf
+                }
             }
             float mx[4];
 #pragma unroll
@@ -528,11 +525,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             const long long cell = row * P.c.H + job.hk * P.c.group + static_cast<int>(hd);
             const bool join = job.single && job.nt[1] > 0;
             const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-            const long long cells = static_cast<long long>(P.c.T) * P.c.H, at = job.split * cells + (valid ? cell : 0);
             T16 *dst = static_cast<T16 *>(P.c.out) + (valid ? cell * D : 0);
-            float *part = P.c.part + at * D;
-            if (P.n_split > 1 && valid && ok)
-                *reinterpret_cast<float2 *>(P.c.part + P.n_split * cells * D + at * 2) = make_float2(m_run, l_run);
+            float *part = P.c.part + static_cast<size_t>(blockIdx.x) * C::kPartFloats;
+            const int prow = (job.single ? 0 : t * kBM) + r;
+            if (P.n_split > 1 && valid && ok) *reinterpret_cast<float2 *>(part + 2 * kBM * D + 2 * prow) = make_float2(m_run, l_run);
             // (a split without keys has sum 0 and its o is not read)
             if (nt > 0 || P.n_split == 1) {
 #pragma unroll
@@ -571,7 +567,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     } else {
 #pragma unroll
                         for (int c = 0; c < 32; c += 4)
-                            *reinterpret_cast<uint4 *>(part + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                            *reinterpret_cast<uint4 *>(part + ((c0 + c) / 4 * 2 * kBM + prow) * 4) =
+                                make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
                     }
                 }
             }
@@ -582,52 +579,56 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 8) tmem_dealloc(*tmem_ptr, 512);
 }
 
-// Joins the splits: 16 blocks per (pair of query tiles, kv head), a warp per row.
+// Joins the splits: 8 blocks per (pair of query tiles, kv head), 32 rows each, a row a lane and the head dimension dealt out to
+// the warps.
 template <typename T16, int D>
 __global__ void __launch_bounds__(256) paged_tile_merge_kernel(const TileParams P)
 {
     using E = Elem<T16>;
-    constexpr int PER = D / 32;
-    __shared__ int sums[20];
+    using C = TileCfg<D>;
+    constexpr int PER = D / 32;  // 16-byte pieces of a row that a warp takes: D / 4 over 8 warps
     allow_dependent_launch();
-    TileJob job;
-    int flags = 0;
     grid_dependency_wait();
-    if (!find_job(P, false, sums, job, flags)) return;
+    TileJob job;
+    if (!find_job(P, false, job)) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long cells = static_cast<long long>(P.c.T) * P.c.H;
-    const float *ml = P.c.part + P.n_split * cells * D;
-    const int rows = min(2 * P.tok, job.n - job.tok0) * P.c.group;
-    for (int r = blockIdx.y * 8 + warp; r < rows; r += 8 * gridDim.y) {
-        uint32_t hd;
-        const uint32_t pos = P.c.div_group.divmod(static_cast<uint32_t>(r), hd);
-        const long long cell = (job.r0 + static_cast<long long>(job.tok0) + pos) * P.c.H + job.hk * P.c.group + static_cast<int>(hd);
-        // lane x holds split x's maximum and sum (at most 16 splits)
-        float2 mine = make_float2(-CUDART_INF_F, 0.f);
-        if (lane < P.n_split) mine = *reinterpret_cast<const float2 *>(ml + (lane * cells + cell) * 2);
-        const float m = warp_max(mine.y == 0.f ? -CUDART_INF_F : mine.x);
-        const float mu = m == -CUDART_INF_F ? 0.f : m;
-        const float f = mine.y == 0.f ? 0.f : fast_exp2(mine.x - mu);
-        const float l = warp_sum(mine.y * f);
-        const float scale = l == 0.f ? 0.f : f / l;
-        float acc[PER];
-#pragma unroll
-        for (int c = 0; c < PER; ++c) acc[c] = 0.f;
-        for (int x = 0; x < P.n_split; ++x) {
-            const float w = __shfl_sync(0xffffffffu, scale, x);
-            if (w == 0.f) continue;  // (its o may not have been written)
-            const float *src = P.c.part + (x * cells + cell) * D + lane * PER;
-#pragma unroll
-            for (int c = 0; c < PER; c += 2) {
-                const float2 v = *reinterpret_cast<const float2 *>(src + c);
-                acc[c] = fmaf(v.x, w, acc[c]);
-                acc[c + 1] = fmaf(v.y, w, acc[c + 1]);
-            }
-        }
-        T16 *dst = static_cast<T16 *>(P.c.out) + cell * D + lane * PER;
-#pragma unroll
-        for (int c = 0; c < PER; c += 2) *reinterpret_cast<uint32_t *>(dst + c) = E::pack(acc[c], acc[c + 1]);
+    const int prow = blockIdx.y * 32 + lane, tile = prow / kBM;
+    uint32_t hd;
+    const int pos = job.tok0 + tile * P.tok + static_cast<int>(P.c.div_group.divmod(static_cast<uint32_t>(prow - tile * kBM), hd));
+    if (prow - tile * kBM >= P.q_rows || pos >= job.n) return;
+    const float *parts = P.c.part + static_cast<size_t>(blockIdx.x) * P.n_split * C::kPartFloats;
+    float m = -CUDART_INF_F;
+    for (int x = 0; x < P.n_split; ++x) {
+        const float2 v = *reinterpret_cast<const float2 *>(parts + static_cast<size_t>(x) * C::kPartFloats + 2 * kBM * D + 2 * prow);
+        if (v.y != 0.f) m = fmaxf(m, v.x);
     }
+    float4 acc[PER];
+    float l = 0.f;
+#pragma unroll
+    for (int c = 0; c < PER; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int x = 0; x < P.n_split; ++x) {
+        const float *p = parts + static_cast<size_t>(x) * C::kPartFloats;
+        const float2 v = *reinterpret_cast<const float2 *>(p + 2 * kBM * D + 2 * prow);
+        const float f = v.y == 0.f ? 0.f : fast_exp2(v.x - m);
+        l = fmaf(v.y, f, l);
+#pragma unroll
+        for (int c = 0; c < PER; ++c) {
+            const float4 o = *reinterpret_cast<const float4 *>(p + ((warp * PER + c) * 2 * kBM + prow) * 4);
+            if (f == 0.f) continue;  // (its o may not have been written)
+            acc[c].x = fmaf(o.x, f, acc[c].x);
+            acc[c].y = fmaf(o.y, f, acc[c].y);
+            acc[c].z = fmaf(o.z, f, acc[c].z);
+            acc[c].w = fmaf(o.w, f, acc[c].w);
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T16 *dst = static_cast<T16 *>(P.c.out) +
+               ((job.r0 + static_cast<long long>(pos)) * P.c.H + job.hk * P.c.group + static_cast<int>(hd)) * D + warp * PER * 4;
+#pragma unroll
+    for (int c = 0; c < PER; ++c)
+        *reinterpret_cast<uint2 *>(dst + 4 * c) =
+            make_uint2(E::pack(acc[c].x * inv, acc[c].y * inv), E::pack(acc[c].z * inv, acc[c].w * inv));
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -679,7 +680,7 @@ cudaError_t launch(const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorM
     e = hawk_host::launch_dependent(paged_tile_kernel<T16, D>, dim3(base * P.n_split), dim3(kThreads), TileCfg<D>::kSmem, st, mq,
                                     mk, mv, P);
     if (e != cudaSuccess || P.n_split == 1) return e;
-    return hawk_host::launch_dependent(paged_tile_merge_kernel<T16, D>, dim3(base, 16), dim3(256), 0, st, P);
+    return hawk_host::launch_dependent(paged_tile_merge_kernel<T16, D>, dim3(base, 2 * kBM / 32), dim3(256), 0, st, P);
 }
 
 }  // namespace
@@ -687,18 +688,25 @@ cudaError_t launch(const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorM
 size_t hawk_host::paged_tile_workspace_bytes(int S, int T, int max_new, int H, int H_kv, int few, int D, int max_kv)
 {
     const TilePlan p = plan_tiles(S, T, max_new, H, H_kv, few, max_kv);
-    return p.n_split == 1 ? 0 : static_cast<size_t>(p.n_split) * T * H * (D + 2) * sizeof(float);
+    const size_t list = static_cast<size_t>(p.pairs) * sizeof(PagedGroup);
+    if (p.n_split == 1) return list;
+    return list + static_cast<size_t>(p.pairs) * H_kv * p.n_split * sizeof(float) *
+                      (D == 64 ? TileCfg<64>::kPartFloats : TileCfg<128>::kPartFloats);
 }
 
-cudaError_t hawk_host::launch_paged_tile(const hawk_paged_attn_args &a, const PagedParams &base, float *part, cudaStream_t st,
-                                         bool *refused)
+int hawk_host::paged_tile_groups(int S, int T, int max_new, int H, int H_kv, int few)
+{
+    const long long pairs = plan_tiles(S, T, max_new, H, H_kv, few, 0).pairs;
+    return pairs * H_kv * kMaxSplits < (1ll << 31) ? static_cast<int>(pairs) : 0;
+}
+
+cudaError_t hawk_host::launch_paged_tile(const hawk_paged_attn_args &a, const PagedParams &base, float *part, cudaStream_t st)
 {
     const TilePlan p = plan_tiles(a.S, a.T, base.max_new, a.H, a.H_kv, base.rows_few, a.max_kv);
-    *refused = p.pairs * a.H_kv * p.n_split >= (1ll << 31);
-    if (*refused) return cudaSuccess;
     TileParams P;
     P.c = base;
-    P.c.part = part;
+    P.groups = base.groups;
+    P.c.part = part + static_cast<size_t>(p.pairs) * sizeof(PagedGroup) / sizeof(float);
     P.tok = p.tok;
     P.q_rows = p.tok * base.group;
     P.n_split = p.n_split;
