@@ -547,7 +547,8 @@ hawk_status hawk_rope_append(const hawk_rope_append_args *args, int32_t *dev_sta
  *   max_kv     upper bound of kv_len of the streams that are not idle, <= table_width * page_size (sizes the launch
  *              and the workspace); a kv_len outside [0, max_kv] is clamped, HAWK_DEV_BAD_PREFIX
  *   workspace  at least hawk_paged_attn_workspace_bytes(...) bytes, 16-byte aligned, may be NULL when that is 0;
- *              no initialisation.  Calls that may overlap on the GPU need one each.
+ *              no initialisation; the size is for exactly these arguments (a smaller call may need more).  Calls
+ *              that may overlap on the GPU need one each.
  * A page id outside [0, n_pages) reads as zeros and is flagged HAWK_DEV_BAD_PAGE.
  * Supported: D in {64, 128}; page_size a multiple of 8; S <= 4096; H a multiple of H_kv, H/H_kv <= 128.
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, PARAM, CUDA.  S == 0, T == 0 or max_new == 0 returns HAWK_OK

@@ -34,6 +34,7 @@ struct PagedParams {
     int row_blocks;            // rows kernel: blocks that do rows; one more makes the list below, where there is one
     PagedGroup *groups;        // [group_cap], longest first; NULL: no stream goes to the tile kernel
     int group_cap, tile_tok;   // tile_tok: positions a query tile holds
+    int mid_tok;               // mid kernel: positions an item's queries are loaded for
     FastDiv div_page, div_group;
     float scale_log2;          // sm_scale * log2(e)
     int32_t *dev_status;
@@ -215,6 +216,12 @@ constexpr int kPagedSms = 148;  // launch shapes are planned for the B200's 148 
 bool encode_pages(CUtensorMap *map, const hawk_paged_attn_args &a, bool values, int box_rows, int *rows_inner);
 
 int paged_gcd(int a, int b);
+
+constexpr int kPagedMaxStreams = 4096;  // the prefix sums are held in shared memory
+
+// The mid kernel (up to 64 rows per kv head on tcgen05): rows per item it is built for that hold `rows` (16, 32, 64), and its
+// launch (without the merge).
+cudaError_t launch_paged_mid(const hawk_paged_attn_args &a, const hawk::PagedParams &base, int nr, cudaStream_t st);
 
 // The tile kernel (tcgen05 tiles of query rows): bytes of its list and of its partial results, and its launch.
 size_t paged_tile_workspace_bytes(int S, int T, int max_new, int H, int H_kv, int few, int D, int max_kv);

@@ -1,6 +1,7 @@
 // hawk_paged_attn: attention of a ragged batch of new rows over a paged key/value cache.  This file holds the entry point
-// and the kernel for FEW rows per kv head (decode steps, drafted blocks, candidate trees); many rows go to the
-// tile kernel in hawk_paged_tile.cu.  A stream is handled by one of the two, by its own row count.
+// and the kernel for FEW rows per kv head (decode steps, drafted blocks, small candidate trees).  Streams of more than 64
+// rows per kv head go to the tile kernel in hawk_paged_tile.cu, each by its own row count; the others of a call go to the
+// kernel here or, all of them, to the one in hawk_paged_mid.cu, by the call's sizes (plan_rows).
 //
 // With few rows the call is bound by reading every key and value once (r flops per byte for r rows per kv head), so the
 // kernel is organised like the dense verify attention: a flat list of key tiles cut into equal shares, one per warp of a
@@ -27,13 +28,13 @@ using namespace hawk;
 //   group : one item per block, split evenly over its warps, which merge in shared memory.  8 warps of 3 stages and one
 //           block per SM, or (one column tile) 4 of 2 and three blocks per SM.
 // group needs no second kernel and no partial results in memory, so it is taken whenever the items fit the GPU at once
-// and are not so few and long that most SMs would idle (plan_rows has the rule and what both sides measured).
+// and are not so few and long that most SMs would idle (plan_rows has the rules and what both sides measured).
 __host__ __device__ constexpr int shares_warps(int nqt) { return nqt == 1 ? 12 : 8; }
 __host__ __device__ constexpr int shares_stages(int nqt) { return nqt == 1 ? 2 : 3; }
 constexpr int kMinShareTiles = 2;    // shorter shares would only add partial results to merge
 constexpr float kLazy = 8.f;         // log2 units by which a score may exceed the softmax shift
 constexpr int kStageBytes = 8192;
-constexpr int kMaxStreams = 4096;    // the prefix sum is held in shared memory
+constexpr int kMaxStreams = hawk_host::kPagedMaxStreams;
 constexpr int kRecordInts = 8;       // start tile, tiles of the item, first row, rows, kv head, row chunk, total tiles, workers
 
 template <int D>
@@ -610,7 +611,7 @@ constexpr int kMergeWorkers = 8;
 __host__ __device__ constexpr int merge_rows(int D) { return D == 64 ? 8 : 4; }
 
 template <typename T16, int D, int RPI>
-__global__ void __launch_bounds__(256, 3) paged_merge_kernel(const PagedParams P)
+__global__ void __launch_bounds__(256, 3) paged_merge_kernel(const PagedParams P, int workers_max)
 {
     using E = Elem<T16>;
     constexpr int PER = D / 32, RW = merge_rows(D);
@@ -622,7 +623,7 @@ __global__ void __launch_bounds__(256, 3) paged_merge_kernel(const PagedParams P
     // lane i < 8 looks at worker g0 + i
     const int mine = g0 + (lane & 7);
     int4 a = make_int4(0, 1, 0, 0), b = make_int4(0, 0, 0, 1);
-    if (mine < hawk_host::kPagedSms * shares_warps(RPI / 8)) {
+    if (mine < workers_max) {
         a = *reinterpret_cast<const int4 *>(P.records + static_cast<size_t>(mine) * kRecordInts);
         b = *reinterpret_cast<const int4 *>(P.records + static_cast<size_t>(mine) * kRecordInts + 4);
     }
@@ -751,14 +752,38 @@ __global__ void __launch_bounds__(256, 3) paged_merge_kernel(const PagedParams P
 }
 
 // ---------------------------------------------------------------------------------------------- host side
-enum Shape { kShapeShares, kShapeGroup4, kShapeGroup8 };
+enum Shape { kShapeShares, kShapeGroup4, kShapeGroup8, kShapeMid };
 
 struct RowsPlan {
     Shape shape;
     int rpi, grid;
 };
 
+// The kernel with the keys on tcgen05 in place of this file's?  It costs the same up to 64 rows (1.5 us a 128-key tile of a block
+// at D = 128), this one more with each column tile of 8 rows, and its shares, a block each instead of a warp each, leave a tenth
+// of the partial results.  But each of its items costs a few us once, and at D = 64, where a tile is half the bytes, it
+// does not keep up with reading.  Measured, us, that kernel / this one, for (streams x kv heads) items of so many keys:
+//   D = 128, 256 of 2400   8 rows 57 / 50    12: 58 / 63    24: 58 / 64    32: 59 / 114   60: 64 / 158
+//            256 of 600    12 rows 23 / 26   24: 25 / 32    60: 35 / 53
+//            1280 of 400   12 rows 56 / 54   24: 66 / 61    32: 67 / 104   40: 98 / 104   60: 107 / 146
+//            56 of 20000    1 row  95 / 97    8: 95 / 101   32: 96 / 195
+//            8 of 12000     1 row  19 / 28    8: 20 / 32    1 of 20000: 1 row 16 / 45
+//            in place of group, 32 of 1500: 32 rows 17 / 20;  64 of 1200: 12 rows 17 / 17, 32: 19 / 18;  128 of 1500: 12 rows 26 / 21
+//   D = 64,  256 of 2400   12 rows 40 / 37   32: 45 / 47    60: 58 / 72
+//            320 of 500    12 rows 21 / 20   32: 24 / 28    40: 31 / 27   60: 33 / 34;   1280 of 400: 24 rows 64 / 37
+//            8 of 12000     1 row  16 / 25    8: 18 / 34    40: 24 / 30
 // From host-known bounds only, so that the workspace query and the launch agree.
+bool mid_pays(bool shares, long long items, int rows, int D, int max_kv)
+{
+    const bool light = items * ((max_kv + kPagedTileKeys - 1) / kPagedTileKeys) <= 12 * hawk_host::kPagedSms;
+    const bool few = items <= hawk_host::kPagedSms / 2;
+    if (D == 128) {
+        if (!shares) return few && rows > 8 && max_kv >= 1536;
+        return few || (rows > 8 && (rows > 24 || light || max_kv >= 512));
+    }
+    return shares && ((rows > 32 && max_kv >= 1024) || (light && (few || (rows > 24 && rows <= 32))));
+}
+
 RowsPlan plan_rows(int S, int rows, int H_kv, int D, int max_kv)
 {
     RowsPlan p;
@@ -780,11 +805,18 @@ RowsPlan plan_rows(int S, int rows, int H_kv, int D, int max_kv)
         p.shape = kShapeGroup4;
         p.grid = static_cast<int>(items);
     }
+    if (mid_pays(p.shape == kShapeShares, static_cast<long long>(S) * H_kv, rows, D, max_kv)) {
+        p.shape = kShapeMid;
+        p.grid = hawk_host::kPagedSms;
+        p.rpi = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    }
     return p;
 }
 
 size_t rows_workspace_bytes(const RowsPlan &p, int D)
 {
+    if (p.shape == kShapeMid)
+        return static_cast<size_t>(hawk_host::kPagedSms) * (kRecordInts * sizeof(int32_t) + 2ull * 64 * (D + 2) * sizeof(float));
     if (p.shape != kShapeShares) return 0;
     return static_cast<size_t>(hawk_host::kPagedSms) * shares_warps(p.rpi / 8) * (kRecordInts * sizeof(int32_t) + 2ull * p.rpi * (D + 2) * sizeof(float));
 }
@@ -811,6 +843,14 @@ cudaError_t launch_shape(const CUtensorMap &mk, const CUtensorMap &mv, const Pag
                                        st, mk, mv, P);
 }
 
+template <typename T16, int D, int RPI>
+cudaError_t launch_merge(const PagedParams &P, int workers, cudaStream_t st)
+{
+    return hawk_host::launch_dependent(paged_merge_kernel<T16, D, RPI>,
+                                       dim3((workers - 1 + kMergeWorkers - 1) / kMergeWorkers, RPI / merge_rows(D)), dim3(256), 0, st,
+                                       P, workers);
+}
+
 template <typename T16, int D, int NQT>
 cudaError_t launch_rows(const CUtensorMap &mk, const CUtensorMap &mv, const PagedParams &P, const RowsPlan &p, cudaStream_t st)
 {
@@ -820,9 +860,7 @@ cudaError_t launch_rows(const CUtensorMap &mk, const CUtensorMap &mv, const Page
     constexpr int kW = shares_warps(NQT);
     cudaError_t e = launch_shape<T16, D, NQT, kW, shares_stages(NQT), false>(mk, mv, P, p.grid, st);
     if (e != cudaSuccess) return e;
-    const unsigned boundaries = hawk_host::kPagedSms * kW - 1;
-    return hawk_host::launch_dependent(paged_merge_kernel<T16, D, NQT * 8>,
-                                       dim3((boundaries + kMergeWorkers - 1) / kMergeWorkers, NQT * 8 / merge_rows(D)), dim3(256), 0, st, P);
+    return launch_merge<T16, D, NQT * 8>(P, hawk_host::kPagedSms * kW, st);
 }
 
 template <typename T16, int D>
@@ -839,11 +877,7 @@ cudaError_t launch_rows_n(const CUtensorMap &mk, const CUtensorMap &mv, const Pa
 }
 
 // Rows per kv head up to which a stream goes to the rows kernel.
-#ifndef FEW64
-#define FEW64 64
-#define FEW128 48
-#endif
-int few_rows(int D) { return D == 64 ? FEW64 : FEW128; }
+constexpr int kFewRows = 64;
 
 size_t align16(size_t n) { return (n + 15) / 16 * 16; }
 
@@ -880,9 +914,9 @@ extern "C" size_t hawk_paged_attn_workspace_bytes(int S, int T, int max_new, int
         return 0;
     if (max_new > T) max_new = T;
     const long long rows = static_cast<long long>(max_new) * (H / H_kv);
-    const long long few = rows < few_rows(D) ? rows : few_rows(D);
+    const long long few = rows < kFewRows ? rows : kFewRows;
     const size_t a = rows_workspace_bytes(plan_rows(S, static_cast<int>(few), H_kv, D, max_kv), D);
-    const size_t b = rows > few_rows(D) ? hawk_host::paged_tile_workspace_bytes(S, T, max_new, H, H_kv, few_rows(D), D, max_kv) : 0;
+    const size_t b = rows > kFewRows ? hawk_host::paged_tile_workspace_bytes(S, T, max_new, H, H_kv, kFewRows, D, max_kv) : 0;
     return align16(a) + b;
 }
 
@@ -913,9 +947,8 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     }
     const int group = a.H / a.H_kv, max_new = a.max_new < a.T ? a.max_new : a.T;
     const long long rows_all = static_cast<long long>(max_new) * group;
-    const int limit = few_rows(a.D);
-    const bool tiles = rows_all > limit;
-    const int rows = static_cast<int>(tiles ? limit : rows_all);
+    const bool tiles = rows_all > kFewRows;
+    const int rows = static_cast<int>(tiles ? kFewRows : rows_all);
     const RowsPlan plan = plan_rows(a.S, rows, a.H_kv, a.D, a.max_kv);
     // list positions are 32-bit numbers
     const int tk = kStageBytes / (4 * a.D);
@@ -940,7 +973,8 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     P.block_table = a.block_table;
     P.anc_mask = a.anc_mask;
     P.records = static_cast<int32_t *>(a.workspace);
-    P.part = reinterpret_cast<float *>(P.records + static_cast<size_t>(hawk_host::kPagedSms) * shares_warps(plan.rpi / 8) * kRecordInts);
+    P.part = reinterpret_cast<float *>(P.records + static_cast<size_t>(hawk_host::kPagedSms) *
+                                                       (plan.shape == kShapeMid ? 1 : shares_warps(plan.rpi / 8)) * kRecordInts);
     P.q_row_stride = a.q_row_stride;
     P.q_head_stride = a.q_head_stride;
     P.S = a.S;
@@ -966,7 +1000,17 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     }
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
 
-    {
+    if (plan.shape == kShapeMid) {
+        if (hawk_host::launch_paged_mid(a, P, plan.rpi, st) != cudaSuccess) return HAWK_ERR_CUDA;
+        cudaError_t e;
+        if (a.dtype == HAWK_BF16)
+            e = a.D == 64 ? launch_merge<__nv_bfloat16, 64, 64>(P, hawk_host::kPagedSms, st)
+                          : launch_merge<__nv_bfloat16, 128, 64>(P, hawk_host::kPagedSms, st);
+        else
+            e = a.D == 64 ? launch_merge<__half, 64, 64>(P, hawk_host::kPagedSms, st)
+                          : launch_merge<__half, 128, 64>(P, hawk_host::kPagedSms, st);
+        if (e != cudaSuccess) return HAWK_ERR_CUDA;
+    } else {
         CUtensorMap mk, mv;
         P.box_rows = hawk_host::paged_gcd(a.page_size, tk);
         if (!hawk_host::encode_pages(&mk, a, false, P.box_rows, &P.k_rows_inner) ||

@@ -264,14 +264,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     id[1] = id[2];
                     id[2] = id[3];
                 }
-                if (!ok || *abort_flag) {
-                    // let what is in flight land (bounded) before the block retires
-                    *abort_flag = 1;
-                    warp_wait(q_full, 0, nullptr);
-                    for (int i = max(0, issued - C::kStages); i < issued; ++i)
-                        warp_wait(&full[i % C::kStages], (i / C::kStages) & 1u, nullptr);
-                    flags |= HAWK_DEV_TIMEOUT;
-                }
+                // what is in flight lands before the block retires, whoever gives up later (bounded waits)
+                if (!ok) *abort_flag = 1;
+                ok = warp_wait(q_full, 0, nullptr) && ok;
+                for (int i = max(0, issued - C::kStages); i < issued; ++i)
+                    ok = warp_wait(&full[i % C::kStages], (i / C::kStages) & 1u, nullptr) && ok;
+                if (!ok) flags |= HAWK_DEV_TIMEOUT;
             }
             if (flags && P.c.dev_status) atomicOr(P.c.dev_status, flags);
         } else if (warp == 8 && job.tiles > 0) {
