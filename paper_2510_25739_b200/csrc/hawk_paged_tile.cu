@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             bool ok = true;
             int issued = 0;  // ring stages armed
             if (job.tiles > 0) {
-                const uint64_t keep = l2_policy_evict_last();
+                const uint64_t policy = l2_policy_evict_first();
                 const int q_tiles = job.single ? 1 : 2;
                 if (lane == 0) {
                     mbar_arrive_expect_tx(q_full, q_tiles * C::kHalves * P.q_rows * 128);
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         P.c.div_page.divmod(static_cast<uint32_t>(key_of(i)), row);
                         paged_load(ring + st * C::kTileBytes + hf * C::kHalfBytes + box_key * 128, values ? &map_v : &map_k,
                                    values ? P.c.v_rows_inner : P.c.k_rows_inner, hf, static_cast<int>(row), job.hk, pg, &full[st],
-                                   keep);
+                                   policy);
                     }
                     __syncwarp();
                 };
