@@ -86,7 +86,7 @@ constexpr int kPlanWaves = 6;  // jobs of so many waves of blocks even out by th
 // cost classes), so that no long job starts last; where the jobs are many waves of blocks, one stream after the other instead, each
 // from its longest pair on, so that what runs together shares keys and values in L2 (799 against 822 us for 4 x 2048 rows
 // over 8192 keys; for 7B chunks of 300 to 511 rows, under two waves, the sort takes 94 us to 84).
-// A warp looks at 32 streams at once and deals a stream's pairs out to its lanes.
+// A warp looks at 32 streams at once and deals their pairs out to its lanes.
 __device__ __forceinline__ void paged_plan(const PagedParams &P, int *sh, int &flags)
 {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
@@ -114,14 +114,17 @@ __device__ __forceinline__ void paged_plan(const PagedParams &P, int *sh, int &f
                 if (lane >= o) inc += u;
             }
             before += inc - mine;
-            unsigned many = __ballot_sync(0xffffffffu, mine > 0);
-            while (many) {
-                const int b = __ffs(many) - 1;
-                many &= many - 1;
+            const int all = __shfl_sync(0xffffffffu, inc, 31);
+            for (int i0 = 0; i0 < all; i0 += 32) {
+                const int i = i0 + lane;  // pair of these 32 streams
+                int b = 0;                // its stream: the first whose running sum is past i
+#pragma unroll
+                for (int step = 16; step; step >>= 1)
+                    if (__shfl_sync(0xffffffffu, inc, b + step - 1) <= i) b += step;
                 const int r0 = __shfl_sync(0xffffffffu, st.r0, b), n = __shfl_sync(0xffffffffu, st.n, b);
                 const int kv = __shfl_sync(0xffffffffu, st.kv, b), pairs = __shfl_sync(0xffffffffu, mine, b);
-                const int at = __shfl_sync(0xffffffffu, before, b);
-                for (int p = lane; p < pairs; p += 32) {
+                const int p = i - (__shfl_sync(0xffffffffu, inc, b) - pairs), at = __shfl_sync(0xffffffffu, before, b);
+                if (i < all) {
                     // cost: key tiles that the pair's last position sees, twice where both its query tiles have rows
                     const int keys = max(0, min(kv, kv - n + paged_reach(P, n, (p + 1) * per_pair)));
                     const int tiles = (keys + kPagedTileKeys - 1) / kPagedTileKeys;
