@@ -91,7 +91,7 @@ __device__ __forceinline__ void paged_plan(const PagedParams &P, int *sh, int &f
 {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
     const int per_pair = 2 * P.tile_tok;
-    const float scale = (kPlanBuckets - 1) / (2.f * (P.kv_cap / kPagedTileKeys + 1));
+    const float scale = (kPlanBuckets - 1) / (8.f * (P.kv_cap / kPagedTileKeys + 1));
     auto pairs_at = [&](int s, PagedStream &st) {  // pairs of stream s, 0 for one of the rows kernel's or none
         st = {0, 0, 0};
         if (s < P.S) st = paged_stream(P, s, flags);
@@ -125,10 +125,11 @@ __device__ __forceinline__ void paged_plan(const PagedParams &P, int *sh, int &f
                 const int kv = __shfl_sync(0xffffffffu, st.kv, b), pairs = __shfl_sync(0xffffffffu, mine, b);
                 const int p = i - (__shfl_sync(0xffffffffu, inc, b) - pairs), at = __shfl_sync(0xffffffffu, before, b);
                 if (i < all) {
-                    // cost: key tiles that the pair's last position sees, twice where both its query tiles have rows
+                    // cost: key tiles that the pair's last position sees; one takes some 3400 cycles where both query tiles
+                    // have rows, 2150 where only one does
                     const int keys = max(0, min(kv, kv - n + paged_reach(P, n, (p + 1) * per_pair)));
                     const int tiles = (keys + kPagedTileKeys - 1) / kPagedTileKeys;
-                    const int cost = p * per_pair + P.tile_tok >= n ? tiles : 2 * tiles;
+                    const int cost = p * per_pair + P.tile_tok >= n ? 5 * tiles : 8 * tiles;
                     const int bucket = kPlanBuckets - 1 - min(kPlanBuckets - 1, static_cast<int>(cost * scale));
                     visit(bucket, s0 + b, r0, n, kv, p, at + pairs - 1 - p);
                 }

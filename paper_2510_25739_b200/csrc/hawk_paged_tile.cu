@@ -9,7 +9,7 @@
 //   0-3, 4-7  softmax of slot 0 and of slot 1: one query row a thread (row maxima and sums need no shuffles)
 //   8         issues every tcgen05.mma:  S_t = Q_t K^T (both operands in shared memory), O_t += P_t V (P_t in tensor
 //             memory, V in shared memory read along its rows)
-//   9         loads: Q once, then K and V tiles of 128 keys into a ring, as boxes that stay inside a page, a box a lane
+//   9, 10     loads: Q once and K tiles of 128 keys, V tiles, each its part of the ring, as boxes that stay inside a page, a box a lane
 // Tensor memory: S_0, S_1 (128 columns each; P_t overwrites the first half of S_t in 16 bits), O_0, O_1 (D columns each).
 // Order of the products: S_0(0) S_1(0) | P_0(i)V S_0(i+1) P_1(i)V S_1(i+1) | ..., so one slot's softmax runs under the
 // other slot's two products, and when S_t(i) is complete so is O_t up to tile i-1: the softmax warps rescale O_t in
@@ -25,6 +25,10 @@
 // scores never wait for P V, came to 916 us: products of 64 columns read Q from shared memory twice as often.
 // Jobs come from a list that one extra block of the rows kernel (which every call launches before this one) makes: a block reads
 // one record instead of searching the batch, and the longest jobs start first.
+// One warp issued a tile's boxes of 16 keys (32 at D = 128) one lane after the other, some 90 cycles each, which paced a single query
+// tile; two warps took 4 x 128 rows over 2816 keys from 53 to 43 us (pairs of query tiles, which need half as many: 138 to 139).
+// Measured and taken back: results leaving as whole rows through shared memory (140 to 146 us for 16 x 511 rows over 600 keys: row by
+// row the stores need nobody to wait for them); tensor memory taken before the job is known (148).
 // Few blocks: the key range is split too, each split leaves (o, max, sum) in fp32 and a second kernel joins them.
 // Measured and taken back: one persistent block per SM over equal shares of all key tiles.  Changing segments inside a block
 // costs what changing blocks does (some 10 k cycles of draining, epilogue, queries and first scores), cuts add partial results,
@@ -38,7 +42,7 @@ namespace {
 using namespace hawk;
 
 constexpr int kBM = 128, kBN = 128;
-constexpr int kThreads = 384;        // three warpgroups; the third has one warp for the products and one for the loads
+constexpr int kThreads = 384;        // three warpgroups; the third has one warp for the products and two for the loads
 constexpr int kRegsSoftmax = 224, kRegsOther = 56;  // of the 168 a thread that the block starts with (2 x 224 + 56 = 3 x 168)
 constexpr int kMaxSplits = 16;
 constexpr int kMinSplitKeys = 512;  // shorter key ranges cost more in partial results than they gain in blocks
@@ -203,27 +207,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     constexpr uint32_t tmem = 0;  // all 512 columns are the block's: its tensor memory starts at lane 0, column 0
     const int pfx = job.kv - job.n;
-    // K tiles run this many ahead of V tiles in the ring: slot 1 of a single query tile starts on key tile 1
-    const int ahead = job.single ? 2 : 1;
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-        if (warp == 9) {
-            // -------------------------------------------------------------- loads
+        // stages for keys, the others are for values: a single query tile starts on two key tiles, a pair holds value tiles longer
+        const int key_stages = job.single ? (C::kStages + 1) / 2 : C::kStages / 2;
+        if (warp == 9 || warp == 10) {
+            // -------------------------------------------------------------- loads: queries and keys, or values
+            const bool values = warp == 10;
             bool ok = true;
-            int issued = 0;  // ring stages armed
+            int issued = 0;  // tiles of this warp
             if (job.tiles > 0) {
                 const uint64_t policy = l2_policy_evict_first();
-                const int q_tiles = job.single ? 1 : 2;
-                if (lane == 0) {
-                    mbar_arrive_expect_tx(q_full, q_tiles * C::kHalves * P.q_rows * 128);
-                    for (int t = 0; t < q_tiles; ++t)
-                        for (int hf = 0; hf < C::kHalves; ++hf)
-                            tma_load_4d(q_smem + t * C::kTileBytes + hf * C::kHalfBytes, &map_q, hf * 64, job.hk * P.c.group,
-                                        job.r0 + job.tok0 + t * P.tok, 0, q_full);
-                }
                 // lane l loads 64-column half l % halves of box l / halves of every tile (at most 32 of them: boxes have
-                // 8 rows or more); its page id is fetched one tile ahead
+                // 8 rows or more); its page id is fetched three tiles ahead
+                const CUtensorMap *map = values ? &map_v : &map_k;
+                const int rows_inner = values ? P.c.v_rows_inner : P.c.k_rows_inner;
                 const int hf = lane % C::kHalves;
                 const int box_key = lane / C::kHalves * P.c.box_rows;
                 const int32_t *tb = P.c.block_table + static_cast<size_t>(job.s) * P.c.table_width;
@@ -232,43 +231,52 @@ __global__ void __launch_bounds__(kThreads, 1)
                 auto page_id = [&](int i) {
                     return has_box(i) ? tb[P.c.div_page.div(static_cast<uint32_t>(key_of(i)))] : 0;
                 };
-                int id[4] = {page_id(0), page_id(1), page_id(2), 0};  // of tiles j, j + 1, j + 2 (and the one on its way)
-                auto load = [&](int i, bool values, int pg) {
-                    const int st = issued % C::kStages, round = issued / C::kStages;
-                    if (round > 0) ok = ok && warp_wait(&empty[st], (round - 1) & 1u, abort_flag);
-                    if (!ok) return;
+                const int base = values ? key_stages : 0, depth = values ? C::kStages - key_stages : key_stages;
+                int at = 0;         // stage of tile i, and the parity of its use
+                uint32_t use = 0;
+                int id[4] = {page_id(0), page_id(1), page_id(2), 0};  // (on their way while Q is asked for)
+                if (!values && lane == 0) {
+                    const int q_tiles = job.single ? 1 : 2;
+                    mbar_arrive_expect_tx(q_full, q_tiles * C::kHalves * P.q_rows * 128);
+                    for (int t = 0; t < q_tiles; ++t)
+                        for (int hf = 0; hf < C::kHalves; ++hf)
+                            tma_load_4d(q_smem + t * C::kTileBytes + hf * C::kHalfBytes, &map_q, hf * 64, job.hk * P.c.group,
+                                        job.r0 + job.tok0 + t * P.tok, 0, q_full);
+                }
+                for (int i = 0; i < job.tiles; ++i) {
+                    id[3] = page_id(i + 3);
+                    const int st = base + at;
+                    if (i >= depth) ok = warp_wait(&empty[st], use ^ 1u, abort_flag);
+                    if (!ok) break;
                     const int rows = min(kBN, (job.kv - (job.begin + i) * kBN + P.c.box_rows - 1) & -P.c.box_rows);
                     if (lane == 0) {
-                        const bool stall = kTestStallBytes != 0 && blockIdx.x == 0 && issued == 0;
+                        // (test builds only: the first tile of the first block is armed for more bytes than arrive)
+                        const bool stall = kTestStallBytes != 0 && blockIdx.x == 0 && i == 0 && !values;
                         mbar_arrive_expect_tx(&full[st], rows * 128 * C::kHalves + (stall ? kTestStallBytes : 0u));
                     }
                     __syncwarp();
                     ++issued;
                     if (has_box(i)) {
-                        if (pg < 0 || pg >= P.c.n_pages) flags |= HAWK_DEV_BAD_PAGE;  // (outside the tensor map: zeros)
+                        if (id[0] < 0 || id[0] >= P.c.n_pages) flags |= HAWK_DEV_BAD_PAGE;  // (outside the tensor map: zeros)
                         uint32_t row;
                         P.c.div_page.divmod(static_cast<uint32_t>(key_of(i)), row);
-                        paged_load(ring + st * C::kTileBytes + hf * C::kHalfBytes + box_key * 128, values ? &map_v : &map_k,
-                                   values ? P.c.v_rows_inner : P.c.k_rows_inner, hf, static_cast<int>(row), job.hk, pg, &full[st],
-                                   policy);
+                        paged_load(ring + st * C::kTileBytes + hf * C::kHalfBytes + box_key * 128, map, rows_inner, hf,
+                                   static_cast<int>(row), job.hk, id[0], &full[st], policy);
                     }
                     __syncwarp();
-                };
-                load(0, false, id[0]);
-                if (ahead == 2 && job.tiles > 1 && ok) load(1, false, id[1]);
-                for (int j = 0; j < job.tiles && ok; ++j) {
-                    id[3] = page_id(j + 3);
-                    load(j, true, id[0]);
-                    if (ok && j + ahead < job.tiles) load(j + ahead, false, ahead == 2 ? id[2] : id[1]);
                     id[0] = id[1];
                     id[1] = id[2];
                     id[2] = id[3];
+                    if (++at == depth) {
+                        at = 0;
+                        use ^= 1u;
+                    }
                 }
                 // what is in flight lands before the block retires, whoever gives up later (bounded waits)
                 if (!ok) *abort_flag = 1;
-                ok = warp_wait(q_full, 0, nullptr) && ok;
-                for (int i = max(0, issued - C::kStages); i < issued; ++i)
-                    ok = warp_wait(&full[i % C::kStages], (i / C::kStages) & 1u, nullptr) && ok;
+                if (!values) ok = warp_wait(q_full, 0, nullptr) && ok;
+                for (int i = max(0, issued - depth); i < issued; ++i)
+                    ok = warp_wait(&full[base + i % depth], (i / depth) & 1u, nullptr) && ok;
                 if (!ok) flags |= HAWK_DEV_TIMEOUT;
             }
             if (flags && P.c.dev_status) atomicOr(P.c.dev_status, flags);
@@ -287,11 +295,20 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t q_lo = static_cast<uint32_t>(qd), k_lo = static_cast<uint32_t>(kd), v_lo = static_cast<uint32_t>(vd);
             const uint32_t qk_hi = static_cast<uint32_t>(qd >> 32), v_hi = static_cast<uint32_t>(vd >> 32);
             bool ok = warp_wait(q_full, 0, abort_flag);
-            int taken = 0;
-            auto acquire = [&]() {  // the next tile of the ring
-                const int st = taken % C::kStages;
-                ok = ok && warp_wait(&full[st], (taken / C::kStages) & 1u, abort_flag);
-                ++taken;
+            const int n_key = __shfl_sync(0xffffffffu, key_stages, 0);
+            int k_at = 0, v_at = n_key;
+            uint32_t k_use = 0, v_use = 0;
+            auto acquire = [&](bool values) {  // the next tile of keys or of values
+                const int st = values ? v_at : k_at;
+                ok = ok && warp_wait(&full[st], values ? v_use : k_use, abort_flag);
+                if (values && ++v_at == C::kStages) {
+                    v_at = n_key;
+                    v_use ^= 1u;
+                }
+                if (!values && ++k_at == n_key) {
+                    k_at = 0;
+                    k_use ^= 1u;
+                }
                 return st;
             };
             auto release = [&](int st) {
@@ -334,35 +351,35 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
             };
             if (single) {
-                int st = acquire();
+                int st = acquire(false);
                 scores(0, st);
                 release(st);
                 if (tiles > 1) {
-                    st = acquire();
+                    st = acquire(false);
                     scores(1, st);
                     release(st);
                 }
                 for (int j = 0; j < tiles && ok; ++j) {
-                    const int t = j & 1, v = acquire();
+                    const int t = j & 1, v = acquire(true);
                     clean(j, v);
                     values(t, j >> 1, v);
                     release(v);
                     if (j + 2 < tiles) {
-                        const int k = acquire();
+                        const int k = acquire(false);
                         scores(t, k);
                         release(k);
                     }
                 }
             } else {
-                int k = acquire();
+                int k = acquire(false);
                 if (nt0 > 0) scores(0, k);
                 if (nt1 > 0) scores(1, k);
                 release(k);
                 for (int i = 0; i < tiles && ok; ++i) {
-                    const int v = acquire();
+                    const int v = acquire(true);
                     clean(i, v);
                     if (i < nt0) values(0, i, v);
-                    if (i + 1 < tiles) k = acquire();
+                    if (i + 1 < tiles) k = acquire(false);
                     if (i + 1 < nt0) scores(0, k);
                     if (i < nt1) values(1, i, v);
                     release(v);
