@@ -541,7 +541,7 @@ hawk_status hawk_rope_append(const hawk_rope_append_args *args, int32_t *dev_sta
  * finite: a NaN or infinity among a stream's own rows may reach rows of that stream that do not see it.
  *
  *   q          16-bit [T][H][D] at row and head strides
- *   out        16-bit [T][H*D], dense
+ *   out        16-bit [T][H*D], dense; must not overlap any input
  *   anc_mask   uint64 [max_new], device, or NULL; row i of every stream uses entry i.  max_new <= 64 with it.
  *   max_new    upper bound of n_s known on the host; a stream with more rows is skipped, HAWK_DEV_BAD_ROWS
  *   max_kv     upper bound of kv_len of the streams that are not idle, <= table_width * page_size (sizes the launch

@@ -745,6 +745,7 @@ __global__ void __launch_bounds__(256, 3) paged_merge_kernel(const PagedParams P
         const uint32_t pos = P.div_group.divmod(static_cast<uint32_t>(row0 + r), hd);
         T16 *dst = static_cast<T16 *>(P.out) +
                    ((first_row + static_cast<long long>(pos)) * P.H + hk * P.group + static_cast<int>(hd)) * D + lane * PER;
+        if (!HAWK_IN_BOUNDS(P.dev_status, dst - static_cast<T16 *>(P.out) + PER - 1, static_cast<long long>(P.T) * P.H * D)) continue;
 #pragma unroll
         for (int c = 0; c < PER; c += 2)
             *reinterpret_cast<uint32_t *>(dst + c) = E::pack(acc[r][c] * inv, acc[r][c + 1] * inv);

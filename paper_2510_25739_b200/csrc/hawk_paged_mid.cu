@@ -441,6 +441,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tmem_ld_wait();
                 if (!valid) continue;
                 if (whole) {
+                    if (!HAWK_IN_BOUNDS(P.dev_status, dst - static_cast<T16 *>(P.out) + c0 + 31, static_cast<long long>(P.T) * P.H * D))
+                        continue;
 #pragma unroll
                     for (int x = 0; x < 32; x += 8) {
                         uint32_t y[4];

@@ -570,6 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int k = 0; k < 4; ++k) o[c + k] = __float_as_uint(v[k]);
                     }
                     if (!valid || !ok) continue;
+                    if (!HAWK_IN_BOUNDS(P.c.dev_status, cell * D + c0 + 31, static_cast<long long>(P.c.T) * P.c.H * D)) continue;
                     if (P.n_split == 1) {
 #pragma unroll
                         for (int c = 0; c < 32; c += 8) {
