@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (ok && job.single && job.tiles > 1) ok = warp_wait(&o_done[t ^ 1], 0, abort_flag);  // (Q is free then)
         if (!ok) *abort_flag = 1;
         tcgen05_fence_after();
-        if (m_run == -CUDART_INF_F) l_run = 0.f;  // a row that has seen no key
+        if (m_run == -CUDART_INF_F && l_run == l_run) l_run = 0.f;  // a row that has seen no key (NaN scores: NaN)
         // the tensor-memory loads below are for whole warps: rows that do not exist take part and store nothing
         float f_own = 1.f, f_other = 0.f;  // weights of the two slots' O where they are joined
         auto other_at = [&](int c) {       // 16-byte chunk c of row r of slot 1's O (the chunk index turned by the row: no conflicts)
