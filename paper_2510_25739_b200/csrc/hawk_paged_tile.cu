@@ -218,7 +218,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             bool ok = true;
             int issued = 0;  // tiles of this warp
             if (job.tiles > 0) {
-                const uint64_t policy = l2_policy_evict_first();
+                // Keys and values that few other blocks read pass through L2 marked evict-first, which makes room without a search: 7B
+                // chunks of 300 to 511 rows 70 us against 78 kept, 8 x 512 rows of 32 heads on 8 over 2048 keys 159 against
+                // 164.  From 32 pairs of query tiles on it pays to keep them (794 against 815 us for 4 x 2048 rows of 32
+                // heads on 8 over 8192 keys; 16 pairs: the same).
+                const uint64_t policy = job.n > 32 * P.tok ? l2_policy_evict_last() : l2_policy_evict_first();
                 // lane l loads 64-column half l % halves of box l / halves of every tile (at most 32 of them: boxes have
                 // 8 rows or more); its page id is fetched three tiles ahead
                 const CUtensorMap *map = values ? &map_v : &map_k;
