@@ -1,7 +1,7 @@
 // hawk_paged_attn: attention of a ragged batch of new rows over a paged key/value cache.  This file holds the entry point
 // and the kernel for FEW rows per kv head (decode steps, drafted blocks, small candidate trees).  Streams of more than 64
 // rows per kv head go to the tile kernel in hawk_paged_tile.cu, each by its own row count; the others of a call go to the
-// kernel here or, all of them, to the one in hawk_paged_mid.cu, by the call's sizes (plan_rows).
+// kernel here or, in calls without such streams, to the one in hawk_paged_mid.cu, by the call's sizes (plan_rows).
 //
 // With few rows the call is bound by reading every key and value once (r flops per byte for r rows per kv head), so the
 // kernel is organised like the dense verify attention: a flat list of key tiles cut into equal shares, one per warp of a
@@ -15,6 +15,7 @@
 //   - A share that holds part of an item leaves an fp32 partial and a record of what it is part of; the merge kernel
 //     works from the records alone and needs neither the lengths nor the prefix sum again.
 #include <atomic>
+#include <type_traits>
 
 #include "hawk_paged.cuh"
 
@@ -423,117 +424,124 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
         const uint32_t kbase = ring_u32 + st * kStageBytes;
         const uint32_t vbase = kbase + C::kHalves * C::kSubBytes;
 
-        // ---- S^T = K Q^T
-        float sc[NQT][KB][4];
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-            for (int nq = 0; nq < NQT; ++nq) sc[nq][kb][0] = sc[nq][kb][1] = sc[nq][kb][2] = sc[nq][kb][3] = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < DB; ++kk) {
-                uint32_t ka[4];
-                ldmatrix_x4(ka, kbase + kb * 2048 + k_off[kk]);
-#pragma unroll
-                for (int nq = 0; nq < NQT; ++nq) E::mma(sc[nq][kb], ka, qb[nq][kk][0], qb[nq][kk][1]);
-            }
-        }
-        // ---- masks, at the tiles that reach past the prefix (keys behind the stream's last one among them)
-        if (key0 + TK > pfx) {
-#pragma unroll
-            for (int nq = 0; nq < NQT; ++nq)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const uint32_t r = static_cast<uint32_t>(min(row0 + nq * 8 + 2 * tq + c, cc.n * P.group - 1));
-                    const int pos = static_cast<int>(P.div_group.div(r));
-                    const uint64_t m = P.anc_mask ? P.anc_mask[pos] : 0ull;
-                    auto visible = [&](int key) {
-                        const int rel = key - pfx;
-                        if (!P.anc_mask) return rel <= pos;
-                        return rel < 0 || (rel < cc.n && rel < 64 && ((m >> rel) & 1ull));
-                    };
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb) {
-                        const int key = key0 + kb * 16 + g;
-                        if (!visible(key)) sc[nq][kb][c] = -CUDART_INF_F;
-                        if (!visible(key + 8)) sc[nq][kb][2 + c] = -CUDART_INF_F;
-                    }
-                }
-        }
-        // ---- running softmax per row, base 2.  The shift m may be any number as long as o, the sum and p share it; it
-        // is renewed only when a score exceeds it by more than kLazy, so that almost every tile goes without the
-        // reduction across lanes and without touching o (p stays below 2^kLazy: far inside fp16, bf16 and fp32)
-        bool grows = false;
-        float mx[NQT][2];
-#pragma unroll
-        for (int nq = 0; nq < NQT; ++nq) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float m = -CUDART_INF_F;
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) m = fmaxf(m, fmaxf(sc[nq][kb][c], sc[nq][kb][2 + c]));
-                mx[nq][c] = m * P.scale_log2;
-                grows |= mx[nq][c] > mrun[nq][c] + kLazy;
-            }
-        }
-        if (__any_sync(0xffffffffu, grows)) {
-#pragma unroll
-            for (int nq = 0; nq < NQT; ++nq)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float m = mx[nq][c];
-#pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    m = fmaxf(m, mrun[nq][c]);
-                    const float a = fast_exp2(mrun[nq][c] - (m == -CUDART_INF_F ? 0.f : m));
-                    mrun[nq][c] = m;
-                    lrun[nq][c] *= a;
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        ot[nq][db][c] *= a;
-                        ot[nq][db][2 + c] *= a;
-                    }
-                }
-        }
-        uint32_t pb[NQT][KB][2];
-#pragma unroll
-        for (int nq = 0; nq < NQT; ++nq) {
-            const float mu0 = mrun[nq][0] == -CUDART_INF_F ? 0.f : mrun[nq][0];
-            const float mu1 = mrun[nq][1] == -CUDART_INF_F ? 0.f : mrun[nq][1];
+        // The tile's products and softmax for the first NQ column tiles: an item may have fewer rows than its place in the call holds
+        // (single tokens beside chunks of a prompt), and then pays for one.
+        auto columns = [&](auto active) {
+            constexpr int NQ = decltype(active)::value;
+            // ---- S^T = K Q^T
+            float sc[NQ][KB][4];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const float p0 = fast_exp2(fmaf(sc[nq][kb][0], P.scale_log2, -mu0));
-                const float p1 = fast_exp2(fmaf(sc[nq][kb][1], P.scale_log2, -mu1));
-                const float p2 = fast_exp2(fmaf(sc[nq][kb][2], P.scale_log2, -mu0));
-                const float p3 = fast_exp2(fmaf(sc[nq][kb][3], P.scale_log2, -mu1));
-                lrun[nq][0] += p0 + p2;
-                lrun[nq][1] += p1 + p3;
-                pb[nq][kb][0] = movmatrix_trans(E::pack(p0, p1));
-                pb[nq][kb][1] = movmatrix_trans(E::pack(p2, p3));
-            }
-        }
-        // ---- O^T += V^T P^T; values behind the last key hold anything (or are an earlier tile's): zeroed, 0 * NaN is NaN
-        const bool ragged = key0 + TK > kv;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            const int kleft = kv - (key0 + kb * 16);
-            if (ragged && kleft <= 0) break;
+                for (int nq = 0; nq < NQ; ++nq) sc[nq][kb][0] = sc[nq][kb][1] = sc[nq][kb][2] = sc[nq][kb][3] = 0.f;
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                uint32_t va[4];
-                ldmatrix_x4_trans(va, vbase + kb * 2048 + v_off[db]);
-                if (ragged && kleft < 16) {
-                    const int ka = 2 * tq, kb2 = 2 * tq + 8;
-                    const uint32_t ma = (ka < kleft ? 0x0000ffffu : 0u) | (ka + 1 < kleft ? 0xffff0000u : 0u);
-                    const uint32_t mb = (kb2 < kleft ? 0x0000ffffu : 0u) | (kb2 + 1 < kleft ? 0xffff0000u : 0u);
-                    va[0] &= ma;
-                    va[1] &= ma;
-                    va[2] &= mb;
-                    va[3] &= mb;
+                for (int kk = 0; kk < DB; ++kk) {
+                    uint32_t ka[4];
+                    ldmatrix_x4(ka, kbase + kb * 2048 + k_off[kk]);
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) E::mma(sc[nq][kb], ka, qb[nq][kk][0], qb[nq][kk][1]);
                 }
-#pragma unroll
-                for (int nq = 0; nq < NQT; ++nq) E::mma(ot[nq][db], va, pb[nq][kb][0], pb[nq][kb][1]);
             }
-        }
+            // ---- masks, at the tiles that reach past the prefix (keys behind the stream's last one among them)
+            if (key0 + TK > pfx) {
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t r = static_cast<uint32_t>(min(row0 + nq * 8 + 2 * tq + c, cc.n * P.group - 1));
+                        const int pos = static_cast<int>(P.div_group.div(r));
+                        const uint64_t m = P.anc_mask ? P.anc_mask[pos] : 0ull;
+                        auto visible = [&](int key) {
+                            const int rel = key - pfx;
+                            if (!P.anc_mask) return rel <= pos;
+                            return rel < 0 || (rel < cc.n && rel < 64 && ((m >> rel) & 1ull));
+                        };
+#pragma unroll
+                        for (int kb = 0; kb < KB; ++kb) {
+                            const int key = key0 + kb * 16 + g;
+                            if (!visible(key)) sc[nq][kb][c] = -CUDART_INF_F;
+                            if (!visible(key + 8)) sc[nq][kb][2 + c] = -CUDART_INF_F;
+                        }
+                    }
+            }
+            // ---- running softmax per row, base 2.  The shift m may be any number as long as o, the sum and p share it; it
+            // is renewed only when a score exceeds it by more than kLazy, so that almost every tile goes without the
+            // reduction across lanes and without touching o (p stays below 2^kLazy: far inside fp16, bf16 and fp32)
+            bool grows = false;
+            float mx[NQ][2];
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float m = -CUDART_INF_F;
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) m = fmaxf(m, fmaxf(sc[nq][kb][c], sc[nq][kb][2 + c]));
+                    mx[nq][c] = m * P.scale_log2;
+                    grows |= mx[nq][c] > mrun[nq][c] + kLazy;
+                }
+            }
+            if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float m = mx[nq][c];
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                        m = fmaxf(m, mrun[nq][c]);
+                        const float a = fast_exp2(mrun[nq][c] - (m == -CUDART_INF_F ? 0.f : m));
+                        mrun[nq][c] = m;
+                        lrun[nq][c] *= a;
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            ot[nq][db][c] *= a;
+                            ot[nq][db][2 + c] *= a;
+                        }
+                    }
+            }
+            uint32_t pb[NQ][KB][2];
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+                const float mu0 = mrun[nq][0] == -CUDART_INF_F ? 0.f : mrun[nq][0];
+                const float mu1 = mrun[nq][1] == -CUDART_INF_F ? 0.f : mrun[nq][1];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    const float p0 = fast_exp2(fmaf(sc[nq][kb][0], P.scale_log2, -mu0));
+                    const float p1 = fast_exp2(fmaf(sc[nq][kb][1], P.scale_log2, -mu1));
+                    const float p2 = fast_exp2(fmaf(sc[nq][kb][2], P.scale_log2, -mu0));
+                    const float p3 = fast_exp2(fmaf(sc[nq][kb][3], P.scale_log2, -mu1));
+                    lrun[nq][0] += p0 + p2;
+                    lrun[nq][1] += p1 + p3;
+                    pb[nq][kb][0] = movmatrix_trans(E::pack(p0, p1));
+                    pb[nq][kb][1] = movmatrix_trans(E::pack(p2, p3));
+                }
+            }
+            // ---- O^T += V^T P^T; values behind the last key hold anything (or are an earlier tile's): zeroed, 0 * NaN is NaN
+            const bool ragged = key0 + TK > kv;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const int kleft = kv - (key0 + kb * 16);
+                if (ragged && kleft <= 0) break;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    uint32_t va[4];
+                    ldmatrix_x4_trans(va, vbase + kb * 2048 + v_off[db]);
+                    if (ragged && kleft < 16) {
+                        const int ka = 2 * tq, kb2 = 2 * tq + 8;
+                        const uint32_t ma = (ka < kleft ? 0x0000ffffu : 0u) | (ka + 1 < kleft ? 0xffff0000u : 0u);
+                        const uint32_t mb = (kb2 < kleft ? 0x0000ffffu : 0u) | (kb2 + 1 < kleft ? 0xffff0000u : 0u);
+                        va[0] &= ma;
+                        va[1] &= ma;
+                        va[2] &= mb;
+                        va[3] &= mb;
+                    }
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) E::mma(ot[nq][db], va, pb[nq][kb][0], pb[nq][kb][1]);
+                }
+            }
+        };
+        if (NQT > 1 && nrows <= 8) columns(std::integral_constant<int, 1>{});
+        else columns(std::integral_constant<int, NQT>{});
         __syncwarp();
         --in_flight;
         if (ci.left > 0) {
@@ -785,7 +793,8 @@ bool mid_pays(bool shares, long long items, int rows, int D, int max_kv)
     return shares && ((rows > 32 && max_kv >= 1024) || (light && (few || (rows > 24 && rows <= 32))));
 }
 
-RowsPlan plan_rows(int S, int rows, int H_kv, int D, int max_kv)
+// `chunks_too`: some streams may be the tile kernel's, and the bound on the others' rows is then only that kernel's threshold.
+RowsPlan plan_rows(int S, int rows, int H_kv, int D, int max_kv, bool chunks_too)
 {
     RowsPlan p;
     const int cap = rows_max(D), tk = kStageBytes / (4 * D);
@@ -806,7 +815,10 @@ RowsPlan plan_rows(int S, int rows, int H_kv, int D, int max_kv)
         p.shape = kShapeGroup4;
         p.grid = static_cast<int>(items);
     }
-    if (mid_pays(p.shape == kShapeShares, static_cast<long long>(S) * H_kv, rows, D, max_kv)) {
+    // Beside chunks of a prompt the other streams bring single tokens or drafted blocks as a rule, a column tile or two here and a fixed
+    // 64 rows there: 60 tokens over 3000 keys of 32 heads of 64 beside a chunk of 300 rows 256 against 405 us, 200 over 700 keys of 8
+    // heads of 128 122 against 146, 16 blocks of 5 rows 45 against 61; 30 trees of 22 rows 73 against 69.
+    if (!chunks_too && mid_pays(p.shape == kShapeShares, static_cast<long long>(S) * H_kv, rows, D, max_kv)) {
         p.shape = kShapeMid;
         p.grid = hawk_host::kPagedSms;
         p.rpi = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
@@ -916,7 +928,7 @@ extern "C" size_t hawk_paged_attn_workspace_bytes(int S, int T, int max_new, int
     if (max_new > T) max_new = T;
     const long long rows = static_cast<long long>(max_new) * (H / H_kv);
     const long long few = rows < kFewRows ? rows : kFewRows;
-    const size_t a = rows_workspace_bytes(plan_rows(S, static_cast<int>(few), H_kv, D, max_kv), D);
+    const size_t a = rows_workspace_bytes(plan_rows(S, static_cast<int>(few), H_kv, D, max_kv, rows > kFewRows), D);
     const size_t b = rows > kFewRows ? hawk_host::paged_tile_workspace_bytes(S, T, max_new, H, H_kv, kFewRows, D, max_kv) : 0;
     return align16(a) + b;
 }
@@ -950,7 +962,7 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     const long long rows_all = static_cast<long long>(max_new) * group;
     const bool tiles = rows_all > kFewRows;
     const int rows = static_cast<int>(tiles ? kFewRows : rows_all);
-    const RowsPlan plan = plan_rows(a.S, rows, a.H_kv, a.D, a.max_kv);
+    const RowsPlan plan = plan_rows(a.S, rows, a.H_kv, a.D, a.max_kv, tiles);
     // list positions are 32-bit numbers
     const int tk = kStageBytes / (4 * a.D);
     if (static_cast<double>(a.S) * a.H_kv * ((rows + plan.rpi - 1) / plan.rpi) * (a.max_kv / tk + 1) >= 2147483000.0 ||

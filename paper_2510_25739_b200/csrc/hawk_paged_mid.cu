@@ -1,4 +1,4 @@
-// hawk_paged_attn for streams of up to 64 rows per kv head: a few dozen (candidate trees, drafted blocks under grouped heads),
+// hawk_paged_attn for calls of up to 64 rows per kv head: a few dozen (candidate trees, drafted blocks under grouped heads),
 // or any number where the streams are few and long.
 //
 // Up to 64 rows share every key, so the call is bound by reading keys and values once, but past 8 rows the products are too
@@ -188,12 +188,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_proxy_async();
     grid_dependency_wait();
     int flags = 0;
-    if (P.groups && static_cast<int>(blockIdx.x) == P.row_blocks) {  // the block that makes the tile kernel's list
-        __syncthreads();
-        paged_plan(P, reinterpret_cast<int *>(smem), flags);
-        if (flags && P.dev_status) atomicOr(P.dev_status, flags);
-        return;
-    }
 
     // ---- prefix sum over the streams' tiles, and this block's share
     int running = 0;
@@ -202,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int v = 0;
         if (s < P.S) {
             const PagedStream st = paged_stream(P, s, flags);
-            if (st.n > 0 && paged_is_few(P, st)) v = P.H_kv * tiles_of(st.kv);
+            if (st.n > 0) v = P.H_kv * tiles_of(st.kv);
         }
         int inc = v;
 #pragma unroll
@@ -639,7 +633,7 @@ cudaError_t launch_n(const CUtensorMap &mq, const CUtensorMap &mk, const CUtenso
         if (e != cudaSuccess) return e;
         attr_done.fetch_or(1ull << device, std::memory_order_relaxed);
     }
-    return hawk_host::launch_dependent(paged_mid_kernel<T16, D, NR>, dim3(P.row_blocks + (P.groups ? 1 : 0)), dim3(kThreads),
+    return hawk_host::launch_dependent(paged_mid_kernel<T16, D, NR>, dim3(P.row_blocks), dim3(kThreads),
                                        MidCfg<D, NR>::smem(P.S), st, mq, mk, mv, P);
 }
 
@@ -656,8 +650,7 @@ cudaError_t launch(int nr, const CUtensorMap &mq, const CUtensorMap &mk, const C
 cudaError_t hawk_host::launch_paged_mid(const hawk_paged_attn_args &a, const PagedParams &base, int nr, cudaStream_t st)
 {
     PagedParams P = base;
-    // positions of an item (a group of more heads than rows: this kernel then has no streams, only the list to make)
-    const int tile_tok = nr >= P.group ? nr / P.group : 1;
+    const int tile_tok = nr / P.group;  // positions of an item
     P.box_rows = paged_gcd(a.page_size, kKeys);
     CUtensorMap mq, mk, mv;
     const uint64_t row = 2ull * a.q_row_stride, head = 2ull * a.q_head_stride;
