@@ -431,6 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int c0 = 0; c0 < D; c0 += 32) {
                 uint32_t o[32];
+                __syncwarp();  // (rows that store and rows that do not, together again)
                 tmem_ld_32x32(o_addr + c0, o);
                 tmem_ld_wait();
                 if (!valid) continue;
@@ -490,6 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             ok = ok && warp_wait(&s_full[b], (j >> 1) & 1u, abort_flag);
             tcgen05_fence_after();
+            __syncwarp();  // (whole-warp tensor-memory instructions here and below)
             uint32_t u[NH];
             tmem_ld_row<NH>(lane_off + b * 64 + g * NH, u);
             tmem_ld_wait();
@@ -553,6 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     ok = ok && warp_wait(&p_free[b ^ 1], ((j - 1) >> 1) & 1u, abort_flag);
                     tcgen05_fence_after();
                     const float a = lane < NH ? alpha[g * 32 + lane] : 1.f;
+                    __syncwarp();
 #pragma unroll
                     for (int c0 = 0; c0 < D; c0 += 16) {
                         uint32_t o[16];
@@ -614,6 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!ok) *abort_flag = 1;
     }
+    __syncwarp();
     tcgen05_fence_before();
     __syncthreads();
     if (warp == 10) tmem_dealloc(*tmem_ptr, 512);

@@ -199,10 +199,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (warp == 9) {
         __syncwarp();
-        asm volatile("bar.arrive 0, %0;" ::"n"(kThreads) : "memory");  // the barriers are there; the loads need nothing else
+        // The barriers are there; the loads need nothing else.  (Named barrier 2, not 0: this warp does not wait here, and a job
+        // without keys or a slow tensor-memory allocation can bring it to the block's last barrier before the others pass this one.)
+        asm volatile("bar.arrive 2, %0;" ::"n"(kThreads) : "memory");
     } else {
         tcgen05_fence_before();
-        asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+        asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");
         tcgen05_fence_after();
     }
     constexpr uint32_t tmem = 0;  // all 512 columns are the block's: its tensor memory starts at lane 0, column 0
@@ -448,6 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (q * 32 + c >= seen) u[q][c] = 0xff800000u;  // -inf
                 }
             }
+            __syncwarp();  // (whole-warp tensor-memory instructions follow)
             float mx[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -553,6 +556,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int c0 = 0; c0 < D; c0 += 32) {
                     uint32_t o[32];
+                    __syncwarp();  // (rows that store and rows that do not, together again)
                     if (nt > 0) {
                         tmem_ld_32x32(o_addr + c0, o);
                         tmem_ld_wait();
@@ -594,6 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         }
     }
+    __syncwarp();
     tcgen05_fence_before();
     __syncthreads();
     if (warp == 8) tmem_dealloc(*tmem_ptr, 512);

@@ -204,3 +204,21 @@ def test_index_checks_and_guards(new, kv, H, H_kv, D, tree, debug_lib):
     got = f64(out).reshape(b.T, H, D)
     got[:begin[0]] = got[begin[-1]:] = 7.0
     _compare(got, want, size, b.dt)
+
+
+def test_chunks_without_keys_again_and_again():
+    """Chunks whose rows see nothing among chunks that do: blocks without work end while others of their SM begin."""
+    rng = np.random.default_rng(82)
+    new = [int(x) for x in rng.integers(65, 200, 120)]
+    kv = [0 if s % 2 else n for s, n in enumerate(new)]
+    for D in (64, 128):
+        b = Batch(new, kv, 2, 2, D, 16, seed=83)
+        d = b.cuda()
+        first, status = _run(b, dev=d)
+        assert status == 0
+        for s in range(1, 120, 2):
+            assert (first[int(b.row_begin[s]):int(b.row_begin[s + 1])] == 0).all()
+        _check(b, dev=d)
+        for _ in range(30):
+            again, status = _run(b, dev=d)
+            assert status == 0 and np.array_equal(first, again)
