@@ -222,3 +222,37 @@ def test_chunks_without_keys_again_and_again():
         for _ in range(30):
             again, status = _run(b, dev=d)
             assert status == 0 and np.array_equal(first, again)
+
+
+def test_what_the_device_finds_wrong_in_long_streams():
+    """The same findings as in test_gpu_paged_attn.py, in the kernel for few long streams."""
+    b = Batch([12, 9, 3], [3000, 2000, 500], 2, 2, 128, 16, seed=84)
+    want, size = paged.paged_attn(f64(b.q), f64(b.k_pages), f64(b.v_pages), b.block_table.numpy(), b.row_begin.numpy(),
+                                  b.kv_len.numpy(), 128 ** -0.5)
+
+    def others_stand(got, s):
+        ok = np.ones(b.T, dtype=bool)
+        ok[int(b.row_begin[s]):int(b.row_begin[s + 1])] = False
+        h = 2.0 ** -8
+        assert (np.abs(got - want)[ok] <= (h * np.abs(want) + (h + 2.0 ** -11) * size)[ok]).all()
+
+    for page in (b.n_pages, -1, 2 ** 31 - 1):
+        d = b.cuda()
+        d.block_table[1, 77] = page
+        got, status = _run(b, dev=d)
+        assert status == binding.DEV_BAD_PAGE
+        others_stand(got, 1)
+    for bad in (3001, -1):
+        d = b.cuda()
+        d.kv_len[2] = bad
+        got, status = _run(b, dev=d)
+        assert status == binding.DEV_BAD_PREFIX or (bad > 0 and status == binding.DEV_BAD_PREFIX | binding.DEV_BAD_PAGE)
+        others_stand(got, 2)
+    d = b.cuda()
+    d.row_begin[1] = 30
+    got, status = _run(b, dev=d)
+    assert status == binding.DEV_BAD_ROWS and (got[:21] == 7.0).all()
+    d = b.cuda()
+    got, status = _run(b, dev=d, max_new=11)
+    assert status == binding.DEV_BAD_ROWS and (got[:12] == 7.0).all()
+    others_stand(got, 0)
