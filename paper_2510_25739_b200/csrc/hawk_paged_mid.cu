@@ -15,8 +15,10 @@
 //   10        products    11, 12  loads of keys and of values (one warp for both issued a tile's 32 boxes of 16 keys in 3000
 //             cycles, which set the pace)
 // A row's shift m (see the rows kernel: it moves only when a score exceeds it by 2^8) is exact at an item's first tile, from a
-// reduction across the warps; after that a vote of the four warps is all that a tile costs.  Row sums stay in the threads (a key
-// each) until the item ends.
+// reduction across the warps; after that a vote of the four warps is all that a tile costs.  A tile renews its shifts once at most,
+// whatever the scores then look like (they may exceed a new shift by what its rounding lost, again and again).  The query box
+// of a short item ends in rows that are another stream's or nobody's: their shift is -inf, so that they have no vote.
+// Row sums stay in the threads (a key each) until the item ends.
 // Measured (D = 128, 16-row pages): 256 items of 8000 keys in 164 us at 32 rows and 172 at 60, 98 and 93 % of the rate of a
 // copy; of 2400 keys 58 and 64 us against 49 of reading: some 5 us before the first product and 4 of join.  What paces a tile is
 // the loads up to 32 rows and the softmax warps above.  At D = 64 a tile is 16 KB + 16 KB and the softmax sets the pace at any rows
@@ -483,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     masks[g * 32 + key] = m;
                     m_smem[ob * 64 + g * 32 + key] = -CUDART_INF_F;
-                    shift[g * 32 + key] = kNoShift;
+                    shift[g * 32 + key] = r < c.n * P.group ? kNoShift : -CUDART_INF_F;
                 }
 #pragma unroll
                 for (int r2 = 0; r2 < NH / 2; ++r2) lsum[r2] = 0;
@@ -503,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (rel >= 64 || !((masks[g * 32 + r] >> rel) & 1ull)) u[r] = 0xff800000u;  // -inf
                 }
             }
-            bool force = begins;
+            bool renewed = false;
             const uint64_t scale2 = pack2(P.scale_log2, P.scale_log2);
             const ulonglong2 *s4 = reinterpret_cast<const ulonglong2 *>(shift + g * 32);
             float x[NH];
@@ -521,8 +523,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     x[4 * r4 + 3] = hi.y;
                     top = fmaxf(fmaxf(top, fmaxf(lo.x, lo.y)), fmaxf(hi.x, hi.y));
                 }
+                if (renewed) {
+                    // once a tile; the vote also keeps the next item's shifts waiting until all have read this one's
+                    ok = !group_any(bar_id, !ok);
+                    break;
+                }
                 // one vote for both: a score too high, or a wait of this warp that gave up
-                if (!group_any(bar_id, force || top > kLazy || !ok)) break;
+                if (!group_any(bar_id, begins || top > kLazy || !ok)) break;
                 if (group_any(bar_id, !ok)) {  // then all four warps leave together
                     ok = false;
                     break;
@@ -541,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const float m_old = m_smem[ob * 64 + g * 32 + key];
                     const float m_new = fmaxf(m_old, fmaxf(fmaxf(wm[0], wm[32]), fmaxf(wm[64], wm[96])) * P.scale_log2);
                     m_smem[ob * 64 + g * 32 + key] = m_new;
-                    shift[g * 32 + key] = m_new == -CUDART_INF_F ? kNoShift : -m_new;
+                    if (g * NH + key < c.n * P.group) shift[g * 32 + key] = m_new == -CUDART_INF_F ? kNoShift : -m_new;
                     alpha[g * 32 + key] = m_new == -CUDART_INF_F ? 1.f : fast_exp2(m_old - m_new);
                 }
                 group_sync(bar_id);
@@ -567,9 +574,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     tmem_st_wait();
                 }
-                force = false;
+                renewed = true;
             }
-            if (!ok) break;  // (uniform: see the vote)
+            if (!ok) break;  // (uniform: see the votes)
             if (j >= 2) ok = ok && warp_wait(&p_free[b], ((j >> 1) - 1) & 1u, abort_flag);
             uint8_t *prow = p_smem + b * C::kPBytes + key * 128;
 #pragma unroll
