@@ -538,7 +538,8 @@ hawk_status hawk_rope_append(const hawk_rope_append_args *args, int32_t *dev_sta
  * them.  Scores, maxima, sums and accumulators are fp32; the probabilities are rounded to the 16-bit type for the
  * second product, the result once.
  * Cache rows from kv_len[s] on are never used (they may hold anything, NaN included).  Rows below kv_len[s] must be
- * finite: a NaN or infinity among a stream's own rows may reach rows of that stream that do not see it.
+ * finite: a NaN or infinity among a stream's own rows may reach rows of that stream that do not see it.  Scores may have any
+ * size that fp32 holds, before and after sm_scale.
  *
  *   q          16-bit [T][H][D] at row and head strides
  *   out        16-bit [T][H*D], dense; must not overlap any input

@@ -77,6 +77,17 @@ __device__ __forceinline__ bool paged_is_few(const PagedParams &P, const PagedSt
     return static_cast<long long>(st.n) * P.group <= P.rows_few;
 }
 
+// Softmax.  Maxima are kept as the products gave them, not yet scaled (partial results too), so nothing is lost in them.  The
+// exponent of a score s under the shift m is one fma, s * scale - fl(m * scale): the rounding of that product is in every exponent of the
+// row alike, as if the shift were another, and is under 2^-15 for shifts below this bound.  Beyond it (from 2^28 on it could exceed the 2^8
+// that a probability may reach, from 2^31 on what fp32 holds) rows take (s - m) * scale, the difference being exact where it
+// counts, for s near m; or they add what was lost, fl(m * scale) - m * scale, which fp32 holds exactly.  (That sum is off by 2^-24 of what
+// was lost and of the exponent: under 2^-17 up to shifts of 2^30; beyond them scores are 2^6 and more apart or equal, and equal
+// ones give 0.)  Decided for all rows of a warp or group at a renewal of their shifts.
+constexpr float kFarShift = 512.f;  // base 2
+
+__device__ __forceinline__ bool is_far(float m, float scale) { return m != -CUDART_INF_F && fabsf(m * scale) >= kFarShift; }
+
 constexpr int kPagedTileKeys = 128;  // keys of a tile of the tile kernel
 constexpr int kPlanBuckets = 256;
 

@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
     uint32_t qb[NQT][DB][2];
     float ot[NQT][DB][4];
     float mrun[NQT][2], lrun[NQT][2];
+    bool far = false;                     // some row's shift is (see kFarShift)
     int hk = 0, row0 = 0, nrows = 0;      // of the segment's item: kv head, first row of the chunk, rows
     int seg_r0 = 0, seg_tile = 0;
     bool seg_first = true, open = false;  // first segment of the share; a segment is being worked on
@@ -393,6 +394,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
         if (!open) {
             // ---- a new segment: this item's queries, empty state
             open = true;
+            far = false;
             hk = cc.hk;
             row0 = cc.chunk * RPI;
             nrows = min(RPI, cc.n * P.group - row0);
@@ -476,11 +478,12 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
                     float m = -CUDART_INF_F;
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb) m = fmaxf(m, fmaxf(sc[nq][kb][c], sc[nq][kb][2 + c]));
-                    mx[nq][c] = m * P.scale_log2;
-                    grows |= mx[nq][c] > mrun[nq][c] + kLazy;
+                    mx[nq][c] = m;
+                    grows |= (m - mrun[nq][c]) * P.scale_log2 > kLazy;  // (no score yet and none now: NaN, no)
                 }
             }
             if (__any_sync(0xffffffffu, grows)) {
+                bool is = false;
 #pragma unroll
                 for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -489,8 +492,9 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
 #pragma unroll
                         for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
                         m = fmaxf(m, mrun[nq][c]);
-                        const float a = fast_exp2(mrun[nq][c] - (m == -CUDART_INF_F ? 0.f : m));
+                        const float a = fast_exp2((mrun[nq][c] - (m == -CUDART_INF_F ? 0.f : m)) * P.scale_log2);
                         mrun[nq][c] = m;
+                        is |= is_far(m, P.scale_log2);
                         lrun[nq][c] *= a;
 #pragma unroll
                         for (int db = 0; db < DB; ++db) {
@@ -498,18 +502,30 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
                             ot[nq][db][2 + c] *= a;
                         }
                     }
+                far = __any_sync(0xffffffffu, is);
             }
             uint32_t pb[NQ][KB][2];
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq) {
                 const float mu0 = mrun[nq][0] == -CUDART_INF_F ? 0.f : mrun[nq][0];
                 const float mu1 = mrun[nq][1] == -CUDART_INF_F ? 0.f : mrun[nq][1];
+                float sh0 = -mu0 * P.scale_log2, sh1 = -mu1 * P.scale_log2;
+                if (far) {
+                    sh0 = sh1 = 0.f;
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) {
+                        sc[nq][kb][0] -= mu0;
+                        sc[nq][kb][1] -= mu1;
+                        sc[nq][kb][2] -= mu0;
+                        sc[nq][kb][3] -= mu1;
+                    }
+                }
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
-                    const float p0 = fast_exp2(fmaf(sc[nq][kb][0], P.scale_log2, -mu0));
-                    const float p1 = fast_exp2(fmaf(sc[nq][kb][1], P.scale_log2, -mu1));
-                    const float p2 = fast_exp2(fmaf(sc[nq][kb][2], P.scale_log2, -mu0));
-                    const float p3 = fast_exp2(fmaf(sc[nq][kb][3], P.scale_log2, -mu1));
+                    const float p0 = fast_exp2(fmaf(sc[nq][kb][0], P.scale_log2, sh0));
+                    const float p1 = fast_exp2(fmaf(sc[nq][kb][1], P.scale_log2, sh1));
+                    const float p2 = fast_exp2(fmaf(sc[nq][kb][2], P.scale_log2, sh0));
+                    const float p3 = fast_exp2(fmaf(sc[nq][kb][3], P.scale_log2, sh1));
                     lrun[nq][0] += p0 + p2;
                     lrun[nq][1] += p1 + p3;
                     pb[nq][kb][0] = movmatrix_trans(E::pack(p0, p1));
@@ -592,7 +608,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
                 const float2 m_l = *reinterpret_cast<const float2 *>(ps + RPI * D + 2 * r);
                 const float mn = fmaxf(mm, m_l.x);
                 const float mu = mn == -CUDART_INF_F ? 0.f : mn;
-                const float f_old = fast_exp2(mm - mu), f_new = fast_exp2(m_l.x - mu);
+                const float f_old = fast_exp2((mm - mu) * P.scale_log2), f_new = fast_exp2((m_l.x - mu) * P.scale_log2);
                 mm = mn;
                 ll = ll * f_old + m_l.y * f_new;
 #pragma unroll
@@ -699,7 +715,7 @@ __global__ void __launch_bounds__(256, 3) paged_merge_kernel(const PagedParams P
     auto fold_row = [&](int r, float m, float l, const float (&v)[PER]) {
         const float mn = fmaxf(mm[r], m);
         const float mu = mn == -CUDART_INF_F ? 0.f : mn;
-        const float f_old = fast_exp2(mm[r] - mu), f_new = fast_exp2(m - mu);
+        const float f_old = fast_exp2((mm[r] - mu) * P.scale_log2), f_new = fast_exp2((m - mu) * P.scale_log2);
         mm[r] = mn;
         ll[r] = ll[r] * f_old + l * f_new;
 #pragma unroll

@@ -47,8 +47,8 @@ struct MidCfg {
     static constexpr int kQHalfBytes = NR * 128;
     static constexpr int kQBytes = kHalves * kQHalfBytes;
     static constexpr int kPBytes = kKeys * 128;
-    // float m[2][64], alpha[64], shift[64], wmax[2][4][32], sums[2][2][4][32]; uint64 masks[64]; barriers; small things
-    static constexpr int kSmallBytes = 2 * 64 * 4 + 2 * 64 * 4 + 3 * 2 * 4 * 32 * 4 + 64 * 8 + (2 * kStages + 18) * 8 + 256;
+    // float m[2][64], alpha[64], shift[64], lost[64], wmax[2][4][32], sums[2][2][4][32]; uint64 masks[64]; barriers; small things
+    static constexpr int kSmallBytes = 2 * 64 * 4 + 3 * 64 * 4 + 3 * 2 * 4 * 32 * 4 + 64 * 8 + (2 * kStages + 18) * 8 + 256;
     static constexpr size_t smem(int S)
     {
         return 1024 + static_cast<size_t>(kStages) * kTileBytes + 2 * kQBytes + 2 * kPBytes + kSmallBytes +
@@ -149,7 +149,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     float *m_smem = reinterpret_cast<float *>(p_smem + 2 * C::kPBytes);  // [2 items][64]: group g's row r at 32 g + r
     float *alpha = m_smem + 128;                                      // [64]
     float *shift = alpha + 64;                                        // [64]: what a row adds to its scores
-    float *wmax = shift + 64;                                         // [2 groups][4 warps][32]
+    float *lost = shift + 64;                                         // [64]: what that sum of a row's maximum lacks to 0
+    float *wmax = lost + 64;                                          // [2 groups][4 warps][32]
     float *sums = wmax + 256;                                         // [2 items][2 groups][4 warps][32]
     uint64_t *masks = reinterpret_cast<uint64_t *>(sums + 512);       // [64]: block rows that a row sees
     uint64_t *full = masks + 64, *empty = full + C::kStages;
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_ptr + 1);
     int *wsum = reinterpret_cast<int *>(tmem_ptr + 2);  // [16]
     int *prefix = wsum + 16;                            // [S + 1]
-    static_assert(2 * 64 * 4 + 2 * 64 * 4 + 768 * 4 + 64 * 8 + (2 * C::kStages + 17) * 8 + 8 + 64 <= C::kSmallBytes, "");
+    static_assert(2 * 64 * 4 + 3 * 64 * 4 + 768 * 4 + 64 * 8 + (2 * C::kStages + 17) * 8 + 8 + 64 <= C::kSmallBytes, "");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -467,6 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         Cursor c = first;
         int item = 0;
         bool begins = true;
+        bool far = false;       // some row's shift is (see kFarShift)
         uint64_t lsum[NH / 2];  // of this thread's keys, two rows a register pair
         const int tiles = first.left;
         for (int j = 0; j < tiles; ++j) {
@@ -489,6 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
 #pragma unroll
                 for (int r2 = 0; r2 < NH / 2; ++r2) lsum[r2] = 0;
+                far = false;
                 group_sync(bar_id);
             }
             ok = ok && warp_wait(&s_full[b], (j >> 1) & 1u, abort_flag);
@@ -524,16 +527,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                     top = fmaxf(fmaxf(top, fmaxf(lo.x, lo.y)), fmaxf(hi.x, hi.y));
                 }
                 if (renewed) {
-                    // once a tile; the vote also keeps the next item's shifts waiting until all have read this one's
+                    if (far) {
+#pragma unroll
+                        for (int r = 0; r < NH; ++r) x[r] += lost[g * 32 + r];
+                    }
+                    // once a tile, whatever the scores still are.  The vote: a warp that gave up takes the others along, and the next
+                    // item's shifts wait until all have read this one's
                     ok = !group_any(bar_id, !ok);
                     break;
                 }
-                // one vote for both: a score too high, or a wait of this warp that gave up
-                if (!group_any(bar_id, begins || top > kLazy || !ok)) break;
-                if (group_any(bar_id, !ok)) {  // then all four warps leave together
-                    ok = false;
-                    break;
-                }
+                // one vote for all: a score too high, far shifts (renewed at every tile), or a wait of this warp that gave up
+                if (!group_any(bar_id, begins || far || top > kLazy || !ok)) break;
                 // new maxima: across the lanes, then across the four warps
                 float mine = -CUDART_INF_F;
 #pragma unroll
@@ -542,14 +546,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (lane == r) mine = v;
                 }
                 wmax[(g * 4 + wg) * 32 + lane] = mine;
-                group_sync(bar_id);
+                // (a row's maximum is far only if some warp's is)
+                far = group_any(bar_id, far || (lane < NH && g * NH + lane < c.n * P.group && is_far(mine, P.scale_log2)));
                 if (key < NH) {
                     const float *wm = wmax + g * 128 + key;
                     const float m_old = m_smem[ob * 64 + g * 32 + key];
-                    const float m_new = fmaxf(m_old, fmaxf(fmaxf(wm[0], wm[32]), fmaxf(wm[64], wm[96])) * P.scale_log2);
+                    const float m_new = fmaxf(m_old, fmaxf(fmaxf(wm[0], wm[32]), fmaxf(wm[64], wm[96])));
+                    const bool none = m_new == -CUDART_INF_F;
+                    const float sh = none ? kNoShift : -m_new * P.scale_log2;
                     m_smem[ob * 64 + g * 32 + key] = m_new;
-                    if (g * NH + key < c.n * P.group) shift[g * 32 + key] = m_new == -CUDART_INF_F ? kNoShift : -m_new;
-                    alpha[g * 32 + key] = m_new == -CUDART_INF_F ? 1.f : fast_exp2(m_old - m_new);
+                    if (g * NH + key < c.n * P.group) shift[g * 32 + key] = sh;
+                    lost[g * 32 + key] = none ? 0.f : -fmaf(m_new, P.scale_log2, sh);
+                    alpha[g * 32 + key] = none ? 1.f : fast_exp2((m_old - m_new) * P.scale_log2);
                 }
                 group_sync(bar_id);
 #pragma unroll
@@ -557,9 +565,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const float2 a2 = *reinterpret_cast<const float2 *>(alpha + g * 32 + 2 * r2);
                     lsum[r2] = mul2(lsum[r2], pack2(a2.x, a2.y));
                 }
-                if (!begins && wg == g) {
+                if (!begins && wg == g && ok) {
                     // O's lanes of this group: its last product done, the next not started (P of this tile is not out)
-                    ok = ok && warp_wait(&p_free[b ^ 1], ((j - 1) >> 1) & 1u, abort_flag);
+                    ok = warp_wait(&p_free[b ^ 1], ((j - 1) >> 1) & 1u, abort_flag);
                     tcgen05_fence_after();
                     const float a = lane < NH ? alpha[g * 32 + lane] : 1.f;
                     __syncwarp();

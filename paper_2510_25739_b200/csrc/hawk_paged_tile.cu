@@ -421,13 +421,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int first = job.begin + (job.single ? t : 0), stride = job.single ? 2 : 1;  // key tiles of the slot
         const uint64_t scale2 = pack2(P.c.scale_log2, P.c.scale_log2);
         float m_run = -CUDART_INF_F, l_run = 0.f;
+        bool far = false;  // some row's shift is (see kFarShift)
         const int nt = job.nt[t];
         bool ok = true;
-        for (int i = 0; i < nt; ++i) {
+        uint32_t u[4][32];
+        float m_new = 0.f;
+        auto take_scores = [&](int i) {  // tile i's scores, masked, and the row's maximum with them
             ok = warp_wait(&s_full[t], i & 1u, abort_flag);
-            if (!ok) break;
+            if (!ok) return false;
             tcgen05_fence_after();
-            uint32_t u[4][32];
 #pragma unroll
             for (int q = 0; q < 4; ++q) tmem_ld_32x32(s_addr + q * 32, u[q]);
             tmem_ld_wait();
@@ -458,13 +460,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int c = 1; c < 32; ++c) mx[q] = fmaxf(mx[q], __uint_as_float(u[q][c]));
             }
-            const float m_new = fmaxf(m_run, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * P.c.scale_log2);
-            if (i == 0) {
-                m_run = m_new;
-            } else if (__any_sync(0xffffffffu, m_new > m_run + 8.f)) {
+            m_new = fmaxf(m_run, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+            return true;
+        };
+        auto renew = [&](int i) {  // m_new becomes the shift
+            if (i > 0) {
                 const float mu = m_new == -CUDART_INF_F ? 0.f : m_new;
-                const float alpha = fast_exp2(m_run - mu);
-                m_run = m_new;
+                const float alpha = fast_exp2((m_run - mu) * P.c.scale_log2);
                 l_run *= alpha;
 #pragma unroll
                 for (int c0 = 0; c0 < D; c0 += 16) {
@@ -476,16 +478,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tmem_st_32x16(o_addr + c0, o);
                 }
             }
-            const float mu = m_run == -CUDART_INF_F ? 0.f : m_run;
-            const uint64_t shift2 = pack2(-mu, -mu);
-            uint64_t sum_a = 0, sum_b = 0;  // (two zeros each)
+            m_run = m_new;
+        };
+        auto exponentials = [&](auto argument) {  // the tile's probabilities, handed over in halves, and their sum
+            uint64_t sum_a = 0, sum_b = 0;        // (two zeros each)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 uint32_t pk[32];
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
                     const int q = half * 2 + (c >> 4), e = (2 * c) & 31;
-                    const uint64_t x2 = fma2(pack2(__uint_as_float(u[q][e]), __uint_as_float(u[q][e + 1])), scale2, shift2);
+                    const uint64_t x2 = argument(pack2(__uint_as_float(u[q][e]), __uint_as_float(u[q][e + 1])));
                     float2 p;
                     if (D == 64 && c % 4 == 3) {
                         p = exp2_fma(x2);
@@ -506,6 +509,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             const float2 sums2 = unpack2(add2(sum_a, sum_b));
             l_run += sums2.x + sums2.y;
+        };
+        for (int i = 0; i < nt; ++i) {
+            if (!take_scores(i)) break;
+            if (i == 0 || __any_sync(0xffffffffu, (m_new - m_run) * P.c.scale_log2 > 8.f)) {  // (no score yet and none now: NaN, no)
+                renew(i);
+                far = __any_sync(0xffffffffu, valid && is_far(m_run, P.c.scale_log2));
+            }
+            const float mu = m_run == -CUDART_INF_F ? 0.f : m_run;
+            // (two copies: differences taken in place for the far ones cost the long prefill 2.5 % instead of 1.4)
+            if (!far) {
+                const uint64_t shift2 = pack2(-mu * P.c.scale_log2, -mu * P.c.scale_log2);
+                exponentials([&](uint64_t s) { return fma2(s, scale2, shift2); });
+            } else {
+                const uint64_t minus2 = pack2(-mu, -mu);
+                exponentials([&](uint64_t s) { return mul2(add2(s, minus2), scale2); });
+            }
         }
         if (ok && nt > 0) ok = warp_wait(&o_done[t], 0, abort_flag);
         if (ok && job.single && job.tiles > 1) ok = warp_wait(&o_done[t ^ 1], 0, abort_flag);  // (Q is free then)
@@ -536,8 +555,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 o = ml_smem[r];
                 const float m = fmaxf(m_run, o.x);
                 const float mu = m == -CUDART_INF_F ? 0.f : m;
-                f_own = l_run == 0.f ? 0.f : fast_exp2(m_run - mu);
-                f_other = o.y == 0.f ? 0.f : fast_exp2(o.x - mu);
+                f_own = l_run == 0.f ? 0.f : fast_exp2((m_run - mu) * P.c.scale_log2);
+                f_other = o.y == 0.f ? 0.f : fast_exp2((o.x - mu) * P.c.scale_log2);
                 l_run = l_run * f_own + o.y * f_other;
                 m_run = m;
             }
@@ -635,7 +654,7 @@ __global__ void __launch_bounds__(256) paged_tile_merge_kernel(const TileParams 
     for (int x = 0; x < P.n_split; ++x) {
         const float *p = parts + static_cast<size_t>(x) * C::kPartFloats;
         const float2 v = *reinterpret_cast<const float2 *>(p + 2 * kBM * D + 2 * prow);
-        const float f = v.y == 0.f ? 0.f : fast_exp2(v.x - m);
+        const float f = v.y == 0.f ? 0.f : fast_exp2((v.x - m) * P.c.scale_log2);
         l = fmaf(v.y, f, l);
 #pragma unroll
         for (int c = 0; c < PER; ++c) {
