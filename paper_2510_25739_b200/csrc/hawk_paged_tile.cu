@@ -512,7 +512,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         for (int i = 0; i < nt; ++i) {
             if (!take_scores(i)) break;
-            if (i == 0 || __any_sync(0xffffffffu, (m_new - m_run) * P.c.scale_log2 > 8.f)) {  // (no score yet and none now: NaN, no)
+            // (no score yet and none now: NaN, no.  A tile's last rows may be another stream's or nobody's: they have no vote)
+            if (i == 0 || __any_sync(0xffffffffu, valid && (m_new - m_run) * P.c.scale_log2 > 8.f)) {
                 renew(i);
                 far = __any_sync(0xffffffffu, valid && is_far(m_run, P.c.scale_log2));
             }
