@@ -421,7 +421,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int first = job.begin + (job.single ? t : 0), stride = job.single ? 2 : 1;  // key tiles of the slot
         const uint64_t scale2 = pack2(P.c.scale_log2, P.c.scale_log2);
         float m_run = -CUDART_INF_F, l_run = 0.f;
-        bool far = false;  // some row's shift is (see kFarShift)
         const int nt = job.nt[t];
         bool ok = true;
         uint32_t u[4][32];
@@ -510,22 +509,28 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float2 sums2 = unpack2(add2(sum_a, sum_b));
             l_run += sums2.x + sums2.y;
         };
+        // what the fma adds to a row's scores: minus the shift, or for a row without one so much that any score is too high (-inf stays
+        // -inf)
+        constexpr float kNoShift = 3e38f;
+        float sh = kNoShift;
         for (int i = 0; i < nt; ++i) {
             if (!take_scores(i)) break;
-            // (no score yet and none now: NaN, no.  A tile's last rows may be another stream's or nobody's: they have no vote)
-            if (i == 0 || __any_sync(0xffffffffu, valid && (m_new - m_run) * P.c.scale_log2 > 8.f)) {
+            // (a tile's last rows may be another stream's or nobody's: they have no vote)
+            if (__any_sync(0xffffffffu, valid && fmaf(m_new, P.c.scale_log2, sh) > 8.f)) {
                 renew(i);
-                far = __any_sync(0xffffffffu, valid && is_far(m_run, P.c.scale_log2));
+                sh = m_run == -CUDART_INF_F ? kNoShift : -m_run * P.c.scale_log2;
+                // far shifts (see kFarShift) are renewed at every tile, so that the loop's usual way knows nothing of them (a flag in
+                // it cost the prefill 2 % at D = 128 and 5 % at D = 64; this way nothing)
+                if (__any_sync(0xffffffffu, valid && is_far(m_run, P.c.scale_log2))) {
+                    const float minus = m_run == -CUDART_INF_F ? 0.f : -m_run;
+                    const uint64_t minus2 = pack2(minus, minus);
+                    exponentials([&](uint64_t s) { return mul2(add2(s, minus2), scale2); });
+                    sh = kNoShift;  // (so that the next tile comes here again)
+                    continue;
+                }
             }
-            const float mu = m_run == -CUDART_INF_F ? 0.f : m_run;
-            // (two copies: differences taken in place for the far ones cost the long prefill 2.5 % instead of 1.4)
-            if (!far) {
-                const uint64_t shift2 = pack2(-mu * P.c.scale_log2, -mu * P.c.scale_log2);
-                exponentials([&](uint64_t s) { return fma2(s, scale2, shift2); });
-            } else {
-                const uint64_t minus2 = pack2(-mu, -mu);
-                exponentials([&](uint64_t s) { return mul2(add2(s, minus2), scale2); });
-            }
+            const uint64_t shift2 = pack2(sh, sh);
+            exponentials([&](uint64_t s) { return fma2(s, scale2, shift2); });
         }
         if (ok && nt > 0) ok = warp_wait(&o_done[t], 0, abort_flag);
         if (ok && job.single && job.tiles > 1) ok = warp_wait(&o_done[t ^ 1], 0, abort_flag);  // (Q is free then)
