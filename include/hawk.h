@@ -475,13 +475,15 @@ hawk_status hawk_verify_step_host(const hawk_step_host_args *args, hawk_stream_t
  *   q, k         16-bit [T][H][D], [T][H_kv][D] at row and head strides (elements), so that both may be parts of
  *                one projection's output.  H or H_kv may be 0 (that tensor is absent).
  *   q_out, k_out the same shapes, own strides; may be q and k themselves (same strides), else must not overlap them
- *   q_weight, k_weight, q_bias, k_bias   16-bit [D], or with per_head [H][D] / [H_kv][D]; a bias may be NULL
- *                (none); weights are required by a norm of that tensor, ignored with HAWK_NORM_NONE
+ *   q_weight, k_weight, q_bias, k_bias   16-bit [D], or with per_head [H][D] / [H_kv][D]; weights are required by a
+ *                norm of that tensor; a bias may be NULL (none) and goes with HAWK_NORM_LAYER only; all four are ignored
+ *                with HAWK_NORM_NONE
  *   position     int32 [T]
  *   cos_sin      fp32 [n_positions][rot_dim], 16-byte aligned
  * Supported: D in {64, 128}; rot_dim a multiple of 16, 0 <= rot_dim <= D (0: no rotation, position and
  * cos_sin are not read).  A position outside [0, n_positions) is clamped and flagged HAWK_DEV_BAD_POSITION.
- * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, PARAM (eps not a finite number >= 0, unknown dtype or norm), CUDA.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, PARAM (eps not a finite number >= 0, unknown dtype or norm, a bias under
+ * HAWK_NORM_RMS), CUDA.
  * T == 0 returns HAWK_OK without a launch.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct hawk_qk_rope_args {

@@ -8,6 +8,8 @@ import numpy as np
 
 def norm_rope(x, position, cos_sin, norm="none", eps=1e-6, weight=None, bias=None, interleaved=False):
     """x [T, heads, D] float64 -> (y, size): size bounds the terms that each element of y was summed from."""
+    if norm == "rms" and bias is not None:
+        raise ValueError("an RMS norm has no bias")
     x = np.array(x, dtype=np.float64)
     size = np.abs(x)
     if norm == "layer":

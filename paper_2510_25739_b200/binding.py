@@ -548,7 +548,8 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], position:
                  dev_status: Optional[torch.Tensor] = None):
     """Norm of every head ("none", "rms", "layer"), then the position rotation: q [T,H,D], k [T,H_kv,D] (bf16 or fp16, any
     row and head strides) -> (q_out, k_out).  cos_sin fp32 [positions, rot_dim] holds cosines, then sines, of each position;
-    position int32 [T]; None for both: no rotation.  Weights and biases are [D], or [heads, D] one for each head."""
+    position int32 [T]; None for both: no rotation.  Weights and biases are [D], or [heads, D] one for each head; a bias goes with
+    "layer" only."""
     lib = _lib or load_library()
     rc, q_out, k_out = _marshal.qk_norm_rope(lib.address_qk_norm_rope, q, k, position, cos_sin, norm, eps, q_weight, k_weight,
                                              q_bias, k_bias, interleaved, q_out, k_out, dev_status)

@@ -232,6 +232,8 @@ struct Rope {
             a.k_weight = dense(wk, "k_weight", w.dtype, k_shape, w.index);
             a.q_bias = dense(tensor(opts[4], "q_bias", false), "q_bias", w.dtype, q_shape, w.index);
             a.k_bias = dense(tensor(opts[5], "k_bias", false), "k_bias", w.dtype, k_shape, w.index);
+            if (a.norm == HAWK_NORM_RMS && (a.q_bias || a.k_bias))
+                refuse(PyExc_ValueError, std::string(a.q_bias ? "q_bias" : "k_bias") + ": goes with norm 'layer', not with 'rms'");
         }
         if (const at::Tensor *cs = tensor(args[3], "cos_sin", false)) {
             dims(*cs, "cos_sin", 2);

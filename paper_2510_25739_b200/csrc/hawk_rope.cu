@@ -376,6 +376,12 @@ hawk_status check_qk(const hawk_qk_rope_args &a, bool k_dense)
     return HAWK_OK;
 }
 
+// The formula of HAWK_NORM_RMS has no bias: one that is given is refused, not dropped.
+bool has_stray_bias(const hawk_qk_rope_args &a)
+{
+    return a.norm == HAWK_NORM_RMS && ((a.H > 0 && a.q_bias) || (a.H_kv > 0 && a.k_bias));
+}
+
 RopeParams params_of(const hawk_qk_rope_args &a, int32_t *dev_status)
 {
     RopeParams P = {};
@@ -475,6 +481,7 @@ extern "C" hawk_status hawk_qk_norm_rope(const hawk_qk_rope_args *a, int32_t *de
     const hawk_status chk = check_qk(*a, true);
     if (chk != HAWK_OK) return chk;
     if (a->T == 0 || (a->H == 0 && a->H_kv == 0)) return HAWK_OK;
+    if (has_stray_bias(*a)) return HAWK_ERR_PARAM;
     RopeParams P = params_of(*a, dev_status);
     return launch_rope(P, a->D, a->dtype, false, stream);
 }
@@ -494,6 +501,7 @@ extern "C" hawk_status hawk_rope_append(const hawk_rope_append_args *a, int32_t 
     if (!strides_ok(a->v_row_stride, a->v_head_stride) || !strides_ok(a->k_page_stride, a->k_page_head_stride) ||
         !strides_ok(a->v_page_stride, a->v_page_head_stride) || !strides_ok(a->k_page_row_stride, a->v_page_row_stride))
         return HAWK_ERR_ALIGN;
+    if (has_stray_bias(a->qk)) return HAWK_ERR_PARAM;
     RopeParams P = params_of(a->qk, dev_status);
     P.in[2] = a->v;
     P.in_row[2] = a->v_row_stride;
