@@ -77,13 +77,13 @@ def load_library() -> ctypes.CDLL:
         raise RuntimeError(
             f"{_LIB_PATH} is missing: build it with `python -m paper_2510_25739_b200.build` "
             "(or __graft_entry__.build()); there is no fallback path")
-    _load_marshal()
     _lib = _open(_LIB_PATH)
     return _lib
 
 
-def _load_marshal() -> None:
-    """Loads the extension that marshals the calls around the paged cache (built beside the library); raises if absent."""
+def _load_marshal():
+    """The extension that marshals the calls around the paged cache (built beside the library), loaded by the first of them: the
+    other calls do without it.  Raises if it is absent."""
     global _marshal
     if _marshal is None:
         if not _MARSHAL_PATH.exists():
@@ -92,6 +92,7 @@ def _load_marshal() -> None:
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         _marshal = module
+    return _marshal
 
 
 @contextlib.contextmanager
@@ -102,7 +103,6 @@ def alternate_library(path):
     if not Path(path).exists():
         raise RuntimeError(f"{path} is missing")
     saved = _lib
-    _load_marshal()
     _lib = _open(Path(path))
     try:
         yield _lib
@@ -551,8 +551,9 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], position:
     position int32 [T]; None for both: no rotation.  Weights and biases are [D], or [heads, D] one for each head; a bias goes with
     "layer" only."""
     lib = _lib or load_library()
-    rc, q_out, k_out = _marshal.qk_norm_rope(lib.address_qk_norm_rope, q, k, position, cos_sin, norm, eps, q_weight, k_weight,
-                                             q_bias, k_bias, interleaved, q_out, k_out, dev_status)
+    marshal = _marshal or _load_marshal()
+    rc, q_out, k_out = marshal.qk_norm_rope(lib.address_qk_norm_rope, q, k, position, cos_sin, norm, eps, q_weight, k_weight,
+                                            q_bias, k_bias, interleaved, q_out, k_out, dev_status)
     if rc != 0:
         raise HawkError(rc, "hawk_qk_norm_rope")
     return q_out, k_out
@@ -568,8 +569,9 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos
     and rotated as by qk_norm_rope; q [T,H,D] goes the same way into q_out, which is returned.  Stream s owns rows
     row_begin[s] .. row_begin[s+1]-1; kv_len [S] counts its keys with the new ones; block_table [S, pages a stream]."""
     lib = _lib or load_library()
-    rc, q_out = _marshal.rope_append(lib.address_rope_append, q, k, position, cos_sin, v, k_pages, v_pages, block_table, row_begin,
-                                     kv_len, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved, q_out, dev_status)
+    marshal = _marshal or _load_marshal()
+    rc, q_out = marshal.rope_append(lib.address_rope_append, q, k, position, cos_sin, v, k_pages, v_pages, block_table, row_begin,
+                                    kv_len, norm, eps, q_weight, k_weight, q_bias, k_bias, interleaved, q_out, dev_status)
     if rc != 0:
         raise HawkError(rc, "hawk_rope_append")
     return q_out
@@ -587,8 +589,9 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, bl
     max_new and max_kv bound the rows a stream brings and its keys.  With anc_mask (int64 tensor holding the uint64 masks,
     [max_new]) the rows of a stream are nodes of a candidate tree.  Rows of no stream are left as they are in `out`."""
     lib = _lib or load_library()
-    rc, out = _marshal.paged_attn(lib.address_paged_attn, lib.address_paged_attn_workspace_bytes, q, k_pages, v_pages, block_table,
-                                  row_begin, kv_len, max_new, max_kv, sm_scale, anc_mask, out, workspace, dev_status)
+    marshal = _marshal or _load_marshal()
+    rc, out = marshal.paged_attn(lib.address_paged_attn, lib.address_paged_attn_workspace_bytes, q, k_pages, v_pages, block_table,
+                                 row_begin, kv_len, max_new, max_kv, sm_scale, anc_mask, out, workspace, dev_status)
     if rc != 0:
         raise HawkError(rc, "hawk_paged_attn")
     return out
