@@ -91,6 +91,10 @@ def _load_marshal():
         spec = importlib.util.spec_from_file_location("_hawk_marshal", _MARSHAL_PATH)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
+        made_for = getattr(module, "torch_version", "of an earlier build")
+        if made_for != torch.__version__.split("+")[0]:  # (another ABI)
+            raise RuntimeError(f"{_MARSHAL_PATH} was built for torch {made_for}, this is {torch.__version__}: build it "
+                               "again with `python -m paper_2510_25739_b200.build`")
         _marshal = module
     return _marshal
 

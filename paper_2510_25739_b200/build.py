@@ -91,28 +91,34 @@ def build(force: bool = False, verbose: bool = False, lib: Path = LIB, objdir: P
 
 MARSHAL_SOURCE = CSRC / "hawk_marshal.cpp"
 MARSHAL_LIB = PKG / ("_hawk_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+MARSHAL_TAG = PKG / "_build" / "marshal.txt"  # what the extension was made with
 
 
 def build_marshal(force: bool = False) -> Path:
     """Compiles the Python extension that turns tensors into the argument structs of the calls around the paged cache (host
-    code only; links the torch libraries that the process has loaded anyway)."""
-    newest = max(MARSHAL_SOURCE.stat().st_mtime, (PKG.parent / "include" / "hawk.h").stat().st_mtime)
-    if not force and MARSHAL_LIB.exists() and MARSHAL_LIB.stat().st_mtime >= newest:
-        return MARSHAL_LIB
+    code only; links the torch libraries that the process has loaded anyway).  Another torch is another ABI: the extension is
+    rebuilt when the version or the command changes."""
     import torch
+    newest = max(MARSHAL_SOURCE.stat().st_mtime, (PKG.parent / "include" / "hawk.h").stat().st_mtime)
     root = Path(torch.__file__).resolve().parent
     cuda = Path(_nvcc()).resolve().parent.parent
     tmp = MARSHAL_LIB.with_suffix(f".{os.getpid()}.tmp")
     cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-fvisibility=hidden",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", sysconfig.get_paths()["include"],
            "-isystem", str(root / "include"), "-isystem", str(root / "include" / "torch" / "csrc" / "api" / "include"),
-           "-isystem", str(cuda / "include"), str(MARSHAL_SOURCE), "-o", str(tmp), "-L", str(root / "lib"),
+           "-isystem", str(cuda / "include"), str(MARSHAL_SOURCE), "-L", str(root / "lib"),
            "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    made_with = torch.__version__ + "\n" + " ".join(cmd)
+    if (not force and MARSHAL_LIB.exists() and MARSHAL_LIB.stat().st_mtime >= newest and MARSHAL_TAG.exists()
+            and MARSHAL_TAG.read_text() == made_with):
+        return MARSHAL_LIB
+    res = subprocess.run(cmd + ["-o", str(tmp)], capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError("g++ failed on " + MARSHAL_SOURCE.name)
     os.replace(tmp, MARSHAL_LIB)
+    MARSHAL_TAG.parent.mkdir(exist_ok=True)
+    MARSHAL_TAG.write_text(made_with)
     return MARSHAL_LIB
 
 

@@ -9,6 +9,7 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
 
 #include <optional>
 #include <string>
@@ -385,4 +386,12 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_hawk_marshal", nullptr, -1, m
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__hawk_marshal() { return PyModule_Create(&module_def); }
+PyMODINIT_FUNC PyInit__hawk_marshal()
+{
+    PyObject *m = PyModule_Create(&module_def);
+    if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) {  // whose tensors it can look into
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
