@@ -553,7 +553,7 @@ hawk_status hawk_rope_append(const hawk_rope_append_args *args, int32_t *dev_sta
  *              no initialisation; the size is for exactly these arguments (a smaller call may need more).  Calls
  *              that may overlap on the GPU need one each.
  * A page id outside [0, n_pages) reads as zeros and is flagged HAWK_DEV_BAD_PAGE.
- * Supported: D in {64, 128}; page_size a multiple of 8; S <= 4096; H a multiple of H_kv, H/H_kv <= 128.
+ * Supported: D in {64, 128}; page_size a multiple of 8; S <= 4096; max_kv <= 2^30; H a multiple of H_kv, H/H_kv <= 128.
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, PARAM, CUDA.  S == 0, T == 0 or max_new == 0 returns HAWK_OK
  * without a launch.
  * ---------------------------------------------------------------------------------------------- */

@@ -36,6 +36,7 @@ constexpr int kMinShareTiles = 2;    // shorter shares would only add partial re
 constexpr float kLazy = 8.f;         // log2 units by which a score may exceed the softmax shift
 constexpr int kStageBytes = 8192;
 constexpr int kMaxStreams = hawk_host::kPagedMaxStreams;
+constexpr int kMaxKv = 1 << 30;      // key positions, rounded up to tiles, stay 32-bit numbers (and no cache of one stream is longer)
 constexpr int kRecordInts = 8;       // start tile, tiles of the item, first row, rows, kv head, row chunk, total tiles, workers
 
 template <int D>
@@ -939,7 +940,7 @@ bool hawk_host::encode_pages(CUtensorMap *map, const hawk_paged_attn_args &a, bo
 extern "C" size_t hawk_paged_attn_workspace_bytes(int S, int T, int max_new, int H, int H_kv, int D, int max_kv)
 {
     if (S <= 0 || T <= 0 || max_new <= 0 || H <= 0 || H_kv <= 0 || H % H_kv != 0 || (D != 64 && D != 128) || max_kv < 0 ||
-        S > kMaxStreams || H / H_kv > 128)
+        max_kv > kMaxKv || S > kMaxStreams || H / H_kv > 128)
         return 0;
     if (max_new > T) max_new = T;
     const long long rows = static_cast<long long>(max_new) * (H / H_kv);
@@ -961,7 +962,7 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     if (!a.q || !a.k_pages || !a.v_pages || !a.block_table || !a.row_begin || !a.kv_len || !a.out) return HAWK_ERR_NULL;
     if (a.dtype != HAWK_BF16 && a.dtype != HAWK_F16) return HAWK_ERR_PARAM;
     if ((a.D != 64 && a.D != 128) || a.H < 1 || a.H_kv < 1 || a.H % a.H_kv != 0 || a.H / a.H_kv > 128 || a.page_size < 8 ||
-        a.page_size % 8 != 0 || a.S > kMaxStreams || (a.anc_mask && a.max_new > 64))
+        a.page_size % 8 != 0 || a.S > kMaxStreams || a.max_kv > kMaxKv || (a.anc_mask && a.max_new > 64))
         return HAWK_ERR_UNSUPPORTED;
     if (a.n_pages < 1 || a.max_kv > static_cast<long long>(a.table_width) * a.page_size) return HAWK_ERR_SHAPE;
     if (!(a.sm_scale > 0.f) || isinf(a.sm_scale)) return HAWK_ERR_PARAM;

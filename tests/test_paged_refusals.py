@@ -6,7 +6,7 @@ import pytest
 
 from oracle import paged
 from paper_2510_25739_b200 import binding, build
-from tests.test_paged_host import E_PARAM, P, _append, _qk
+from tests.test_paged_host import E_PARAM, E_UNSUP, P, _append, _attn, _qk
 
 NO_BIAS = dict(q_bias=None, k_bias=None)
 
@@ -36,3 +36,12 @@ def test_a_bias_beside_an_absent_tensor(lib):
 def test_the_plain_form_has_none_either():
     with pytest.raises(ValueError, match="no bias"):
         paged.norm_rope(np.ones((1, 1, 8)), None, None, "rms", 0.0, np.ones(8), np.ones(8))
+
+
+def test_key_counts_next_to_the_end_of_32_bits_are_refused(lib):
+    """Positions are rounded up to whole tiles in 32 bits: a bound of 2^31 - 1 keys would wrap."""
+    ws = lib.hawk_paged_attn_workspace_bytes
+    assert ws(128, 1024, 8, 20, 20, 64, 1 << 30) > 0
+    for max_kv in ((1 << 30) + 1, 2 ** 31 - 1):
+        assert ws(128, 1024, 8, 20, 20, 64, max_kv) == 0
+        assert lib.hawk_paged_attn(ctypes.byref(_attn(max_kv=max_kv, table_width=1 << 20, page_size=1 << 11)), None, None) == E_UNSUP
