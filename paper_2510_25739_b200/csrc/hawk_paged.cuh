@@ -23,6 +23,7 @@ struct PagedParams {
     const uint64_t *anc_mask;  // [max_new] or NULL
     float *part;               // partial results (layout: see each kernel)
     int32_t *records;          // rows kernel: one record of kRecordInts per worker
+    long long part_floats, record_ints;  // room in the two (for the index checks of the debug build)
     long long q_row_stride, q_head_stride;
     int S, T, max_new, H, H_kv, group;
     int n_pages, page_size, table_width;

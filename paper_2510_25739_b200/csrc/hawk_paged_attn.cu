@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
         cc.hk = item / cc.chunks;
         cc.chunk = item - cc.hk * cc.chunks;
     }
-    if (kShares && lane == 0) {
+    if (kShares && lane == 0 && HAWK_IN_BOUNDS(P.dev_status, (w + 1) * kRecordInts - 1, P.record_ints)) {
         int32_t *rec = P.records + static_cast<size_t>(w) * kRecordInts;
         *reinterpret_cast<int4 *>(rec) = make_int4(cc.tile, cc.nt, cc.r0, cc.n);
         *reinterpret_cast<int4 *>(rec + 4) = make_int4(cc.hk, cc.chunk, total, W);
@@ -369,6 +369,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
         float *ps = kGroup ? reinterpret_cast<float *>(ring)
                            : P.part + (static_cast<size_t>(w) * 2 + (seg_first ? 0 : 1)) * RPI * (D + 2);
         static_assert(!kGroup || RPI * (D + 2) * 4 <= kStages * kStageBytes, "a partial fits the ring");
+        if (!kGroup && !HAWK_IN_BOUNDS(P.dev_status, ps - P.part + RPI * (D + 2) - 1, P.part_floats)) return;
         if (kGroup && lane == 0) has_part[warp] = 1;
 #pragma unroll
         for (int nq = 0; nq < NQT; ++nq)
@@ -592,7 +593,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
     if (flags && lane == 0 && P.dev_status) atomicOr(P.dev_status, flags);
 
     if constexpr (kGroup) {
-        // ---- the four warps' partial results of the block's item, folded in share order from shared memory
+        // ---- the warps' partial results of the block's item, folded in share order from shared memory
         __syncthreads();
         if (head.n == 0) return;
         constexpr int PER = D / 32;
@@ -616,7 +617,9 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
                 for (int c = 0; c < PER; ++c) acc[c] = acc[c] * f_old + ps[r * D + lane * PER + c] * f_new;
             }
             const float inv = ll == 0.f ? 0.f : 1.f / ll;
-            T16 *dst = static_cast<T16 *>(P.out) + out_row(r, head.r0, kvh, c_row0) + lane * PER;
+            const long long o = out_row(r, head.r0, kvh, c_row0) + lane * PER;
+            T16 *dst = static_cast<T16 *>(P.out) + o;
+            if (!HAWK_IN_BOUNDS(P.dev_status, o, out_elems) || !HAWK_IN_BOUNDS(P.dev_status, o + PER - 1, out_elems)) continue;
 #pragma unroll
             for (int c = 0; c < PER; c += 2)
                 *reinterpret_cast<uint32_t *>(dst + c) = E::pack(acc[c] * inv, acc[c + 1] * inv);
@@ -1003,8 +1006,9 @@ extern "C" hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t
     P.block_table = a.block_table;
     P.anc_mask = a.anc_mask;
     P.records = static_cast<int32_t *>(a.workspace);
-    P.part = reinterpret_cast<float *>(P.records + static_cast<size_t>(hawk_host::kPagedSms) *
-                                                       (plan.shape == kShapeMid ? 1 : shares_warps(plan.rpi / 8)) * kRecordInts);
+    P.record_ints = static_cast<long long>(hawk_host::kPagedSms) * (plan.shape == kShapeMid ? 1 : shares_warps(plan.rpi / 8)) * kRecordInts;
+    P.part = reinterpret_cast<float *>(P.records + P.record_ints);
+    P.part_floats = static_cast<long long>(rows_ws / sizeof(float)) - P.record_ints;
     P.q_row_stride = a.q_row_stride;
     P.q_head_stride = a.q_head_stride;
     P.S = a.S;

@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         first.hk = loc / first.nt;
         first.tile = loc - first.hk * first.nt;
     }
-    if (tid == 0) {
+    if (tid == 0 && HAWK_IN_BOUNDS(P.dev_status, (w + 1) * 8 - 1, P.record_ints)) {
         int32_t *rec = P.records + static_cast<size_t>(w) * 8;
         *reinterpret_cast<int4 *>(rec) = make_int4(first.tile, first.nt, first.r0, first.n);
         *reinterpret_cast<int4 *>(rec + 4) = make_int4(first.hk, 0, total, W);
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok) break;
             tcgen05_fence_after();
             const int r = g * NH + lane;  // row of the item
-            const bool valid = lane < NH && r < n * P.group;
+            bool valid = lane < NH && r < n * P.group;
             uint32_t hd;
             const uint32_t pos = P.div_group.divmod(static_cast<uint32_t>(valid ? r : 0), hd);
             const uint32_t o_addr = lane_off + kO + ob * kOStride;
@@ -430,6 +430,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that has seen no key: zeros)
             T16 *dst = static_cast<T16 *>(P.out) + ((r0 + static_cast<long long>(pos)) * P.H + hk * P.group + static_cast<int>(hd)) * D;
             float *part = P.part + (static_cast<size_t>(w) * 2 + (item > 0 ? 1 : 0)) * 64 * (D + 2);
+            if (!whole && !HAWK_IN_BOUNDS(P.dev_status, part - P.part + 64 * (D + 2) - 1, P.part_floats)) valid = false;
             if (valid && !whole) *reinterpret_cast<float2 *>(part + 64 * D + 2 * r) = make_float2(m_smem[ob * 64 + g * 32 + lane], l);
 #pragma unroll
             for (int c0 = 0; c0 < D; c0 += 32) {

@@ -575,6 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             T16 *dst = static_cast<T16 *>(P.c.out) + (valid ? cell * D : 0);
             float *part = P.c.part + static_cast<size_t>(blockIdx.x) * C::kPartFloats;
             const int prow = (job.single ? 0 : t * kBM) + r;
+            if (P.n_split > 1 && !HAWK_IN_BOUNDS(P.c.dev_status, part - P.c.part + C::kPartFloats - 1, P.c.part_floats)) ok = false;
             if (P.n_split > 1 && valid && ok) *reinterpret_cast<float2 *>(part + 2 * kBM * D + 2 * prow) = make_float2(m_run, l_run);
             // (a split without keys has sum 0 and its o is not read)
             if (nt > 0 || P.n_split == 1) {
@@ -673,8 +674,11 @@ __global__ void __launch_bounds__(256) paged_tile_merge_kernel(const TileParams 
         }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    T16 *dst = static_cast<T16 *>(P.c.out) +
-               ((job.r0 + static_cast<long long>(pos)) * P.c.H + job.hk * P.c.group + static_cast<int>(hd)) * D + warp * PER * 4;
+    const long long at = ((job.r0 + static_cast<long long>(pos)) * P.c.H + job.hk * P.c.group + static_cast<int>(hd)) * D + warp * PER * 4;
+    T16 *dst = static_cast<T16 *>(P.c.out) + at;
+    if (!HAWK_IN_BOUNDS(P.c.dev_status, at, static_cast<long long>(P.c.T) * P.c.H * D) ||
+        !HAWK_IN_BOUNDS(P.c.dev_status, at + PER * 4 - 1, static_cast<long long>(P.c.T) * P.c.H * D))
+        return;
 #pragma unroll
     for (int c = 0; c < PER; ++c)
         *reinterpret_cast<uint2 *>(dst + 4 * c) =
@@ -757,6 +761,9 @@ cudaError_t hawk_host::launch_paged_tile(const hawk_paged_attn_args &a, const Pa
     P.c = base;
     P.groups = base.groups;
     P.c.part = part + static_cast<size_t>(p.pairs) * sizeof(PagedGroup) / sizeof(float);
+    P.c.part_floats = p.n_split == 1 ? 0
+                                     : static_cast<long long>(p.pairs) * a.H_kv * p.n_split *
+                                           (a.D == 64 ? TileCfg<64>::kPartFloats : TileCfg<128>::kPartFloats);
     P.tok = p.tok;
     P.q_rows = p.tok * base.group;
     P.n_split = p.n_split;
