@@ -8,6 +8,7 @@
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
 
@@ -274,15 +275,16 @@ void pages_and_batch(Args &a, const Where &w, PyObject *k_pages, PyObject *v_pag
     a.kv_len = static_cast<const int32_t *>(dense(tensor(kv_len, "kv_len"), "kv_len", at::kInt, {S}, w.index));
 }
 
-// A C++ or Python error inside becomes a Python error; nothing leaves through the C boundary.
+// A C++ or Python error inside becomes the Python error that torch has for it (torch.OutOfMemoryError of an allocation among
+// them); nothing leaves through the C boundary.
 template <class F>
 PyObject *guarded(F &&f)
 {
     try {
         return f();
     } catch (const Refused &) {
-    } catch (const std::exception &e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        torch::translate_exception_to_python(std::current_exception());
     }
     return nullptr;
 }
