@@ -160,8 +160,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t *tmem_ptr = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_ptr + 1);
     int *wsum = reinterpret_cast<int *>(tmem_ptr + 2);  // [16]
-    int *prefix = wsum + 16;                            // [S + 1]
-    static_assert(2 * 64 * 4 + 3 * 64 * 4 + 768 * 4 + 64 * 8 + (2 * C::kStages + 17) * 8 + 8 + 64 <= C::kSmallBytes, "");
+    int *any_far = wsum + 16;                           // [2 groups]: some row's shift is (see kFarShift)
+    int *prefix = any_far + 2;                          // [S + 1]
+    static_assert(2 * 64 * 4 + 3 * 64 * 4 + 768 * 4 + 64 * 8 + (2 * C::kStages + 17) * 8 + 8 + 64 + 8 <= C::kSmallBytes, "");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -488,6 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     masks[g * 32 + key] = m;
                     m_smem[ob * 64 + g * 32 + key] = -CUDART_INF_F;
+                    any_far[g] = 0;
                     shift[g * 32 + key] = r < c.n * P.group ? kNoShift : -CUDART_INF_F;
                 }
 #pragma unroll
@@ -547,8 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (lane == r) mine = v;
                 }
                 wmax[(g * 4 + wg) * 32 + lane] = mine;
-                // (a row's maximum is far only if some warp's is)
-                far = group_any(bar_id, far || (lane < NH && g * NH + lane < c.n * P.group && is_far(mine, P.scale_log2)));
+                group_sync(bar_id);
                 if (key < NH) {
                     const float *wm = wmax + g * 128 + key;
                     const float m_old = m_smem[ob * 64 + g * 32 + key];
@@ -556,11 +557,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const bool none = m_new == -CUDART_INF_F;
                     const float sh = none ? kNoShift : -m_new * P.scale_log2;
                     m_smem[ob * 64 + g * 32 + key] = m_new;
-                    if (g * NH + key < c.n * P.group) shift[g * 32 + key] = sh;
+                    if (g * NH + key < c.n * P.group) {
+                        shift[g * 32 + key] = sh;
+                        if (is_far(m_new, P.scale_log2)) any_far[g] = 1;
+                    }
                     lost[g * 32 + key] = none ? 0.f : -fmaf(m_new, P.scale_log2, sh);
                     alpha[g * 32 + key] = none ? 1.f : fast_exp2((m_old - m_new) * P.scale_log2);
                 }
                 group_sync(bar_id);
+                far = any_far[g] != 0;  // (until the item ends)
 #pragma unroll
                 for (int r2 = 0; r2 < NH / 2; ++r2) {
                     const float2 a2 = *reinterpret_cast<const float2 *>(alpha + g * 32 + 2 * r2);
