@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             m_run = m_new;
         };
-        auto exponentials = [&](auto argument) {  // the tile's probabilities, handed over in halves, and their sum
+        auto exponentials = [&](uint64_t shift2) {  // the tile's probabilities, handed over in halves, and their sum
             uint64_t sum_a = 0, sum_b = 0;        // (two zeros each)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -487,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
                     const int q = half * 2 + (c >> 4), e = (2 * c) & 31;
-                    const uint64_t x2 = argument(pack2(__uint_as_float(u[q][e]), __uint_as_float(u[q][e + 1])));
+                    const uint64_t x2 = fma2(pack2(__uint_as_float(u[q][e]), __uint_as_float(u[q][e + 1])), scale2, shift2);
                     float2 p;
                     if (D == 64 && c % 4 == 3) {
                         p = exp2_fma(x2);
@@ -509,6 +509,45 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float2 sums2 = unpack2(add2(sum_a, sum_b));
             l_run += sums2.x + sums2.y;
         };
+        // The same for far shifts (see kFarShift), differences first.  A small loop over 32 columns that takes the scores from tensor
+        // memory again (a part's probabilities go over scores that it has read): as long as the loop above, its code alone cost jobs
+        // of few tiles 5 %.
+        auto far_exponentials = [&](int i) {
+            const int seen = limit - (first + i * stride) * kBN;
+            const float minus = m_run == -CUDART_INF_F ? 0.f : -m_run;
+            const uint64_t minus2 = pack2(minus, minus);
+            uint64_t sum = 0;
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+                uint32_t w[32], pk[16];
+                __syncwarp();
+                tmem_ld_32x32(s_addr + q * 32, w);
+                tmem_ld_wait();
+                const int left = seen - q * 32;
+                const uint32_t open = P.c.anc_mask ? tree_word(-left, nodes) : left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
+#pragma unroll
+                for (int c = 0; c < 32; ++c)
+                    if (!(open >> c & 1u)) w[c] = 0xff800000u;
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    float2 p = unpack2(mul2(add2(pack2(__uint_as_float(w[2 * c]), __uint_as_float(w[2 * c + 1])), minus2), scale2));
+                    p.x = fast_exp2(p.x);
+                    p.y = fast_exp2(p.y);
+                    sum = add2(sum, pack2(p.x, p.y));
+                    pk[c] = E::pack(p.x, p.y);
+                }
+                __syncwarp();
+                tmem_st_32x16(s_addr + q * 16, pk);
+                tmem_st_wait();
+                if (q & 1) {
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_ready[2 * t + (q >> 1)]);
+                }
+            }
+            const float2 sums2 = unpack2(sum);
+            l_run += sums2.x + sums2.y;
+        };
         // what the fma adds to a row's scores: minus the shift, or for a row without one so much that any score is too high (-inf stays
         // -inf)
         constexpr float kNoShift = 3e38f;
@@ -519,18 +558,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (__any_sync(0xffffffffu, valid && fmaf(m_new, P.c.scale_log2, sh) > 8.f)) {
                 renew(i);
                 sh = m_run == -CUDART_INF_F ? kNoShift : -m_run * P.c.scale_log2;
-                // far shifts (see kFarShift) are renewed at every tile, so that the loop's usual way knows nothing of them (a flag in
-                // it cost the prefill 2 % at D = 128 and 5 % at D = 64; this way nothing)
+                // far shifts are renewed at every tile, so that the loop's usual way knows nothing of them (a flag in it cost the
+                // prefill 2 % at D = 128 and 5 % at D = 64; this way 0 and 1)
                 if (__any_sync(0xffffffffu, valid && is_far(m_run, P.c.scale_log2))) {
-                    const float minus = m_run == -CUDART_INF_F ? 0.f : -m_run;
-                    const uint64_t minus2 = pack2(minus, minus);
-                    exponentials([&](uint64_t s) { return mul2(add2(s, minus2), scale2); });
+                    far_exponentials(i);
                     sh = kNoShift;  // (so that the next tile comes here again)
                     continue;
                 }
             }
-            const uint64_t shift2 = pack2(sh, sh);
-            exponentials([&](uint64_t s) { return fma2(s, scale2, shift2); });
+            exponentials(pack2(sh, sh));
         }
         if (ok && nt > 0) ok = warp_wait(&o_done[t], 0, abort_flag);
         if (ok && job.single && job.tiles > 1) ok = warp_wait(&o_done[t ^ 1], 0, abort_flag);  // (Q is free then)
