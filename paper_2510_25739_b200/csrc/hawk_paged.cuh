@@ -1,4 +1,4 @@
-// What the two kernels behind hawk_paged_attn share: the call's parameters, the view of one stream of the ragged batch,
+// What the three kernels behind hawk_paged_attn share: the call's parameters, the view of one stream of the ragged batch,
 // the 16-bit element types, and the launchers.
 #pragma once
 

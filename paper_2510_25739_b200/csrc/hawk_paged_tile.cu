@@ -20,7 +20,8 @@
 // is computed on the FMA pipe instead, 2^x = 2^n 2^f with n the nearest integer and a degree-4 polynomial for 2^f on
 // [-1/2, 1/2] (least squares on Chebyshev points, relative error 2.6e-6); 4 x 2048 rows over 8192 keys, 32 heads sharing 8: 726 to
 // 702 us.  At D = 128 it gains nothing (790 against 794).
-// Measured there: 1217 TFLOP/s at D = 128, 0.73 of the measured burst peak.  What it took: MMAs issued under a predicate with
+// Measured there in a graph of back-to-back calls: 1.2 PFLOP/s at D = 128, 0.72 of the measured burst peak (called alone 931 us,
+// 1.03 PFLOP/s).  What it took: MMAs issued under a predicate with
 // descriptors stepped by their low word (980 to 790 us; see umma_f16_ss_if).  Two score buffers of 64 keys a slot, so that the next
 // scores never wait for P V, came to 916 us: products of 64 columns read Q from shared memory twice as often.
 // Jobs come from a list that one extra block of the rows kernel (which every call launches before this one) makes: a block reads
