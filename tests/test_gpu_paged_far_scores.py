@@ -130,3 +130,68 @@ def test_a_far_row_beside_ordinary_ones(D):
                                       b.kv_len.numpy(), D ** -0.5)
         got[row] = want[row]
         _compare(got, want, size, b.dt)
+
+
+def _keys(b, major, minor):
+    """Keys of b such that key j of stream s scores (before the scale) 16 * 2^15 major(s, j) + 2^15 minor(s, j)."""
+    q = torch.zeros(b.D)
+    q[:16] = q[18] = 2.0 ** 15
+    b.q = q.expand(b.T, b.H, b.D).to(b.dt)
+    for s, kv in enumerate(b.kv):
+        for j in range(b.need[s]):
+            for row in range(min(b.page, kv - j * b.page)):
+                k = torch.zeros(b.D)
+                k[:16], k[18] = major(s, j * b.page + row), minor(s, j * b.page + row)
+                b.k_pages[int(b.block_table[s, j]), :, row] = k.to(b.dt)
+                assert (b.k_pages[int(b.block_table[s, j]), 0, row].float() == k).all()
+    return b
+
+
+@pytest.mark.parametrize("up", [True, False])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: s[0])
+def test_from_far_to_near_and_back(shape, up):
+    """The first half of a stream's keys score -4 * 10^9 and the second around 0 (weights of 1 to 2^-16 among them), or around 0 and
+    then 4 * 10^9: shifts cross the bound between the two ways in the middle of an item.  (fp32 numbers next to 2^32 lie 2^9 apart:
+    steps of 4 there would not be exact, those of 2^10 are.)"""
+    _, new, kv, H, H_kv, D = shape
+    b = Batch(new, kv, H, H_kv, D, 16, seed=102, back=3)
+    rng = np.random.default_rng(9)
+    t = rng.integers(-15, 1, max(kv) + 1)
+    step = 2.0 ** -13  # 4 units of a score, 0.7 in the exponent
+
+    def major(s, j):
+        return (0.0 if j >= b.kv[s] // 2 else -2.0 ** 13) if up else (0.0 if j < b.kv[s] // 2 else 2.0 ** 13)
+
+    _check(_keys(b, major, lambda s, j: float(t[j]) * step * (256 if major(s, j) else 1)))
+
+
+@pytest.mark.parametrize("scale,magnitude", [(2.0 ** -18, 2.0 ** 12), (40.0, 2.0 ** 12), (1e-30, 2.0 ** 14), (3.0, 2.0 ** -11)])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: s[0])
+def test_scales(shape, scale, magnitude):
+    """Other factors than D^-1/2: scores that are large before it and small behind, the other way round, and all alike behind it (where it
+    does not matter that 2^33 + 2^8 t is not an fp32 number; the others are)."""
+    import paper_2510_25739_b200 as hawk
+    _, new, kv, H, H_kv, D = shape
+    b = Batch(new, kv, H, H_kv, D, 16, seed=103, back=3)
+    t = np.random.default_rng(10).integers(0, 32, max(kv) + 1)
+    _keys(b, lambda s, j: magnitude, lambda s, j: float(t[j]) * 2.0 ** -7)
+    d = b.cuda()
+    out = torch.full((b.T, H * D), 7.0, dtype=b.dt, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    hawk.paged_attn(d.q, d.k_pages, d.v_pages, d.block_table, d.row_begin, d.kv_len, b.max_new, b.max_kv, scale, out=out, dev_status=status)
+    want, size = paged.paged_attn(f64(b.q), f64(b.k_pages), f64(b.v_pages), b.block_table.numpy(), b.row_begin.numpy(),
+                                  b.kv_len.numpy(), scale)
+    assert int(status.item()) == 0
+    _compare(f64(out).reshape(b.T, H, D), want, size, b.dt)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,kv", [([5, 9], [3, 0]), ([20, 12, 5], [9, 2000, 1]), ([60, 41], [50, 2000]), ([130, 90], [100, 0])])
+def test_rows_that_see_nothing_beside_far_ones(new, kv, D):
+    """Fewer keys than rows: the first rows see none and give zeros, the others' scores are far."""
+    b = _far(Batch(new, kv, 2, 2, D, 16, seed=104), "shuffled", -1)
+    _check(b)
+    got, _ = _run(b)
+    for s, (n, l) in enumerate(zip(new, kv)):
+        r0 = int(b.row_begin[s])
+        assert (got[r0:r0 + max(0, n - l)] == 0).all()
