@@ -216,8 +216,9 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 4 ? 3 : 1)
                 c.chunk = 0;
                 if (++c.hk == P.H_kv) {
                     c.hk = 0;
-                    do ++c.s;
-                    while (prefix[c.s + 1] == prefix[c.s]);  // (ends: tiles are left)
+                    // (tiles are left, so a stream with some follows; the bound holds even if the lengths change under the call)
+                    do c.s = min(c.s + 1, P.S - 1);
+                    while (c.s < P.S - 1 && prefix[c.s + 1] == prefix[c.s]);
                     enter_stream<D, RPI>(c, P, flags);
                 }
             }

@@ -82,8 +82,9 @@ __device__ __forceinline__ void advance(Cursor &c, const PagedParams &P, const i
         c.tile = 0;
         if (++c.hk == P.H_kv) {
             c.hk = 0;
-            do ++c.s;
-            while (prefix[c.s + 1] == prefix[c.s]);  // (ends: tiles are left)
+            // (tiles are left, so a stream with some follows; the bound holds even if the lengths change under the call)
+            do c.s = min(c.s + 1, P.S - 1);
+            while (c.s < P.S - 1 && prefix[c.s + 1] == prefix[c.s]);
             enter_stream(c, P, flags);
         }
     }
