@@ -13,7 +13,11 @@
  *   hawk_spec_cache_*, hawk_pool_*  the cache of vertical predictions and the sampling pool that feed it;
  *   hawk_head_proj_cfg, hawk_*_accept_guided  the head with the guidance combine in its epilogue;
  *   hawk_qk_norm_rope, hawk_rope_append, hawk_paged_attn  what surrounds the attention when the cache is paged:
- *                     norm and rotation of the heads, writing the new rows, attention of a chunk of them.
+ *                     norm and rotation of the heads, writing the new rows, attention of a chunk of them;
+ *   hawk_sample       a token from a row of logits (guidance, temperature, top-k, top-p, min-p), for steps without drafts
+ *                     and for the draft side, whose distributions the verification reads;
+ *   hawk_pages_*      the paged cache between two steps: streams grow, are cut, forked and freed, pages are copied and
+ *                     packed, the rows of an accepted path move to the front.
  *
  * Conventions common to all entry points
  *   - Every pointer is a DEVICE pointer owned by the caller unless the comment says "host".  The
@@ -62,6 +66,8 @@ typedef enum {
 #define HAWK_DEV_BAD_ROWS 64  /* row_begin does not cut the new rows into streams as the call says; the stream was skipped */
 #define HAWK_DEV_BAD_PAGE 128 /* a page id lay outside [0, n_pages)                             */
 #define HAWK_DEV_BAD_POSITION 256 /* a rotation position lay outside [0, n_positions) and was clamped */
+#define HAWK_DEV_NO_PAGES 512 /* more pages were needed than are free; streams that found none stay as they were */
+#define HAWK_DEV_BAD_SETTING 1024 /* a row's temperature, top_p or min_p was no usable number and taken as off */
 #define HAWK_DEV_BOUNDS 32    /* libraries built with -DHAWK_DEBUG only: an index lay outside its array, the access was skipped */
 
 const char *hawk_status_string(hawk_status status);
@@ -576,6 +582,183 @@ typedef struct hawk_paged_attn_args {
 size_t hawk_paged_attn_workspace_bytes(int S, int T, int max_new, int H, int H_kv, int D, int max_kv);
 
 hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t *dev_status, hawk_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hawk_sample - one token from every row of logits, by given random numbers.
+ *
+ * The plain step beside the verification (Sec. 5 gives its settings: guidance, temperature, top-k): the first token behind a
+ * prompt, streams without drafts, and the draft side, which draws its tokens and hands hawk_cfg_accept and hawk_tree_accept the
+ * distributions they were drawn from (`probs`, laid out as their q_probs).
+ *
+ * Operation, per row r over the ids v_begin <= v < v_end:
+ *   1. l[v] = lu[v] + cfg_scale*(lc[v] - lu[v]) in fp32 (subtract, fused multiply-add; -inf in either gives -inf), or the logit itself
+ *      without guidance.  NaN and +inf count as -inf and are flagged HAWK_DEV_NONFINITE.
+ *   2. top-k, 0 < top_k: ids below the top_k-th largest l leave; ties with it stay (as in hawk_cfg_accept).
+ *   3. w[v] = exp((l[v] - max l) / temperature), 0 for ids that left.  top-p, top_p < 1: with t the largest value for which
+ *      the w of all l >= t sum to at least top_p times the sum of all w, ids below t leave; ties with t stay.
+ *   4. min-p, 0 < min_p: ids with exp((l - max l) / temperature) < min_p leave; the maximum always stays.
+ *   5. token = the smallest id whose running sum of w (ascending id) exceeds u * sum(w); p = w / sum(w).
+ * temperature 0: the lowest id of the maximum, with p = 1; steps 2 to 5 have no say.  A row without a finite logit: token -1, p = 0.
+ * Exponentials are taken in fp64 and held as whole multiples of 2^-44 of the largest, sums of them in 64-bit integers: no order
+ * changes a sum, so equal inputs give equal tokens whatever the launch (a w below 2^-45 counts as 0).
+ *
+ *   dtype        HAWK_F32, HAWK_BF16 or HAWK_F16: the logits' type
+ *   logits       [R][V] at row_stride (elements, not negative; 0: all rows draw from one; any alignment that the type needs)
+ *   uncond       the same at uncond_row_stride: the unconditional rows; NULL: no guidance
+ *   temperature, top_k, top_p, min_p, cfg_scale      for all rows; top_k <= 0, top_p >= 1 and min_p <= 0 are off
+ *   row_temperature, row_top_k, row_top_p, row_min_p, row_cfg_scale   device [R] or NULL: take the place of the number above.
+ *                A row's NaN, or a temperature that is negative or infinite, is flagged HAWK_DEV_BAD_SETTING and taken as off
+ *                (temperature 1).  row_cfg_scale is used as it is.
+ *   u            fp32 [R], uniforms in [0,1); others are clamped into it
+ *   token        int32 [R] (out)
+ *   token_prob   fp32 [R] (out) or NULL: p of the token
+ *   probs        fp32 [R][V] at probs_row_stride (out) or NULL: p, 0 outside the range
+ * Supported: 1 <= v_end - v_begin <= 262144.  No workspace.
+ * Errors: NULL, SHAPE (a range outside [0, V], a negative stride, rows of probs that overlap), ALIGN (a base that its type cannot have), UNSUPPORTED,
+ * PARAM (dtype; a temperature that is negative or not finite, a NaN), CUDA.  R == 0 returns HAWK_OK without a launch.
+ * ---------------------------------------------------------------------------------------------- */
+#define HAWK_F32 2
+
+typedef struct hawk_sample_args {
+    int dtype, R, V, v_begin, v_end, top_k;
+    float temperature, top_p, min_p, cfg_scale;
+    const void *logits, *uncond;
+    long long row_stride, uncond_row_stride;
+    const float *row_temperature, *row_top_p, *row_min_p, *row_cfg_scale;
+    const int32_t *row_top_k;
+    const float *u;
+    int32_t *token;
+    float *token_prob, *probs;
+    long long probs_row_stride;
+} hawk_sample_args;
+
+hawk_status hawk_sample(const hawk_sample_args *args, int32_t *dev_status, hawk_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hawk_pages_* - the paged cache between two steps.
+ *
+ * State of a cache, in device memory and the caller's:
+ *   block_table  int32 [S][table_width] and kv_len int32 [S], as for hawk_paged_attn: stream s uses its first
+ *                ceil(kv_len[s] / page_size) entries; the others may hold anything and are not written
+ *   page_refs    int32 [n_pages]: table entries in use that name the page.  0: the page is free.  A caller keeps a page out of use, or
+ *                holds a prompt that no stream uses at the moment, by a count of its own on top.
+ * The calls below work on the state alone, once for all layers, and say which pages have to be copied:
+ *   copies       int32 [.][3]: page to copy from, page to copy to, rows (the first ones); -1, -1, 0: nothing
+ * hawk_pages_copy does that for the pages of all layers, and hawk_pages_keep moves rows inside them.  Every out_* may be the tensor it
+ * comes from (in place) unless the call says otherwise; tensors that overlap in part are not supported.  What is counted in this
+ * section is whole numbers; results do not depend on the launch.
+ * Lengths outside [0, table_width * page_size] are flagged HAWK_DEV_BAD_PREFIX and their streams stay as they are; a page id outside
+ * [0, n_pages) is flagged HAWK_DEV_BAD_PAGE and nothing is counted for it.
+ * Supported: S <= 4096, n_pages <= 2^20, page_size <= 65536, S * table_width and table_width * page_size + 65536 below 2^31.
+ * page_refs, out_refs, workspaces and pages are 16-byte aligned, the other tensors as their type is.
+ *
+ * hawk_pages_resize: stream s goes from kv_len[s] to new_len[s] keys.
+ *   1. Streams that shrink release the entries they need no more (to 0: the stream is freed).  A count that is 0 already stays 0,
+ *      HAWK_DEV_BAD_PAGE.
+ *   2. A stream that grows takes ceil(new/page_size) - ceil(old/page_size) pages; and one more if its last page is partly filled and,
+ *      after step 1, named by other entries too: it gets a copy of its own, copies[s] = (shared page, new page, old % page_size), and
+ *      releases the shared one (all streams that grow into a shared page do, the last of them as well).
+ *      Pages are those that are free after step 1, lowest id first, to streams in ascending order, each stream's entries in ascending
+ *      order (the copy's is the first).
+ *   3. When the pages run out, the streams from there on that need any stay as they were, HAWK_DEV_NO_PAGES.
+ *   out_len[s] = new_len[s], or kv_len[s] for a stream that stayed.  out_table gets the entries that are then in use.
+ *   new_len may be out_len.  Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, CUDA.  S == 0: out_refs is copied.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct hawk_pages_resize_args {
+    int S, table_width, n_pages, page_size;
+    const int32_t *block_table, *kv_len, *new_len, *page_refs;
+    int32_t *out_table, *out_len, *out_refs;
+    int32_t *copies; /* [S][3] */
+} hawk_pages_resize_args;
+
+hawk_status hawk_pages_resize(const hawk_pages_resize_args *args, int32_t *dev_status, hawk_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hawk_pages_fork - streams that continue others: out stream t has the first min(length[t], kv_len[p]) keys of stream p = parent[t]
+ * (length NULL: all), none for p = -1.  Pages are shared: out_table[t] names the parent's, and out_refs = page_refs less the entries in
+ * use of the S old streams plus those of the S_out new ones, whatever that gives.  So one call reorders a batch, has several streams go on from one, keeps some and
+ * frees others.  hawk_pages_resize makes the copy when one of them grows into a shared page.
+ * A parent outside [-1, S) is flagged HAWK_DEV_BAD_ROWS and taken as -1; a negative length counts as 0 and is flagged HAWK_DEV_BAD_PREFIX; a
+ * stream whose kv_len is out of range has no entries.
+ *   parent     int32 [S_out], length int32 [S_out] or NULL
+ *   out_table  int32 [S_out][table_width], out_len int32 [S_out]: not block_table and kv_len (PARAM)
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, PARAM, CUDA.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct hawk_pages_fork_args {
+    int S, S_out, table_width, n_pages, page_size;
+    const int32_t *block_table, *kv_len, *page_refs, *parent, *length;
+    int32_t *out_table, *out_len, *out_refs;
+} hawk_pages_fork_args;
+
+hawk_status hawk_pages_fork(const hawk_pages_fork_args *args, int32_t *dev_status, hawk_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hawk_pages_compact - pages in use to the lowest ids, at most max_moves of them a call: with f_0 < f_1 < ... the free pages and
+ * u_0 > u_1 > ... the pages in use, all from first_page on, page u_i becomes page f_i for as long as f_i < u_i and i < max_moves.
+ *   copies     int32 [max_moves][3]: copies[i] = (u_i, f_i, page_size)
+ *   out_table  the table with the new ids, out_refs the counts that moved with them
+ *   top        int32 [1] or NULL: all pages from this id on are free then (at least first_page)
+ *   workspace  at least hawk_pages_compact_workspace_bytes(n_pages, max_moves) bytes, 16-byte aligned, no initialisation; calls that may
+ *              overlap on the GPU need one each
+ * A page that the caller holds by a count of its own moves like the others (copies tell where).
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, CUDA.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct hawk_pages_compact_args {
+    int S, table_width, n_pages, page_size, first_page, max_moves;
+    const int32_t *block_table, *kv_len, *page_refs;
+    int32_t *out_table, *out_refs;
+    int32_t *copies; /* [max_moves][3] */
+    int32_t *top;
+    void *workspace;
+    size_t workspace_bytes;
+} hawk_pages_compact_args;
+
+size_t hawk_pages_compact_workspace_bytes(int n_pages, int max_moves);
+
+hawk_status hawk_pages_compact(const hawk_pages_compact_args *args, int32_t *dev_status, hawk_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * hawk_pages_copy - rows of pages to other pages, keys and values of all layers: for each of the n_copies entries (a, b, n) of
+ * `copies` with a >= 0, rows 0 .. n-1 of page a to page b (n is clamped to [0, page_size]).  No page may be written by two
+ * entries, or written by one and read by another (what the calls above give never is).  An id outside [0, n_pages) skips the
+ * entry, HAWK_DEV_BAD_PAGE.
+ *   k_pages, v_pages   16-bit, element (layer, page, head, row, d) at layer * layer_stride + page * page_stride +
+ *                      head * head_stride + row * row_stride + d (strides in elements, multiples of 8; bases 16-byte aligned)
+ * Supported: D a multiple of 8; page_size, H_kv and D at most 65536, H_kv * page_size * D <= 2^30; layers <= 32767.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, CUDA.  n_copies == 0 or layers == 0 returns HAWK_OK without a launch.
+ *
+ * hawk_pages_keep - the rows of an accepted path to the front of their block, and the length that the stream then has.  Stream s
+ * has brought n_s rows (row_begin, kv_len: the batch of hawk_paged_attn, its keys at cache rows base = kv_len[s] - n_s on), and
+ * a_s = accept_len[s % B] of them were accepted behind the first `first` rows, which stay: with path, row base + path[s % B][i] moves to
+ * row base + first + i for i < a_s, and out_len[s] = base + min(n_s, first + a_s).
+ * first = 1 and path, accept_len are what hawk_tree_accept gives for streams b and B + b of sequence b, whose row 0 is the root.  Without
+ * path (NULL: a chain, whose rows lie in order) nothing moves, the page arguments are not looked at, and only out_len is written.
+ * The path has to ascend, from `first` on and below n_s, as the nodes of a tree do; a stream whose path does not, or whose accept_len lies
+ * outside [0, path_width] (without path: is negative), stays as it was with out_len = kv_len, HAWK_DEV_BAD_TREE.  An idle stream (n_s = 0)
+ * stays as well.  A stream whose rows or length contradict the batch is flagged HAWK_DEV_BAD_ROWS or HAWK_DEV_BAD_PREFIX and stays; a row
+ * with a page id outside [0, n_pages) on either side is skipped, HAWK_DEV_BAD_PAGE.  The rows that move lie in pages of their stream alone
+ * (hawk_pages_resize sees to that when it makes room for them).
+ *   path  int32 [B][path_width] or NULL, accept_len int32 [B], S a multiple of B; out_len int32 [S], not kv_len (PARAM)
+ * Limits of the pages as above.  Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, PARAM, CUDA.  S == 0 returns HAWK_OK without a launch.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct hawk_page_tensors {
+    int layers, n_pages, H_kv, page_size, D;
+    void *k_pages, *v_pages;
+    long long k_layer_stride, k_page_stride, k_head_stride, k_row_stride;
+    long long v_layer_stride, v_page_stride, v_head_stride, v_row_stride;
+} hawk_page_tensors;
+
+hawk_status hawk_pages_copy(const hawk_page_tensors *pages, const int32_t *copies, int n_copies, int32_t *dev_status,
+                            hawk_stream_t stream);
+
+typedef struct hawk_pages_keep_args {
+    hawk_page_tensors pages;
+    int S, B, table_width, path_width, first;
+    const int32_t *block_table, *row_begin, *kv_len, *path, *accept_len;
+    int32_t *out_len;
+} hawk_pages_keep_args;
+
+hawk_status hawk_pages_keep(const hawk_pages_keep_args *args, int32_t *dev_status, hawk_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -17,6 +17,7 @@ _BINDING_NAMES = (
     "pool_build", "pool_sample", "pool_sample_workspace_bytes",
     "head_proj_cfg", "cfg_accept_guided", "tree_accept_guided",
     "qk_norm_rope", "rope_append", "paged_attn", "paged_attn_workspace_bytes",
+    "sample", "pages_resize", "pages_fork", "pages_compact", "pages_compact_workspace_bytes", "pages_copy", "pages_keep",
 )
 
 

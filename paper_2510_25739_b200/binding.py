@@ -12,7 +12,7 @@ import ctypes
 import importlib.util
 import sysconfig
 from pathlib import Path
-from typing import Optional
+from typing import Optional, Union
 
 import torch
 
@@ -24,6 +24,7 @@ _marshal = None
 
 DEV_TIMEOUT, DEV_BAD_DRAFT, DEV_NONFINITE, DEV_BAD_PREFIX, DEV_BAD_TREE, DEV_BOUNDS = 1, 2, 4, 8, 16, 32
 DEV_BAD_ROWS, DEV_BAD_PAGE, DEV_BAD_POSITION = 64, 128, 256
+DEV_NO_PAGES, DEV_BAD_SETTING = 512, 1024
 
 EXPORTS = (
     "hawk_status_string", "hawk_version",
@@ -37,6 +38,8 @@ EXPORTS = (
     "hawk_pool_build", "hawk_pool_sample_workspace_bytes", "hawk_pool_sample",
     "hawk_head_proj_cfg", "hawk_cfg_accept_guided", "hawk_tree_accept_guided",
     "hawk_qk_norm_rope", "hawk_rope_append", "hawk_paged_attn_workspace_bytes", "hawk_paged_attn",
+    "hawk_sample", "hawk_pages_resize", "hawk_pages_fork", "hawk_pages_compact_workspace_bytes", "hawk_pages_compact",
+    "hawk_pages_copy", "hawk_pages_keep",
 )
 
 
@@ -164,14 +167,20 @@ def _open(path: Path) -> ctypes.CDLL:
     lib.hawk_pool_sample_workspace_bytes.argtypes = [i32, i32]
     lib.hawk_pool_sample.restype = i32
     lib.hawk_pool_sample.argtypes = [vp] * 4 + [i32] * 6 + [vp, sz, vp, vp]
-    for name in ("hawk_qk_norm_rope", "hawk_rope_append", "hawk_paged_attn"):  # (argument struct, status word, stream)
+    for name in ("hawk_qk_norm_rope", "hawk_rope_append", "hawk_paged_attn", "hawk_sample", "hawk_pages_resize", "hawk_pages_fork",
+                 "hawk_pages_compact", "hawk_pages_keep"):  # (argument struct, status word, stream)
         getattr(lib, name).restype = i32
         getattr(lib, name).argtypes = [vp, vp, vp]
+    lib.hawk_pages_compact_workspace_bytes.restype = sz
+    lib.hawk_pages_compact_workspace_bytes.argtypes = [i32, i32]
+    lib.hawk_pages_copy.restype = i32
+    lib.hawk_pages_copy.argtypes = [vp, vp, i32, vp, vp]
     lib.hawk_paged_attn_workspace_bytes.restype = sz
     lib.hawk_paged_attn_workspace_bytes.argtypes = [i32] * 7
     lib.hawk_verify_step_host.restype = i32
     lib.hawk_verify_step_host.argtypes = [ctypes.POINTER(StepHostArgs), vp]
-    for name in ("qk_norm_rope", "rope_append", "paged_attn", "paged_attn_workspace_bytes"):  # for the marshalling extension
+    for name in ("qk_norm_rope", "rope_append", "paged_attn", "paged_attn_workspace_bytes", "sample", "pages_resize", "pages_fork",
+                 "pages_compact", "pages_compact_workspace_bytes", "pages_copy", "pages_keep"):  # for the marshalling extension
         setattr(lib, "address_" + name, ctypes.cast(getattr(lib, "hawk_" + name), vp).value)
     return lib
 
@@ -599,6 +608,103 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, bl
     if rc != 0:
         raise HawkError(rc, "hawk_paged_attn")
     return out
+
+
+Setting = Union[float, torch.Tensor]
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Setting = 1.0, top_k: Union[int, torch.Tensor] = 0,
+           top_p: Setting = 1.0, min_p: Setting = 0.0, cfg_scale: Optional[Setting] = None, v_begin: int = 0,
+           v_end: Optional[int] = None, token: Optional[torch.Tensor] = None, token_prob: Optional[torch.Tensor] = None,
+           probs: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One token a row of logits [R,V] (fp32, bf16 or fp16, any row stride) by the uniform numbers u fp32 [R] -> token int32 [R].  With
+    cfg_scale, logits is [2R,V]: the conditional rows, then the unconditional ones.  A setting is a number, or a tensor with one
+    for each row (fp32, top_k int32); temperature 0 takes the maximum.  token_prob fp32 [R] receives the token's probability,
+    probs fp32 [R,V] the distribution that it was drawn from (as cfg_accept takes it as q_probs)."""
+    lib = _lib or load_library()
+    marshal = _marshal or _load_marshal()
+    rc, token = marshal.sample(lib.address_sample, logits, u, temperature, top_k, top_p, min_p, cfg_scale, v_begin, v_end, token,
+                               token_prob, probs, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_sample")
+    return token
+
+
+def pages_resize(block_table: torch.Tensor, kv_len: torch.Tensor, new_len: torch.Tensor, page_refs: torch.Tensor, page_size: int,
+                 out_table: Optional[torch.Tensor] = None, out_len: Optional[torch.Tensor] = None,
+                 out_refs: Optional[torch.Tensor] = None, copies: Optional[torch.Tensor] = None,
+                 dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Streams of a paged cache go from kv_len [S] to new_len [S] keys: they take free pages (lowest first), or release pages;
+    a shared page that a stream grows into is replaced.  page_refs int32 [n_pages] counts the table entries that name a page, 0: free.
+    block_table, kv_len and page_refs are changed in place, or go to out_*.  Returns copies int32 [S,3], what pages_copy
+    then has to copy (from page, to page, rows; -1: nothing)."""
+    lib = _lib or load_library()
+    marshal = _marshal or _load_marshal()
+    rc, copies = marshal.pages_resize(lib.address_pages_resize, block_table, kv_len, new_len, page_refs, page_size, out_table, out_len,
+                                      out_refs, copies, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_pages_resize")
+    return copies
+
+
+def pages_fork(block_table: torch.Tensor, kv_len: torch.Tensor, parent: torch.Tensor, page_refs: torch.Tensor, page_size: int,
+               length: Optional[torch.Tensor] = None, out_table: Optional[torch.Tensor] = None,
+               out_len: Optional[torch.Tensor] = None, out_refs: Optional[torch.Tensor] = None,
+               dev_status: Optional[torch.Tensor] = None):
+    """Stream t of the new batch goes on from stream parent[t] of the old one (int32, -1: empty), from its first length[t] keys if
+    length is given; pages are shared, page_refs is changed in place or goes to out_refs -> (out_table [S_out, width], out_len [S_out]),
+    new tensors or the given ones (entries past a stream's pages are left as they are)."""
+    lib = _lib or load_library()
+    marshal = _marshal or _load_marshal()
+    rc, out_table, out_len = marshal.pages_fork(lib.address_pages_fork, block_table, kv_len, parent, page_refs, page_size, length,
+                                                out_table, out_len, out_refs, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_pages_fork")
+    return out_table, out_len
+
+
+def pages_compact_workspace_bytes(n_pages: int, max_moves: int) -> int:
+    return int(load_library().hawk_pages_compact_workspace_bytes(n_pages, max_moves))
+
+
+def pages_compact(block_table: torch.Tensor, kv_len: torch.Tensor, page_refs: torch.Tensor, page_size: int, max_moves: int,
+                  first_page: int = 0, out_table: Optional[torch.Tensor] = None, out_refs: Optional[torch.Tensor] = None,
+                  copies: Optional[torch.Tensor] = None, top: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The highest pages in use take the ids of the lowest free ones (from first_page on, max_moves at most), in place or to out_*.
+    Returns copies int32 [max_moves,3] for pages_copy; top int32 [1] receives the id from which on all pages are free."""
+    lib = _lib or load_library()
+    marshal = _marshal or _load_marshal()
+    rc, copies = marshal.pages_compact(lib.address_pages_compact, lib.address_pages_compact_workspace_bytes, block_table, kv_len, page_refs,
+                                       page_size, max_moves, first_page, out_table, out_refs, copies, top, workspace, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_pages_compact")
+    return copies
+
+
+def pages_copy(k_pages: torch.Tensor, v_pages: torch.Tensor, copies: torch.Tensor, dev_status: Optional[torch.Tensor] = None) -> None:
+    """Copies rows of pages: for each (a, b, n) of copies [.,3] with a >= 0, rows 0..n-1 of page a to page b.  k_pages, v_pages are
+    [n_pages,H_kv,page_size,D], or [layers,n_pages,H_kv,page_size,D] for all layers at once (bf16 or fp16, any strides)."""
+    lib = _lib or load_library()
+    marshal = _marshal or _load_marshal()
+    rc = marshal.pages_copy(lib.address_pages_copy, k_pages, v_pages, copies, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_pages_copy")
+
+
+def pages_keep(k_pages: Optional[torch.Tensor], v_pages: Optional[torch.Tensor], block_table: Optional[torch.Tensor],
+               row_begin: torch.Tensor, kv_len: torch.Tensor, path: Optional[torch.Tensor], accept_len: torch.Tensor, first: int = 1,
+               out_len: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The rows of an accepted path to the front of the rows that a stream has brought, and the length it then has -> out_len [S], which
+    pages_resize takes as new_len.  path [B,depth] and accept_len [B] are tree_accept's, for streams b and B + b of sequence b; the first
+    `first` rows stay.  path None: a chain, nothing moves (accept_len of cfg_accept)."""
+    lib = _lib or load_library()
+    marshal = _marshal or _load_marshal()
+    rc, out_len = marshal.pages_keep(lib.address_pages_keep, k_pages, v_pages, block_table, row_begin, kv_len, path, accept_len, first,
+                                     out_len, dev_status)
+    if rc != 0:
+        raise HawkError(rc, "hawk_pages_keep")
+    return out_len
 
 
 def verify_step_host(args: StepHostArgs) -> None:

@@ -17,7 +17,7 @@ PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libhawk_verify.so"
 SOURCES = ["hawk_api.cu", "hawk_accept.cu", "hawk_attn.cu", "hawk_head.cu", "hawk_step.cu", "hawk_pool.cu",
-           "hawk_rope.cu", "hawk_paged_attn.cu", "hawk_paged_mid.cu", "hawk_paged_tile.cu"]
+           "hawk_rope.cu", "hawk_paged_attn.cu", "hawk_paged_mid.cu", "hawk_paged_tile.cu", "hawk_pages.cu", "hawk_sample.cu"]
 ARCH_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
 

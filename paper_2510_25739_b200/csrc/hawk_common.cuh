@@ -326,6 +326,21 @@ __device__ __forceinline__ uint32_t map_shared_to_cta(const void *p, uint32_t ra
     return out;
 }
 
+// Reads through the cluster's shared window.
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t cluster_addr)
+{
+    unsigned long long v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
+
 // One arrival on an mbarrier that may live in the other CTA of the cluster.  Default semantics
 // (release at CTA scope): the data these signals guard moves through the async proxy or tensor memory
 // and is ordered by the tcgen05 fences, and a cluster-scope release measured ~0.7 us per arrival.
@@ -706,6 +721,28 @@ inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 bl
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// The same in clusters of `cluster` blocks along x (the grid is a multiple of it).
+template <class... KArgs, class... Args>
+inline cudaError_t launch_dependent_clusters(void (*kernel)(KArgs...), int cluster, dim3 grid, dim3 block, size_t smem,
+                                             cudaStream_t stream, Args &&...args)
+{
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 

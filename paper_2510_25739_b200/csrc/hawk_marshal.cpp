@@ -1,6 +1,7 @@
-// Python marshalling of the calls around the paged cache (hawk_qk_norm_rope, hawk_rope_append, hawk_paged_attn).
+// Python marshalling of the calls around the paged cache (hawk_qk_norm_rope, hawk_rope_append, hawk_paged_attn, hawk_pages_*) and of
+// hawk_sample.
 //
-// These calls run once or twice a layer on tensors of a few kilobytes, where the kernel takes 3 us and looking at a dozen tensors
+// These calls run once or twice a layer, or several a step, on tensors of a few kilobytes, where the kernel takes 3 us and looking at a dozen tensors
 // from Python takes 7.  So the tensors are checked and turned into the C ABI's argument structs here, in under 1 us; nothing
 // is computed.  Entry points are reached by the address that the caller passes (of the library build it has loaded).
 #include <Python.h>
@@ -377,10 +378,315 @@ PyObject *paged_attn(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// ---------------------------------------------------------------------------------------------- sampling
+// A setting of the rows: a number for all, or a tensor with one for each.
+template <typename N, class Read>
+const N *setting(PyObject *o, const char *name, at::ScalarType dtype, int64_t rows, int index, N &all, Read &&read)
+{
+    if (THPVariable_Check(o)) return static_cast<const N *>(dense(&THPVariable_Unpack(o), name, dtype, {rows}, index));
+    all = read(o);
+    return nullptr;
+}
+
+// Rows of a matrix: last dimension contiguous, any row stride.
+void *rows_of(const at::Tensor &t, const char *name, at::ScalarType dtype, at::IntArrayRef shape, int index, long long &stride)
+{
+    check(t, name, dtype, shape, index);
+    if (t.size(1) > 1 && t.stride(1) != 1) refuse(PyExc_ValueError, std::string(name) + ": the last dimension must be contiguous");
+    stride = t.size(0) > 1 ? t.stride(0) : t.size(1);
+    return t.data_ptr();
+}
+
+// (entry point, logits, u, temperature, top_k, top_p, min_p, cfg_scale, v_begin, v_end, token, token_prob, probs, dev_status) ->
+// (status, token)
+PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        expect(n, 14);
+        const auto fn = reinterpret_cast<decltype(&hawk_sample)>(address(args[0]));
+        const at::Tensor &x = *tensor(args[1], "logits");
+        if (!x.is_cuda()) refuse(PyExc_ValueError, "logits: must be a CUDA tensor");
+        dims(x, "logits", 2);
+        const int index = x.get_device();
+        const at::ScalarType dtype = x.scalar_type();
+        if (dtype != at::kFloat && dtype != at::kBFloat16 && dtype != at::kHalf)
+            refuse(PyExc_TypeError, "logits: expected torch.float32, torch.bfloat16 or torch.float16, got " + name_of(dtype));
+        const bool guided = args[7] != Py_None;
+        if (guided && x.size(0) % 2) refuse(PyExc_ValueError, "logits: with cfg_scale, the conditional rows come first, then as many unconditional");
+        const int64_t R = guided ? x.size(0) / 2 : x.size(0), V = x.size(1);
+        hawk_sample_args a = {};
+        a.dtype = dtype == at::kFloat ? HAWK_F32 : dtype == at::kBFloat16 ? HAWK_BF16 : HAWK_F16;
+        a.R = as_int(R, "rows");
+        a.V = as_int(V, "ids");
+        a.logits = rows_of(x, "logits", dtype, x.sizes(), index, a.row_stride);
+        if (guided) {
+            a.uncond = static_cast<const char *>(a.logits) + R * a.row_stride * static_cast<int64_t>(x.element_size());
+            a.uncond_row_stride = a.row_stride;
+        }
+        a.row_temperature = setting(args[3], "temperature", at::kFloat, R, index, a.temperature, number);
+        a.row_top_k = setting(args[4], "top_k", at::kInt, R, index, a.top_k, [](PyObject *o) { return integer(o, "top_k"); });
+        a.row_top_p = setting(args[5], "top_p", at::kFloat, R, index, a.top_p, number);
+        a.row_min_p = setting(args[6], "min_p", at::kFloat, R, index, a.min_p, number);
+        if (guided) a.row_cfg_scale = setting(args[7], "cfg_scale", at::kFloat, R, index, a.cfg_scale, number);
+        a.u = static_cast<const float *>(dense(tensor(args[2], "u"), "u", at::kFloat, {R}, index));
+        a.v_begin = integer(args[8], "v_begin");
+        a.v_end = args[9] == Py_None ? a.V : integer(args[9], "v_end");
+        std::optional<at::Tensor> made;
+        const at::Tensor *out = tensor(args[10], "token", false);
+        if (!out) out = &made.emplace(at::empty({R}, x.options().dtype(at::kInt)));
+        a.token = static_cast<int32_t *>(const_cast<void *>(dense(out, "token", at::kInt, {R}, index)));
+        a.token_prob = static_cast<float *>(const_cast<void *>(dense(tensor(args[11], "token_prob", false), "token_prob", at::kFloat, {R}, index)));
+        if (const at::Tensor *probs = tensor(args[12], "probs", false)) {
+            const int64_t shape[2] = {R, V};
+            a.probs = static_cast<float *>(rows_of(*probs, "probs", at::kFloat, shape, index, a.probs_row_stride));
+        }
+        int32_t *status = status_word(args[13], index);
+        const long rc = run_on(index, [&](hawk_stream_t st) { return fn(&a, status, st); });
+        return Py_BuildValue("lN", rc, owned(args[10], made ? &*made : nullptr));
+    });
+}
+
+// ---------------------------------------------------------------------------------------------- pages
+const int32_t *ints(PyObject *o, const char *name, at::IntArrayRef shape, int index, bool needed = true)
+{
+    return static_cast<const int32_t *>(dense(tensor(o, name, needed), name, at::kInt, shape, index));
+}
+
+// An int32 result: the given tensor, or `made`, new.
+int32_t *result(PyObject *o, const char *name, at::IntArrayRef shape, int index, const at::Tensor &like, std::optional<at::Tensor> &made)
+{
+    if (o == Py_None) return static_cast<int32_t *>(made.emplace(at::empty(shape, like.options())).data_ptr());
+    return const_cast<int32_t *>(ints(o, name, shape, index));
+}
+
+// An int32 result in place of `input` where none is given.
+int32_t *in_place(PyObject *o, const char *name, at::IntArrayRef shape, int index, const int32_t *input)
+{
+    return o == Py_None ? const_cast<int32_t *>(input) : const_cast<int32_t *>(ints(o, name, shape, index));
+}
+
+// The cache's state: block_table, kv_len, page_refs, page_size from args[0], args[1], args[at], args[at + 1] on.
+struct Pages {
+    const at::Tensor &table;
+    int index, S, W, n_pages, page_size;
+    const int32_t *block_table, *kv_len, *refs;
+
+    Pages(PyObject *t, PyObject *kv, PyObject *r, PyObject *page) : table(*tensor(t, "block_table"))
+    {
+        if (!table.is_cuda()) refuse(PyExc_ValueError, "block_table: must be a CUDA tensor");
+        dims(table, "block_table", 2);
+        index = table.get_device();
+        S = as_int(table.size(0), "streams");
+        W = as_int(table.size(1), "table width");
+        block_table = ints(t, "block_table", table.sizes(), index);
+        kv_len = ints(kv, "kv_len", {table.size(0)}, index);
+        const at::Tensor &counts = *tensor(r, "page_refs");
+        dims(counts, "page_refs", 1);
+        n_pages = as_int(counts.size(0), "pages");
+        refs = ints(r, "page_refs", counts.sizes(), index);
+        page_size = integer(page, "page_size");
+    }
+};
+
+// (entry point, block_table, kv_len, new_len, page_refs, page_size, out_table, out_len, out_refs, copies, dev_status) -> (status, copies)
+PyObject *pages_resize(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        expect(n, 11);
+        const auto fn = reinterpret_cast<decltype(&hawk_pages_resize)>(address(args[0]));
+        const Pages p(args[1], args[2], args[4], args[5]);
+        const int64_t S = p.S, W = p.W, N = p.n_pages, all[2] = {S, W}, three[2] = {S, 3};
+        hawk_pages_resize_args a = {};
+        a.S = p.S;
+        a.table_width = p.W;
+        a.n_pages = p.n_pages;
+        a.page_size = p.page_size;
+        a.block_table = p.block_table;
+        a.kv_len = p.kv_len;
+        a.page_refs = p.refs;
+        a.new_len = ints(args[3], "new_len", {S}, p.index);
+        a.out_table = in_place(args[6], "out_table", all, p.index, p.block_table);
+        a.out_len = in_place(args[7], "out_len", {S}, p.index, p.kv_len);
+        a.out_refs = in_place(args[8], "out_refs", {N}, p.index, p.refs);
+        std::optional<at::Tensor> made;
+        a.copies = result(args[9], "copies", three, p.index, p.table, made);
+        int32_t *status = status_word(args[10], p.index);
+        const long rc = run_on(p.index, [&](hawk_stream_t st) { return fn(&a, status, st); });
+        return Py_BuildValue("lN", rc, owned(args[9], made ? &*made : nullptr));
+    });
+}
+
+// (entry point, block_table, kv_len, parent, page_refs, page_size, length, out_table, out_len, out_refs, dev_status) -> (status, out_table,
+// out_len)
+PyObject *pages_fork(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        expect(n, 11);
+        const auto fn = reinterpret_cast<decltype(&hawk_pages_fork)>(address(args[0]));
+        const Pages p(args[1], args[2], args[4], args[5]);
+        const at::Tensor &parent = *tensor(args[3], "parent");
+        dims(parent, "parent", 1);
+        const int64_t S = parent.size(0), W = p.W, N = p.n_pages, all[2] = {S, W};
+        hawk_pages_fork_args a = {};
+        a.S = p.S;
+        a.S_out = as_int(S, "streams");
+        a.table_width = p.W;
+        a.n_pages = p.n_pages;
+        a.page_size = p.page_size;
+        a.block_table = p.block_table;
+        a.kv_len = p.kv_len;
+        a.page_refs = p.refs;
+        a.parent = ints(args[3], "parent", {S}, p.index);
+        a.length = ints(args[6], "length", {S}, p.index, false);
+        std::optional<at::Tensor> table_made, len_made;
+        a.out_table = result(args[7], "out_table", all, p.index, p.table, table_made);
+        a.out_len = result(args[8], "out_len", {S}, p.index, p.table, len_made);
+        a.out_refs = in_place(args[9], "out_refs", {N}, p.index, p.refs);
+        int32_t *status = status_word(args[10], p.index);
+        const long rc = run_on(p.index, [&](hawk_stream_t st) { return fn(&a, status, st); });
+        return Py_BuildValue("lNN", rc, owned(args[7], table_made ? &*table_made : nullptr), owned(args[8], len_made ? &*len_made : nullptr));
+    });
+}
+
+// (entry point, workspace query, block_table, kv_len, page_refs, page_size, max_moves, first_page, out_table, out_refs, copies, top, workspace,
+// dev_status) -> (status, copies)
+PyObject *pages_compact(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        expect(n, 14);
+        const auto fn = reinterpret_cast<decltype(&hawk_pages_compact)>(address(args[0]));
+        const auto need_of = reinterpret_cast<decltype(&hawk_pages_compact_workspace_bytes)>(address(args[1]));
+        const Pages p(args[2], args[3], args[4], args[5]);
+        hawk_pages_compact_args a = {};
+        a.S = p.S;
+        a.table_width = p.W;
+        a.n_pages = p.n_pages;
+        a.page_size = p.page_size;
+        a.block_table = p.block_table;
+        a.kv_len = p.kv_len;
+        a.page_refs = p.refs;
+        a.max_moves = integer(args[6], "max_moves");
+        if (a.max_moves < 0) refuse(PyExc_ValueError, "max_moves: must not be negative");
+        a.first_page = integer(args[7], "first_page");
+        const int64_t S = p.S, W = p.W, N = p.n_pages, all[2] = {S, W}, three[2] = {a.max_moves, 3};
+        a.out_table = in_place(args[8], "out_table", all, p.index, p.block_table);
+        a.out_refs = in_place(args[9], "out_refs", {N}, p.index, p.refs);
+        std::optional<at::Tensor> made, ws_made;
+        a.copies = result(args[10], "copies", three, p.index, p.table, made);
+        a.top = const_cast<int32_t *>(ints(args[11], "top", {1}, p.index, false));
+        if (const at::Tensor *ws = tensor(args[12], "workspace", false)) {
+            a.workspace = const_cast<void *>(dense(ws, "workspace", ws->scalar_type(), ws->sizes(), p.index));
+            a.workspace_bytes = static_cast<size_t>(ws->numel()) * ws->element_size();
+        } else if (const size_t need = need_of(a.n_pages, a.max_moves)) {
+            a.workspace = ws_made.emplace(at::empty({static_cast<int64_t>(need)}, p.table.options().dtype(at::kByte))).data_ptr();
+            a.workspace_bytes = need;
+        }
+        int32_t *status = status_word(args[13], p.index);
+        const long rc = run_on(p.index, [&](hawk_stream_t st) { return fn(&a, status, st); });
+        return Py_BuildValue("lN", rc, owned(args[10], made ? &*made : nullptr));
+    });
+}
+
+// Page tensors [n_pages, H_kv, page_size, D], or [layers, n_pages, H_kv, page_size, D].
+hawk_page_tensors page_tensors(PyObject *k, PyObject *v, int &index)
+{
+    const at::Tensor &kp = *tensor(k, "k_pages"), &vp = *tensor(v, "v_pages");
+    const Where w = where(kp, "k_pages");
+    index = w.index;
+    if (kp.dim() != 4 && kp.dim() != 5) refuse(PyExc_ValueError, "k_pages: expected 4 or 5 dimensions, got " + text_of(kp.sizes()));
+    hawk_page_tensors p = {};
+    const int64_t at = kp.dim() - 4;
+    p.k_pages = strided(kp, "k_pages", w.dtype, kp.sizes(), w.index);
+    p.v_pages = strided(vp, "v_pages", w.dtype, kp.sizes(), w.index);
+    p.layers = at ? as_int(kp.size(0), "layers") : 1;
+    p.n_pages = as_int(kp.size(at), "pages");
+    p.H_kv = as_int(kp.size(at + 1), "heads");
+    p.page_size = as_int(kp.size(at + 2), "page size");
+    p.D = as_int(kp.size(at + 3), "head dimension");
+    auto stride = [](const at::Tensor &t, int64_t d) -> long long { return t.size(d) > 1 ? t.stride(d) : 0; };
+    p.k_layer_stride = at ? stride(kp, 0) : 0;
+    p.v_layer_stride = at ? stride(vp, 0) : 0;
+    p.k_page_stride = stride(kp, at);
+    p.v_page_stride = stride(vp, at);
+    p.k_head_stride = stride(kp, at + 1);
+    p.v_head_stride = stride(vp, at + 1);
+    p.k_row_stride = stride(kp, at + 2);
+    p.v_row_stride = stride(vp, at + 2);
+    return p;
+}
+
+// (entry point, k_pages, v_pages, copies, dev_status) -> status
+PyObject *pages_copy(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        expect(n, 5);
+        const auto fn = reinterpret_cast<decltype(&hawk_pages_copy)>(address(args[0]));
+        int index;
+        const hawk_page_tensors p = page_tensors(args[1], args[2], index);
+        const at::Tensor &copies = *tensor(args[3], "copies");
+        dims(copies, "copies", 2);
+        const int64_t three[2] = {copies.size(0), 3};
+        const int32_t *list = ints(args[3], "copies", three, index);
+        const int count = as_int(copies.size(0), "copies");
+        int32_t *status = status_word(args[4], index);
+        const long rc = run_on(index, [&](hawk_stream_t st) { return fn(&p, list, count, status, st); });
+        return Py_BuildValue("l", rc);
+    });
+}
+
+// (entry point, k_pages, v_pages, block_table, row_begin, kv_len, path, accept_len, first, out_len, dev_status) -> (status, out_len)
+PyObject *pages_keep(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        expect(n, 11);
+        const auto fn = reinterpret_cast<decltype(&hawk_pages_keep)>(address(args[0]));
+        const at::Tensor &kv = *tensor(args[5], "kv_len");
+        if (!kv.is_cuda()) refuse(PyExc_ValueError, "kv_len: must be a CUDA tensor");
+        dims(kv, "kv_len", 1);
+        int index = kv.get_device();
+        const int64_t S = kv.size(0);
+        hawk_pages_keep_args a = {};
+        a.S = as_int(S, "streams");
+        a.kv_len = ints(args[5], "kv_len", {S}, index);
+        a.row_begin = ints(args[4], "row_begin", {S + 1}, index);
+        const at::Tensor &accepted = *tensor(args[7], "accept_len");
+        dims(accepted, "accept_len", 1);
+        const int64_t B = accepted.size(0);
+        a.B = as_int(B, "sequences");
+        a.accept_len = ints(args[7], "accept_len", {B}, index);
+        a.first = integer(args[8], "first");
+        if (const at::Tensor *path = tensor(args[6], "path", false)) {
+            dims(*path, "path", 2);
+            const int64_t shape[2] = {B, path->size(1)};
+            a.path = ints(args[6], "path", shape, index);
+            a.path_width = as_int(path->size(1), "path");
+            int pages_index;
+            a.pages = page_tensors(args[1], args[2], pages_index);
+            if (pages_index != index) refuse(PyExc_ValueError, "k_pages: must be on cuda:" + std::to_string(index));
+            const at::Tensor &table = *tensor(args[3], "block_table");
+            dims(table, "block_table", 2);
+            const int64_t all[2] = {S, table.size(1)};
+            a.block_table = ints(args[3], "block_table", all, index);
+            a.table_width = as_int(table.size(1), "table width");
+        }
+        std::optional<at::Tensor> made;
+        a.out_len = result(args[9], "out_len", {S}, index, kv, made);
+        int32_t *status = status_word(args[10], index);
+        const long rc = run_on(index, [&](hawk_stream_t st) { return fn(&a, status, st); });
+        return Py_BuildValue("lN", rc, owned(args[9], made ? &*made : nullptr));
+    });
+}
+
 PyMethodDef methods[] = {
     {"qk_norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(qk_norm_rope)), METH_FASTCALL, nullptr},
     {"rope_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(rope_append)), METH_FASTCALL, nullptr},
     {"paged_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(paged_attn)), METH_FASTCALL, nullptr},
+    {"sample", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(sample)), METH_FASTCALL, nullptr},
+    {"pages_resize", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(pages_resize)), METH_FASTCALL, nullptr},
+    {"pages_fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(pages_fork)), METH_FASTCALL, nullptr},
+    {"pages_compact", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(pages_compact)), METH_FASTCALL, nullptr},
+    {"pages_copy", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(pages_copy)), METH_FASTCALL, nullptr},
+    {"pages_keep", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(pages_keep)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
