@@ -697,7 +697,7 @@ hawk_status hawk_pages_fork(const hawk_pages_fork_args *args, int32_t *dev_statu
  * u_0 > u_1 > ... the pages in use, all from first_page on, page u_i becomes page f_i for as long as f_i < u_i and i < max_moves.
  *   copies     int32 [max_moves][3]: copies[i] = (u_i, f_i, page_size)
  *   out_table  the table with the new ids, out_refs the counts that moved with them
- *   top        int32 [1] or NULL: all pages from this id on are free then (at least first_page)
+ *   top        int32 [1] or NULL: all pages from this id on are free then (at least first_page, which is at most n_pages)
  *   workspace  at least hawk_pages_compact_workspace_bytes(n_pages, max_moves) bytes, 16-byte aligned, no initialisation; calls that may
  *              overlap on the GPU need one each
  * A page that the caller holds by a count of its own moves like the others (copies tell where).

@@ -28,29 +28,43 @@ struct Div {  // number of pages of `keys` keys
     __device__ __forceinline__ int pages(int keys) const { return static_cast<int>(page.div(static_cast<uint32_t>(keys) + page.d - 1)); }
 };
 
-__device__ __forceinline__ int warp_inclusive(int v)
+template <typename N>
+__device__ __forceinline__ N warp_inclusive(N v)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, v, o);
+        const N u = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += u;
     }
     return v;
 }
 
-// Exclusive prefix sum over the block's threads; *total: of all.  `sh` holds kBookWarps ints.
-__device__ __forceinline__ int block_exclusive(int v, int *sh, int *total)
+// Exclusive prefix sum over the block's threads; *total: of all.  `sh` holds kBookWarps numbers.
+template <typename N>
+__device__ __forceinline__ N block_exclusive(N v, N *sh, N *total)
 {
-    const int inc = warp_inclusive(v), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const N inc = warp_inclusive(v);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     __syncthreads();  // (sh may still be read from the sum before)
     if (lane == 31) sh[warp] = inc;
     __syncthreads();
-    const int mine = sh[lane < kBookWarps ? lane : 0];
-    const int sums = warp_inclusive(lane < kBookWarps ? mine : 0);
+    static_assert(kBookWarps == 32, "a sum a lane");
+    const N sums = warp_inclusive(sh[lane]);
     *total = __shfl_sync(0xffffffffu, sums, kBookWarps - 1);
-    const int before = warp > 0 ? __shfl_sync(0xffffffffu, sums, warp - 1) : 0;
-    return before + inc - v;
+    const N before = __shfl_sync(0xffffffffu, sums, warp > 0 ? warp - 1 : 0);
+    return (warp > 0 ? before : N(0)) + inc - v;
+}
+
+// Sum over the block's threads.
+__device__ __forceinline__ int block_sum(int v, int *sh)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    v = __reduce_add_sync(0xffffffffu, v);
+    __syncthreads();  // (sh may still be read from the sum before)
+    if (lane == 0) sh[warp] = v;
+    __syncthreads();
+    return __reduce_add_sync(0xffffffffu, sh[lane]);
 }
 
 // Barrier of the cluster (lanes that a branch parted come together first).
@@ -136,156 +150,189 @@ struct ResizeParams {
 };
 
 struct ResizeShared {
-    uint32_t bits[kSlice / 32];
-    int end[kMaxStreams];    // running sum of the pages that streams need
-    int kv[kMaxStreams];     // keys now; -1: the stream stays as it is (its lengths are out of range)
-    int have[kMaxStreams];   // pages now, times two, plus one where the last is copied
+    uint32_t bits[kSlice / 32];  // the share's free pages
+    int before[kSlice / 32];     // free pages of the share in front of each word
+    int end[kMaxStreams];        // running sum of the pages that streams need
+    int kv[kMaxStreams], next[kMaxStreams];  // lengths; -1: out of range, the stream stays as it is
+    int last[kMaxStreams];       // the page that a stream grows into, -1: none
     int sums[kBookWarps];
-    int slot, any;
+    int slot;
 };
 
+// The n-th set bit (from 0) of a word that has it.
+__device__ __forceinline__ int nth_bit(uint32_t word, int n)
+{
+    int at = 0;
+#pragma unroll
+    for (int half = 16; half; half >>= 1) {
+        const int low = __popc((word >> at) & ((1u << half) - 1));
+        if (n >= low) {
+            n -= low;
+            at += half;
+        }
+    }
+    return at;
+}
+
+// The first entry of a non-decreasing array that is past r.
+__device__ __forceinline__ int first_past(const int *ends, int n, int r)
+{
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (ends[mid] > r) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+// Everything that the block reads of the state as it was on entry it reads before the first barrier of the cluster, and nobody writes the
+// state in place before it (but a block the counts of its own share of the pages).
 __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(ResizeParams P)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     ResizeShared &sh = *reinterpret_cast<ResizeShared *>(smem_raw);
     hawk::allow_dependent_launch();
     hawk::grid_dependency_wait();
-    const int tid = threadIdx.x, lane = tid & 31, rank = static_cast<int>(hawk::cluster_cta_rank());
-    const int worker = rank * kBookWarps + (tid >> 5);  // warp of the cluster
-    constexpr int kWorkers = kBookBlocks * kBookWarps;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = static_cast<int>(hawk::cluster_cta_rank());
     const long long cap = static_cast<long long>(P.W) * P.div.page.d;
     int flags = 0, first, end;
     slice_of(P.n_pages, rank, first, end);
 
-    // ---- lengths; entries that stay; counts to where they are kept.  Everything that is decided is decided by the lengths as they
-    // were on entry, which every block reads before the barrier in front of the writes.
-    if (tid == 0) sh.any = 0;
-    __syncthreads();
-    bool shrinks = false;
+    // ---- lengths, pages that streams grow into; the share's counts to where they are kept
+    if (P.out_refs != P.refs) {
+        for (int i = first / 4 + tid; i < end / 4; i += kBookThreads)
+            reinterpret_cast<int4 *>(P.out_refs)[i] = reinterpret_cast<const int4 *>(P.refs)[i];
+        for (int i = max(first, end & ~3) + tid; i < end; i += kBookThreads) P.out_refs[i] = P.refs[i];
+    }
     for (int s = tid; s < P.S; s += kBookThreads) {
         const int old = P.kv[s], next = P.next[s];
         const bool ok = old >= 0 && old <= cap && next >= 0 && next <= cap;
         if (!ok) flags |= HAWK_DEV_BAD_PREFIX;
+        int last = -1;
+        if (ok && next > old) {
+            uint32_t part;
+            const int full = static_cast<int>(P.div.page.divmod(static_cast<uint32_t>(old), part));
+            if (part != 0) {
+                last = P.table[static_cast<size_t>(s) * P.W + full];
+                if (last < 0 || last >= P.n_pages) {
+                    flags |= HAWK_DEV_BAD_PAGE;
+                    last = -1;
+                }
+            }
+        }
         sh.kv[s] = ok ? old : -1;
-        shrinks |= ok && next < old;
-    }
-    if (shrinks) sh.any = 1;
-    const bool moved_refs = P.out_refs != P.refs;
-    if (moved_refs) {
-        for (int i = first / 4 + tid; i < end / 4; i += kBookThreads)
-            reinterpret_cast<int4 *>(P.out_refs)[i] = reinterpret_cast<const int4 *>(P.refs)[i];
-        for (int i = (end & ~3) + tid; i < end; i += kBookThreads) P.out_refs[i] = P.refs[i];
+        sh.next[s] = ok ? next : -1;
+        sh.last[s] = last;
     }
     __syncthreads();
-    const bool any = sh.any != 0;  // the same in all blocks
-    if (any && moved_refs) meet();
 
-    // ---- streams that shrink release pages
-    if (any || P.out_table != P.table) {
-        for (int s = worker; s < P.S; s += kWorkers) {
+    // ---- streams that shrink: each block releases what lies in its share (all look through the entries, which is less than a barrier
+    // costs unless very many are released); entries that stay, where the table goes elsewhere
+    for (int s = warp; s < P.S; s += kBookWarps) {
+        const int old = sh.kv[s], next = sh.next[s];
+        if (next >= old) continue;
+        const int have = P.div.pages(old);
+        const size_t row = static_cast<size_t>(s) * P.W;
+        for (int j = P.div.pages(next) + lane; j < have; j += 32) {
+            const int page = P.table[row + j];
+            if (page < 0 || page >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;
+            else if (page >= first && page < end) release(P.out_refs, page, P.n_pages, flags);
+        }
+    }
+    if (P.out_table != P.table) {
+        for (int s = rank * kBookWarps + warp; s < P.S; s += kBookBlocks * kBookWarps) {
             const int old = sh.kv[s];
             if (old < 0) continue;
-            const int next = P.next[s], have = P.div.pages(old), stay = next < old ? P.div.pages(next) : have;
+            const int stay = P.div.pages(min(old, sh.next[s]));
             const size_t row = static_cast<size_t>(s) * P.W;
-            if (P.out_table != P.table)
-                for (int j = lane; j < stay; j += 32) P.out_table[row + j] = P.table[row + j];
-            for (int j = stay + lane; j < have; j += 32) release(P.out_refs, P.table[row + j], P.n_pages, flags);
-        }
-    }
-    if (any || moved_refs) meet();
-
-    // ---- what every stream needs (each block for itself), and the free pages of the block's share
-    int need[kMaxStreams / kBookThreads], sum = 0;
+            for (int j = lane; j < stay; j += 128) {  // (four loads in flight)
+                int page[4];
 #pragma unroll
-    for (int i = 0; i < kMaxStreams / kBookThreads; ++i) {
-        const int s = tid * (kMaxStreams / kBookThreads) + i;
-        need[i] = 0;
-        if (s >= P.S) continue;
-        const int old = sh.kv[s];
-        int have = 0, copy = 0;
-        if (old >= 0) {
-            const int next = P.next[s];
-            uint32_t part;
-            have = P.div.pages(old);
-            P.div.page.divmod(static_cast<uint32_t>(old), part);
-            if (next > old) {
-                if (part != 0) {
-                    const int page = P.table[static_cast<size_t>(s) * P.W + have - 1];
-                    if (page < 0 || page >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;
-                    else copy = __ldcg(P.out_refs + page) > 1;
-                }
-                need[i] = P.div.pages(next) - have + copy;
+                for (int k = 0; k < 4; ++k) page[k] = j + 32 * k < stay ? P.table[row + j + 32 * k] : 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (j + 32 * k < stay) P.out_table[row + j + 32 * k] = page[k];
             }
         }
-        sh.have[s] = have * 2 + copy;
-        sum += need[i];
     }
-    int total_need, total_free, free_before, mine;
-    int run = block_exclusive(sum, sh.sums, &total_need);
-#pragma unroll
-    for (int i = 0; i < kMaxStreams / kBookThreads; ++i) {
-        const int s = tid * (kMaxStreams / kBookThreads) + i;
-        run += need[i];
-        if (s < P.S) sh.end[s] = run;
-    }
+    __syncthreads();
+
+    // ---- the share's free pages
     const int words = (end - first + 31) / 32;
-    int count = mark_pages(P.out_refs, first, end, sh.bits, [](int c, int) { return c == 0; });
-    (void)block_exclusive(count, sh.sums, &mine);  // (its barriers publish bits and end)
+    (void)mark_pages(P.out_refs, first, end, sh.bits, [](int c, int) { return c == 0; });
+    __syncthreads();
+    const int per = (words + kBookThreads - 1) / kBookThreads, w0 = min(words, tid * per), w1 = min(words, w0 + per);
+    int in = 0, mine, free_before, total_free, total_need;
+    for (int w = w0; w < w1; ++w) in += __popc(sh.bits[w]);
+    int at = block_exclusive(in, sh.sums, &mine);
+    for (int w = w0; w < w1; ++w) {
+        at += __popc(sh.bits[w]);
+        sh.before[w] = at;  // (with the word's own)
+    }
     exchange_counts(mine, &sh.slot, rank, free_before, total_free);
 
-    // ---- the free pages of the share to the streams whose turn they are
-    if (free_before < total_need && total_need > 0) {
-        const int per = (words + kBookThreads - 1) / kBookThreads;  // consecutive words a thread
-        int in = 0, dummy;
-        for (int w = tid * per; w < min(words, (tid + 1) * per); ++w) in += __popc(sh.bits[w]);
-        int r = free_before + block_exclusive(in, sh.sums, &dummy);
-        for (int w = tid * per; w < min(words, (tid + 1) * per) && r < total_need; ++w) {
-            for (uint32_t m = sh.bits[w]; m && r < total_need; m &= m - 1, ++r) {
-                const int page = first + w * 32 + __ffs(m) - 1;
-                int lo = 0, hi = P.S - 1;  // the first stream whose running sum is past r
-                while (lo < hi) {
-                    const int mid = (lo + hi) / 2;
-                    if (sh.end[mid] > r) hi = mid;
-                    else lo = mid + 1;
-                }
-                if (sh.end[lo] > total_free) continue;  // this stream and all behind it stay as they were
-                const int copy = sh.have[lo] & 1, have = sh.have[lo] >> 1;
-                const int at = r - (lo > 0 ? sh.end[lo - 1] : 0);
-                const int j = have - copy + at;
-                const size_t e = static_cast<size_t>(lo) * P.W + j;
-                if (!HAWK_IN_BOUNDS(P.dev_status, j, P.W) || !HAWK_IN_BOUNDS(P.dev_status, page, P.n_pages)) continue;
-                if (copy && at == 0) {
-                    const int from = P.table[e];
-                    uint32_t part;
-                    P.div.page.divmod(static_cast<uint32_t>(sh.kv[lo]), part);
-                    P.copies[3 * lo] = from;
-                    P.copies[3 * lo + 1] = page;
-                    P.copies[3 * lo + 2] = static_cast<int>(part);
-                    release(P.out_refs, from, P.n_pages, flags);
-                }
-                P.out_table[e] = page;
-                P.out_refs[page] = 1;
-            }
-        }
+    // ---- what every stream needs: each block for itself
+    constexpr int kPer = kMaxStreams / kBookThreads;
+    const int streams = (P.S + kBookThreads - 1) / kBookThreads;  // a thread
+    int need[kPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = tid * streams + i;
+        need[i] = 0;
+        if (i >= streams || s >= P.S) continue;
+        const int old = sh.kv[s], next = sh.next[s];
+        if (next <= old) continue;
+        need[i] = P.div.pages(next) - P.div.pages(old);
+        if (sh.last[s] >= 0 && __ldcg(P.out_refs + sh.last[s]) > 1) ++need[i];
+        else sh.last[s] = -1;  // (from here on: the page that is copied)
+        sum += need[i];
     }
+    int run = block_exclusive(sum, sh.sums, &total_need);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = tid * streams + i;
+        run += need[i];
+        if (i < streams && s < P.S) sh.end[s] = run;
+    }
+    __syncthreads();
+
+    // ---- the share's free pages to the streams whose turn they are, a page a thread
+    for (int i = tid; i < mine && free_before + i < total_need; i += kBookThreads) {
+        const int r = free_before + i, word = first_past(sh.before, words, i);
+        const int page = first + word * 32 + nth_bit(sh.bits[word], i - (word > 0 ? sh.before[word - 1] : 0));
+        const int s = first_past(sh.end, P.S, r);
+        if (sh.end[s] > total_free) continue;  // this stream and all behind it stay as they were
+        const int old = sh.kv[s], copied = sh.last[s], nth = r - (s > 0 ? sh.end[s - 1] : 0);
+        const int j = P.div.pages(old) + nth - (copied >= 0);
+        if (!HAWK_IN_BOUNDS(P.dev_status, j, P.W) || !HAWK_IN_BOUNDS(P.dev_status, page, P.n_pages)) continue;
+        if (copied >= 0 && nth == 0) {
+            uint32_t part;
+            P.div.page.divmod(static_cast<uint32_t>(old), part);
+            P.copies[3 * s] = copied;
+            P.copies[3 * s + 1] = page;
+            P.copies[3 * s + 2] = static_cast<int>(part);
+        }
+        P.out_table[static_cast<size_t>(s) * P.W + j] = page;
+        P.out_refs[page] = 1;
+    }
+    meet();  // (the counts of shared pages have been looked at by all; nobody's numbers are read any more)
     for (int s = rank * kBookThreads + tid; s < P.S; s += kBookBlocks * kBookThreads) {
         const int needs = sh.end[s] - (s > 0 ? sh.end[s - 1] : 0);
         const bool served = needs == 0 || sh.end[s] <= total_free;
         if (!served) flags |= HAWK_DEV_NO_PAGES;
-        if (!(sh.have[s] & 1) || !served) {
+        const int copied = sh.next[s] > sh.kv[s] && served ? sh.last[s] : -1;
+        if (copied >= 0) {
+            release(P.out_refs, copied, P.n_pages, flags);
+        } else {
             P.copies[3 * s] = -1;
             P.copies[3 * s + 1] = -1;
             P.copies[3 * s + 2] = 0;
         }
-        if (sh.kv[s] < 0) {
-            if (P.out_len != P.kv) P.out_len[s] = P.kv[s];
-        } else {
-            const int next = P.next[s];
-            P.out_len[s] = served ? next : sh.kv[s];
-        }
+        if (sh.kv[s] >= 0) P.out_len[s] = served ? sh.next[s] : sh.kv[s];
+        else if (P.out_len != P.kv) P.out_len[s] = P.kv[s];
     }
     report(P.dev_status, flags);
-    meet();  // nobody leaves while its numbers are read
 }
 
 // ---------------------------------------------------------------------------------------------- fork
@@ -309,9 +356,11 @@ __global__ void __launch_bounds__(256) copy_ints_kernel(const int32_t *from, int
     }
 }
 
-// A block of 128 lanes takes one stream's entries, old and new: entry j of out stream t is its parent's; the count of a page that t
+constexpr int kForkThreads = 128;
+
+// A block takes one stream's entries, old and new, four a thread in flight: entry j of out stream t is its parent's; the count of a page that t
 // named before and names still (a stream that goes on) is not touched at all.
-__global__ void __launch_bounds__(128) fork_kernel(ForkParams P)
+__global__ void __launch_bounds__(kForkThreads) fork_kernel(ForkParams P)
 {
     hawk::allow_dependent_launch();
     hawk::grid_dependency_wait();
@@ -343,17 +392,29 @@ __global__ void __launch_bounds__(128) fork_kernel(ForkParams P)
     const int held = t < P.S ? P.div.pages(keys_of(t)) : 0;
     const int same = from == t ? min(take, held) : 0;  // entries that go on
     const size_t row = static_cast<size_t>(t) * P.W, source = static_cast<size_t>(max(from, 0)) * P.W;
-    for (int j = tid; j < take; j += 128) {
-        const int page = P.table[source + j];
-        P.out_table[row + j] = page;
-        if (j < same) continue;
-        if (page < 0 || page >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;
-        else atomicAdd(P.refs + page, 1);
-    }
-    for (int j = same + tid; j < held; j += 128) {
-        const int page = P.table[row + j];
-        if (page < 0 || page >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;
-        else atomicSub(P.refs + page, 1);
+    constexpr int kFlight = 4;
+    const int most = max(take, held);
+    for (int j0 = tid; j0 < most; j0 += kForkThreads * kFlight) {
+        int now[kFlight], was[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            const int j = j0 + k * kForkThreads;
+            now[k] = j < take ? P.table[source + j] : 0;
+            was[k] = j >= same && j < held ? P.table[row + j] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            const int j = j0 + k * kForkThreads;
+            if (j < take) {
+                P.out_table[row + j] = now[k];
+                if (now[k] < 0 || now[k] >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;
+                else if (j >= same) atomicAdd(P.refs + now[k], 1);
+            }
+            if (j >= same && j < held) {
+                if (was[k] < 0 || was[k] >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;
+                else atomicSub(P.refs + was[k], 1);
+            }
+        }
     }
     report(P.dev_status, flags);
 }
@@ -362,40 +423,44 @@ __global__ void __launch_bounds__(128) fork_kernel(ForkParams P)
 struct CompactParams {
     const int32_t *table, *kv, *refs;
     int32_t *out_table, *out_refs, *copies, *top;
-    int32_t *to, *from;   // [moves + 1] the lowest free pages, ascending, and the highest in use, descending
-    int32_t *place;       // [n_pages] place in the lists of the pages that move
+    int32_t *to, *from;   // [lists] the lowest free pages, ascending, and the highest in use, descending
+    int32_t *place;       // [n_pages] place in the lists of the pages that may move
+    int32_t *counts;      // [kBookBlocks] pages in use of each share that lie behind where the pages in use would end
     int S, W, n_pages, first_page, moves;
     Div div;
+    hawk::FastDiv div_runs;  // runs of 128 entries a stream
     int32_t *dev_status;
 };
 
 struct CompactShared {
     uint32_t used[kSlice / 32];
     int sums[kBookWarps];
+    uint32_t packed[kBookWarps];
     int slot_used, slot_free;
 };
 
+// Packed, the pages in use end at `border`: those behind it have to move, and as many free ones lie in front of it.  Both lists are made
+// by rank; then every block knows all it needs, and the moves and the new ids are written without another barrier.
 __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams P)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     CompactShared &sh = *reinterpret_cast<CompactShared *>(smem_raw);
     hawk::allow_dependent_launch();
     hawk::grid_dependency_wait();
-    const int tid = threadIdx.x, lane = tid & 31, rank = static_cast<int>(hawk::cluster_cta_rank());
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = static_cast<int>(hawk::cluster_cta_rank());
     const long long cap = static_cast<long long>(P.W) * P.div.page.d;
     int flags = 0, first, end;
     slice_of(P.n_pages, rank, first, end);
     if (P.out_refs != P.refs) {
         for (int i = first / 4 + tid; i < end / 4; i += kBookThreads)
             reinterpret_cast<int4 *>(P.out_refs)[i] = reinterpret_cast<const int4 *>(P.refs)[i];
-        for (int i = (end & ~3) + tid; i < end; i += kBookThreads) P.out_refs[i] = P.refs[i];
+        for (int i = max(first, end & ~3) + tid; i < end; i += kBookThreads) P.out_refs[i] = P.refs[i];
     }
     const int words = (end - first + 31) / 32;
-    // pages of the share from first_page on
     const int from_page = P.first_page;
     const int count = mark_pages(P.refs, first, end, sh.used, [=](int c, int p) { return c != 0 && p >= from_page; });
-    int mine, used_before, used, free_before, free_all;
-    (void)block_exclusive(count, sh.sums, &mine);
+    int mine = count, used_before, used, free_before, free_all;
+    mine = block_sum(mine, sh.sums);
     const int eligible = max(0, end - max(first, from_page));
     if (tid == 0) sh.slot_free = eligible - mine;
     exchange_counts(mine, &sh.slot_used, rank, used_before, used);
@@ -407,43 +472,44 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams 
         free_all += n;
     }
 
-    // ---- the lowest free pages and the highest in use, by rank
-    const int lists = P.moves + 1;
-    const int per = (words + kBookThreads - 1) / kBookThreads;
-    const int w0 = tid * per, w1 = min(words, w0 + per);
-    int in = 0, open = 0, dummy;
-    auto free_bits = [&](int w) {  // of word w: not in use, inside the share, from first_page on
-        const int p = first + w * 32;
-        uint32_t m = ~sh.used[w];
-        if (end - p < 32) m &= (1u << (end - p)) - 1;
-        if (from_page > p) m &= from_page - p >= 32 ? 0u : ~((1u << (from_page - p)) - 1);
-        return m;
-    };
-    for (int w = w0; w < w1; ++w) {
-        in += __popc(sh.used[w]);
-        open += __popc(free_bits(w));
-    }
-    int u = used_before + block_exclusive(in, sh.sums, &dummy), f = free_before + block_exclusive(open, sh.sums, &dummy);
-    for (int w = w0; w < w1; ++w) {
-        const int p = first + w * 32;
-        if (used - u - __popc(sh.used[w]) < lists) {  // (the word's last page in use is of this rank from the top)
-            for (uint32_t m = sh.used[w]; m; m &= m - 1, ++u) {
-                const int i = used - 1 - u;
-                if (i < lists && HAWK_IN_BOUNDS(P.dev_status, i, lists)) P.from[i] = p + __ffs(m) - 1;
-            }
-        } else {
-            u += __popc(sh.used[w]);
+    // ---- the lowest free pages and the highest in use, by rank; a word a thread
+    const int border = from_page + used, lists = P.moves + 1;
+    int behind = 0, u = 0, f = 0;
+    for (int w0 = 0; w0 < words; w0 += kBookThreads) {
+        const int w = w0 + tid, p = first + w * 32;
+        uint32_t in = 0, open = 0;
+        if (w < words) {
+            in = sh.used[w];
+            open = ~in;  // of the share, from first_page on
+            if (end - p < 32) open &= (1u << (end - p)) - 1;
+            if (from_page > p) open &= from_page - p >= 32 ? 0u : ~((1u << (from_page - p)) - 1);
         }
-        for (uint32_t m = f < lists ? free_bits(w) : 0u; m; m &= m - 1, ++f)
-            if (f < lists && HAWK_IN_BOUNDS(P.dev_status, f, lists)) P.to[f] = p + __ffs(m) - 1;
+        uint32_t both;  // of kBookThreads words: 2^15 pages at most, so that the two numbers fit one
+        const uint32_t at = block_exclusive(static_cast<uint32_t>(__popc(in)) << 16 | __popc(open), sh.packed, &both);
+        int i_u = used_before + u + static_cast<int>(at >> 16), i_f = free_before + f + static_cast<int>(at & 0xffff);
+        u += static_cast<int>(both >> 16);
+        f += static_cast<int>(both & 0xffff);
+        for (uint32_t m = in; m; m &= m - 1, ++i_u) {
+            const int page = p + __ffs(m) - 1, i = used - 1 - i_u;  // rank from the top
+            behind += page >= border;
+            if (i < lists && HAWK_IN_BOUNDS(P.dev_status, i, lists)) {
+                P.from[i] = page;
+                P.place[page] = i;
+            }
+        }
+        for (uint32_t m = i_f < lists && p < border ? open : 0u; m; m &= m - 1, ++i_f)
+            if (i_f < lists && HAWK_IN_BOUNDS(P.dev_status, i_f, lists)) P.to[i_f] = p + __ffs(m) - 1;
     }
+    behind = block_sum(behind, sh.sums);
+    if (tid == 0) P.counts[rank] = behind;
     meet();
+    int moved = 0;
+#pragma unroll
+    for (int r = 0; r < kBookBlocks; ++r) moved += __ldcg(P.counts + r);
+    const int all_moves = moved;
+    moved = min(moved, P.moves);
 
-    // ---- moves: pairs of the lists for as long as they go down (once one does not, none behind it does)
-    const int pairs = min(P.moves, min(used, free_all));
-    int down = 0, moved;
-    for (int i = tid; i < pairs; i += kBookThreads) down += __ldcg(P.to + i) < __ldcg(P.from + i);
-    (void)block_exclusive(down, sh.sums, &moved);  // each block counts them for itself
+    // ---- moves
     for (int i = rank * kBookThreads + tid; i < P.moves; i += kBookBlocks * kBookThreads) {
         int a = -1, b = -1;
         if (i < moved) {
@@ -451,27 +517,23 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams 
             b = __ldcg(P.to + i);
             P.out_refs[b] = P.refs[a];
             P.out_refs[a] = 0;
-            P.place[a] = i;
         }
         P.copies[3 * i] = a;
         P.copies[3 * i + 1] = b;
         P.copies[3 * i + 2] = a < 0 ? 0 : static_cast<int>(P.div.page.d);
     }
-    if (P.top && rank == 0 && tid == 0) {
-        int top = from_page;  // behind the highest page in use: one that stayed, or the last that moved in
-        if (moved < used) top = max(top, __ldcg(P.from + moved) + 1);
-        if (moved > 0) top = max(top, __ldcg(P.to + moved - 1) + 1);
-        *P.top = top;
-    }
-    const int lowest = moved > 0 ? __ldcg(P.from + moved - 1) : INT_MAX;  // pages in use from here on have moved
-    meet();
+    if (P.top && rank == 0 && tid == 0) *P.top = moved == all_moves ? border : __ldcg(P.from + moved) + 1;
 
-    // ---- the new ids into the table
+    // ---- the new ids into the table: runs of 128 entries a warp
     if (moved == 0 && P.out_table == P.table) {
         report(P.dev_status, flags);
-        return;  // (moved is the same in all blocks, and no block reads another's shared memory any more)
+        return;
     }
-    for (int s = rank * kBookWarps + (tid >> 5); s < P.S; s += kBookBlocks * kBookWarps) {
+    const int lowest = moved > 0 ? __ldcg(P.from + moved - 1) : INT_MAX;  // pages in use from here on move
+    const int runs = P.S * static_cast<int>(P.div_runs.d);
+    for (int t = rank * kBookWarps + warp; t < runs; t += kBookBlocks * kBookWarps) {
+        uint32_t part;
+        const int s = static_cast<int>(P.div_runs.divmod(static_cast<uint32_t>(t), part)), j0 = static_cast<int>(part) * 128 + lane;
         const int kv = P.kv[s];
         if (kv < 0 || kv > cap) {
             flags |= HAWK_DEV_BAD_PREFIX;
@@ -479,15 +541,23 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams 
         }
         const int n = P.div.pages(kv);
         const size_t row = static_cast<size_t>(s) * P.W;
-        for (int j = lane; j < n; j += 32) {
-            int page = P.table[row + j];
-            if (page < 0 || page >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;
-            else if (page >= lowest) {
-                const int i = __ldcg(P.place + page);  // (no more than a guess for a page that the counts say is free)
-                if (i >= 0 && i < moved && __ldcg(P.from + i) == page) page = __ldcg(P.to + i);
+        int page[4], i[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) page[k] = j0 + 32 * k < n ? P.table[row + j0 + 32 * k] : 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            i[k] = -1;
+            if (page[k] < 0 || page[k] >= P.n_pages) flags |= HAWK_DEV_BAD_PAGE;
+            else if (page[k] >= lowest) i[k] = __ldcg(P.place + page[k]);  // (a guess, for a page that the counts say is free)
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (j0 + 32 * k >= n) continue;
+            if (page[k] >= lowest && page[k] < P.n_pages) {
+                if (i[k] >= 0 && i[k] < moved && __ldcg(P.from + i[k]) == page[k]) page[k] = __ldcg(P.to + i[k]);
                 else flags |= HAWK_DEV_BAD_PAGE;
             }
-            P.out_table[row + j] = page;
+            P.out_table[row + j0 + 32 * k] = page[k];
         }
     }
     report(P.dev_status, flags);
@@ -509,10 +579,10 @@ struct PageParams {
 
 constexpr int kCopyThreads = 256;
 constexpr int kCopyUnroll = 8;  // loads in flight a thread
-constexpr int kCopyPieces = 2 * kCopyThreads * kCopyUnroll;  // of a block: 64 KB
+constexpr int kCopyPieces = kCopyThreads * kCopyUnroll;  // of a block, 32 KB, or twice as many in calls of many blocks
 
-// Block (x, y, z): entry x; keys or values of layer y / 2; z: which kCopyPieces of the page.  Pieces are taken in the order of memory.
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(PageParams P, const int32_t *copies)
+// Block (x, y, z): entry x; keys or values of layer y / 2; z: which `share` pieces of the page.  Pieces are taken in the order of memory.
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(PageParams P, const int32_t *copies, uint32_t share)
 {
     hawk::allow_dependent_launch();
     hawk::grid_dependency_wait();
@@ -530,8 +600,8 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(PageParams P, const 
     const uint4 *from = layer + a * side.page;
     uint4 *to = layer + b * side.page;
     const uint32_t all = static_cast<uint32_t>(P.H) * P.page_size * P.pieces;
-    const uint32_t last = min(all, (blockIdx.z + 1) * static_cast<uint32_t>(kCopyPieces));
-    for (uint32_t c0 = blockIdx.z * static_cast<uint32_t>(kCopyPieces) + threadIdx.x; c0 < last; c0 += kCopyThreads * kCopyUnroll) {
+    const uint32_t last = min(all, (blockIdx.z + 1) * share);
+    for (uint32_t c0 = blockIdx.z * share + threadIdx.x; c0 < last; c0 += kCopyThreads * kCopyUnroll) {
         uint4 v[kCopyUnroll];
         long long at[kCopyUnroll];
 #pragma unroll
@@ -763,14 +833,14 @@ extern "C" hawk_status hawk_pages_fork(const hawk_pages_fork_args *a, int32_t *d
     if (streams == 0) return HAWK_OK;
     ForkParams P = {a->block_table, a->kv_len, a->parent, a->length, a->out_table, a->out_len, a->out_refs,
                     a->S, a->S_out, a->table_width, a->n_pages, make_div(a->page_size), dev_status};
-    return done(hawk_host::launch_dependent(fork_kernel, dim3(streams), dim3(128), 0, st, P));
+    return done(hawk_host::launch_dependent(fork_kernel, dim3(streams), dim3(kForkThreads), 0, st, P));
 }
 
 extern "C" size_t hawk_pages_compact_workspace_bytes(int n_pages, int max_moves)
 {
     if (n_pages < 1 || n_pages > kMaxPages || max_moves < 0) return 0;
     const size_t moves = max_moves < n_pages ? max_moves : n_pages;
-    return sizeof(int32_t) * (static_cast<size_t>(n_pages) + 2 * (moves + 1));
+    return sizeof(int32_t) * (static_cast<size_t>(n_pages) + 2 * (moves + 1) + kBookBlocks);
 }
 
 extern "C" hawk_status hawk_pages_compact(const hawk_pages_compact_args *a, int32_t *dev_status, hawk_stream_t stream)
@@ -779,13 +849,13 @@ extern "C" hawk_status hawk_pages_compact(const hawk_pages_compact_args *a, int3
     if (!a) return HAWK_ERR_NULL;
     const hawk_status chk = check_state(a->S, a->table_width, a->n_pages, a->page_size);
     if (chk != HAWK_OK) return chk;
-    if (a->first_page < 0 || a->max_moves < 0) return HAWK_ERR_SHAPE;
+    if (a->n_pages < 1 || a->first_page < 0 || a->first_page > a->n_pages || a->max_moves < 0) return HAWK_ERR_SHAPE;
     if (a->max_moves > kMaxPages) return HAWK_ERR_UNSUPPORTED;
     if (a->S > 0 && (!a->block_table || !a->kv_len || !a->out_table)) return HAWK_ERR_NULL;
-    if (a->n_pages > 0 && (!a->page_refs || !a->out_refs)) return HAWK_ERR_NULL;
+    if (!a->page_refs || !a->out_refs) return HAWK_ERR_NULL;
     if (a->max_moves > 0 && !a->copies) return HAWK_ERR_NULL;
     if (!aligned16(a->page_refs) || !aligned16(a->out_refs) || !aligned16(a->workspace)) return HAWK_ERR_ALIGN;
-    if (a->n_pages > 0 && (!a->workspace || a->workspace_bytes < hawk_pages_compact_workspace_bytes(a->n_pages, a->max_moves)))
+    if (!a->workspace || a->workspace_bytes < hawk_pages_compact_workspace_bytes(a->n_pages, a->max_moves))
         return HAWK_ERR_WORKSPACE;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
     static unsigned long long seen = 0;
@@ -802,10 +872,12 @@ extern "C" hawk_status hawk_pages_compact(const hawk_pages_compact_args *a, int3
     P.to = static_cast<int32_t *>(a->workspace);
     P.from = P.to + lists;
     P.place = P.from + lists;
+    P.counts = P.place + a->n_pages;
+    P.div_runs.set(static_cast<uint32_t>(a->table_width > 128 ? (a->table_width + 127) / 128 : 1));
     P.S = a->S;
     P.W = a->table_width;
     P.n_pages = a->n_pages;
-    P.first_page = a->first_page < a->n_pages ? a->first_page : a->n_pages;
+    P.first_page = a->first_page;
     P.moves = a->max_moves;
     P.div = make_div(a->page_size);
     P.dev_status = dev_status;
@@ -826,8 +898,11 @@ extern "C" hawk_status hawk_pages_copy(const hawk_page_tensors *pages, const int
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
     const PageParams P = page_params(*pages, dev_status);
     const long long all = static_cast<long long>(P.H) * P.page_size * P.pieces;
-    const dim3 grid(n_copies, 2 * pages->layers, static_cast<unsigned>((all + kCopyPieces - 1) / kCopyPieces));
-    return done(hawk_host::launch_dependent(copy_kernel, grid, dim3(kCopyThreads), 0, reinterpret_cast<cudaStream_t>(stream), P, copies));
+    // 4096 pages of 40 KB: 72 us with a page in two blocks, 68 in one; 16 pages of 98 KB: 5.2 us in twice as many blocks, 6.0 else
+    const long long share = static_cast<long long>(n_copies) * 2 * pages->layers >= 4 * 148 ? 2 * kCopyPieces : kCopyPieces;
+    const dim3 grid(n_copies, 2 * pages->layers, static_cast<unsigned>((all + share - 1) / share));
+    return done(hawk_host::launch_dependent(copy_kernel, grid, dim3(kCopyThreads), 0, reinterpret_cast<cudaStream_t>(stream), P, copies,
+                                            static_cast<uint32_t>(share)));
 }
 
 extern "C" hawk_status hawk_pages_keep(const hawk_pages_keep_args *a, int32_t *dev_status, hawk_stream_t stream)
