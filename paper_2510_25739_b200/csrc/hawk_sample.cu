@@ -8,7 +8,8 @@
 //   2. a sample of 4 ids a thread says between which two values the threshold lies (for top-p beside the row's mass in fp32, which a sample
 //      would miss when few ids have most of it);
 //   3. one pass over the weights: their sum above those values and below, for each warp, and a list of the ids between them;
-//   4. a histogram of the list finds the step that the threshold is in, and the step's members against each other the value;
+//   4. a histogram of the list finds the step that the threshold is in, and the step's members against each other the value (one warp does
+//      what is not for each id: all the warps doing it would take as long as a pass over the row);
 //   5. the sums of what stays tell the warp that the draw falls on, which finds the id.
 // With top-k and top-p, 2 to 4 run for each.  Where the list does not hold the threshold (the sample misled, or too many are equal), step 4
 // is done on the whole row, as many times as it takes (search()).  Neither changes a result.
@@ -16,7 +17,7 @@
 // say and a token does not depend on the launch.  fp32 sums would not do: with 16 thousand ids one draw in some hundred falls so near to a
 // border that their rounding decides it.
 //
-// A block holds 32768 ids at most; longer rows, and rows of calls with few of them, are shared by a cluster, whose blocks exchange
+// A block holds 40960 ids at most; longer rows, and rows of calls with few of them, are shared by a cluster, whose blocks exchange
 // histograms, members and sums through distributed shared memory.
 #include <climits>
 
@@ -31,9 +32,9 @@ using u64 = unsigned long long;
 constexpr int kBins = 256;       // steps of a histogram: 8 a lane, so that each warp sums them up for itself
 constexpr int kFinal = 256;      // members of a step that are ranked against each other
 constexpr int kList = 2048;      // ids that are looked at one by one, an equal share for each warp
-constexpr int kTooMany = 1 << 20;
 constexpr float kLowest = -3.402823466e38f;  // the lowest number: what is below is none
-constexpr int kMaxSlice = 32768; // ids of a row that a block holds
+constexpr int kMaxSlice = 40960; // ids of a row that a block holds
+constexpr int kMaxIds = 1 << 18;
 constexpr int kMaxCluster = 8;
 constexpr int kOneBits = 44;                // the largest logit's weight is 2^44; 2^18 such weights fit 64 bits
 constexpr double kOne = 17592186044416.0;
@@ -63,19 +64,24 @@ __device__ __forceinline__ int place_of(int bin) { return (bin & 7) * 32 + (bin 
 
 struct SampleShared {
     double table[kParts];  // 2^(i / kParts)
-    uint32_t hist[3][kBins];  // number of a step, or its mass in parts of 15 bits (of weights, whose 2^15 add up to less than 2^32)
+    uint32_t hist[3][kBins];  // number of a step, or its mass in parts of 15 bits (40960 of which add up to less than 2^32)
     uint32_t sample[kBins];
+    float window_lo, window_hi;  // what one warp finds for all: the list's window, ...
+    int bin, ok, complete;  // ... the step of the threshold, the mass or number above it, and whether there is one
+    u64 bin_above, target;
     float list_v[kList];   // the warps' shares one after the other
     u64 list_w[kList];
     u64 last_w[kFinal], all_w[kFinal];  // members of the last step: the block's, the row's
     float last_v[kFinal], all_v[kFinal];
-    u64 warp_a[32], warp_b[32], warp_c[32];
+    u64 warp_a[32], warp_b[32], warp_c[32], warp_d[32];
     uint32_t warp_lo[32], warp_hi[32];
+    int over;              // a warp's share of the list was too small
     float warp_f[32];
     Swap swap[6];  // one for each kind of exchange, so that a barrier lies between two uses of the same
     double rate, least;
-    int last, over, pick;
-    uint32_t tau_key;
+    int last, pick;
+    uint32_t last_lo, last_hi;  // keys of the last step's smallest and largest
+    float tau;
 };
 
 // Barrier of the row's blocks (lanes that a branch parted come together first).
@@ -198,17 +204,14 @@ private:
     float *vals;  // [m] logits of the block's ids, -inf around them; m is a multiple of 4
     int m, rank, flags = 0;
     int base, end;      // the warp's stretch of ids
-    int listed;         // the warp's, in its share of the list; more than fit: kShare + 1
+    int listed;         // its members of the list
     float mx, nothing;  // the largest; from `nothing`, 32 temperatures below it, down a weight is 0
     double rate;        // kParts / (temperature * ln 2)
 
-    struct Window {  // values that the threshold should lie between; the sums of a pass: from hi up and below lo (without the list)
-        float lo, hi;
-        u64 above, below, between;  // mass; `between`: the list's
-        int count, members;         // from hi up, in the list
-    };
-
     __device__ __forceinline__ bool shared() const { return P.cluster > 1; }
+    // Three times how far the rank of a threshold in a sample is off (and a little, for few).
+    __device__ __forceinline__ float margin_ranks(float rank) const { return each() > 1 ? 3.f * sqrtf(rank) + 4.f : 1.f; }
+    __device__ __forceinline__ int each() const { return (P.slice + 4095) / 4096; }  // logits that one of the sample stands for
     __device__ __forceinline__ void barrier() const
     {
         if (shared()) meet();
@@ -231,15 +234,17 @@ private:
         e = n >> kPartBits;
         return fma(f, r * fma(r, fma(r, c3, c2), c1), f);
     }
-    // ... in whole multiples of 2^-44.  (At `nothing` and below, -inf too, that is 0: e^-32 of them.)
-    __device__ __forceinline__ u64 weight(float l) const
+    // ... as a multiple of 2^-44, not yet whole.  The last bit is set, so that no sum of it is a tie: added to a number between 2^52 and 2^53 it
+    // counts as the nearest whole multiple, whatever the sum so far.  (At `nothing` and below, -inf too, that is 0: e^-32 of them.)
+    __device__ __forceinline__ double raw_weight(float l) const
     {
         int e;
         const double w = power(fmaxf(l, nothing), e);
-        constexpr double kWhole = 4503599627370496.0;  // 2^52: the sum's low bits are the nearest whole number
-        const double whole = __hiloint2double(__double2hiint(w) + (e + kOneBits) * (1 << 20), __double2loint(w)) + kWhole;
-        return static_cast<u64>(__double_as_longlong(whole)) & ((1ull << 52) - 1);
+        return __hiloint2double(__double2hiint(w) + (e + kOneBits) * (1 << 20), __double2loint(w) | 1);
     }
+    static constexpr double kWhole = 4503599627370496.0;  // 2^52, from where a thread's sums start: 256 weights fit on top
+    static __device__ __forceinline__ u64 whole(double sum) { return static_cast<u64>(__double_as_longlong(sum)) & ((1ull << 52) - 1); }
+    __device__ __forceinline__ u64 weight(float l) const { return whole(raw_weight(l) + kWhole); }
     // ... as a number, times `factor`
     __device__ __forceinline__ float share(float l, double factor) const
     {
@@ -259,11 +264,11 @@ private:
         s.n = static_cast<int>(hawk::ld_cluster_u32(at + 32));
         return s;
     }
-    // Lane's four logits of the warp's run from place j on (-inf behind its stretch).
-    __device__ __forceinline__ void four(int j, float (&l)[4]) const
+    // Lane's four logits of the run of 128 from place j on (-inf from `stop` on).
+    __device__ __forceinline__ void four(int j, int stop, float (&l)[4]) const
     {
         const int at = j + 4 * static_cast<int>(threadIdx.x & 31);
-        const float4 x = at < end ? *reinterpret_cast<const float4 *>(vals + at)
+        const float4 x = at < stop ? *reinterpret_cast<const float4 *>(vals + at)
                                   : make_float4(-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F);
         l[0] = x.x;
         l[1] = x.y;
@@ -272,13 +277,25 @@ private:
     }
     __device__ __forceinline__ int load(long long row, int first, int n, float scale, float &lo, float &hi);
     __device__ __forceinline__ void ends(float &lo, float &hi, int slot);
+    __device__ __forceinline__ void clear();
     __device__ __forceinline__ float mass_of_row();
     __device__ __forceinline__ void sample(const Steps &step);
-    __device__ __forceinline__ Window between_ranks(const Steps &step, float bottom, float above, float margin);
-    __device__ __forceinline__ Window between_masses(const Steps &step, float bottom, float from, float below, float margin);
-    template <bool kBelow>
-    __device__ __forceinline__ void pass(Window &w, float from);
-    template <bool kMass, bool kFromList>
+    template <typename N>
+    __device__ __forceinline__ void of_row(const uint32_t *hist, N (&part)[kBins / 32]) const;
+    __device__ __forceinline__ void between_ranks(float bottom, float above, float margin);
+    __device__ __forceinline__ void between_masses(const Steps &step, float bottom, float from, float below, float margin);
+    template <bool kMass>
+    __device__ __forceinline__ void pass(const Steps &step, float lo, float hi, float from, float least);
+    template <bool kMass>
+    __device__ __forceinline__ void count(int at, u64 weight);
+    template <bool kMass>
+    __device__ __forceinline__ void find_step(u64 above, u64 target, u64 count_above, float share);
+    __device__ __forceinline__ void push(float l, u64 weight, uint32_t &low, uint32_t &high);
+    __device__ __forceinline__ void range(uint32_t low, uint32_t high);
+    __device__ __forceinline__ bool finish(u64 target, float &low, float &high);
+    template <bool kMass>
+    __device__ __forceinline__ bool from_list(const Steps &step, float lo, float hi, u64 want, float share, float &tau, u64 &target, bool &complete);
+    template <bool kMass>
     __device__ __forceinline__ bool search(float lo, float hi, float bottom, u64 target, float &tau);
 };
 
@@ -288,10 +305,24 @@ __device__ __forceinline__ void Row<T, NT>::prepare()
 {
     for (int i = threadIdx.x; i < kParts; i += NT) sh.table[i] = exp2(static_cast<double>(i) / kParts);
     for (int i = threadIdx.x; i < kBins; i += NT) sh.sample[i] = 0;
+    clear();
+}
+
+// For a histogram and its last step.
+template <typename T, int NT>
+__device__ __forceinline__ void Row<T, NT>::clear()
+{
+    for (int i = threadIdx.x; i < 3 * kBins; i += NT) sh.hist[0][i] = 0;
+    if (threadIdx.x == 0) {
+        sh.last = 0;
+        sh.over = 0;
+        sh.last_lo = 0xffffffffu;
+        sh.last_hi = 0;
+    }
 }
 
 // The block's n logits from id v_begin + first on into vals[pad ..]; returns pad, by which the 16-byte pieces of memory lie on 16-byte places of vals.  hi: the
-// largest; lo: the smallest number among the pieces' first ones.
+// largest; lo: the smallest among some of them.
 template <typename T, int NT>
 __device__ __forceinline__ int Row<T, NT>::load(long long row, int first, int n, float scale, float &lo, float &hi)
 {
@@ -300,46 +331,46 @@ __device__ __forceinline__ int Row<T, NT>::load(long long row, int first, int n,
     const bool has = P.uncond != nullptr;
     const T *u = has ? static_cast<const T *>(P.uncond) + row * P.uncond_stride + P.v_begin + first : c;
     const int pad = static_cast<int>((reinterpret_cast<uintptr_t>(c) & 15u) / sizeof(T));
-    const bool alike = ((reinterpret_cast<uintptr_t>(c) ^ reinterpret_cast<uintptr_t>(u)) & 15u) == 0;  // pieces of both lie alike
     const int pieces = n > 0 ? (pad + n + kN - 1) / kN : 0;
     m = pieces * kN;
     hi = -CUDART_INF_F;
     lo = CUDART_INF_F;
-    auto take = [&](int at, const float (&x)[kN]) {
-#pragma unroll
-        for (int i = 0; i < kN; ++i) hi = fmaxf(hi, x[i]);
-        if (x[0] >= kLowest) lo = fminf(lo, x[0]);
-#pragma unroll
-        for (int i = 0; i < kN; i += 4) *reinterpret_cast<float4 *>(vals + at + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-    };
-    constexpr int kFlight = 4;
-    for (int q0 = threadIdx.x; q0 < pieces; q0 += NT * kFlight) {
+    // whole pieces, where those of both rows lie alike
+    const bool alike = ((reinterpret_cast<uintptr_t>(c) ^ reinterpret_cast<uintptr_t>(u)) & 15u) == 0;
+    const int q0 = pad > 0 ? 1 : 0, q1 = alike ? (pad + n) / kN : q0;
+    constexpr int kFlight = (sizeof(T) == 4 ? 4 : 2) * (NT <= 256 ? 2 : 1);
+    for (int q = q0 + threadIdx.x; q < q1; q += NT * kFlight) {
         Piece<T> pc[kFlight], pu[kFlight];
-        bool whole[kFlight];
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            const int q = q0 + k * NT, e = q * kN - pad;
-            whole[k] = alike && e >= 0 && e + kN <= n;
-            if (whole[k]) {
-                pc[k].raw = __ldcs(reinterpret_cast<const uint4 *>(c + e));
-                pu[k].raw = has ? __ldcs(reinterpret_cast<const uint4 *>(u + e)) : pc[k].raw;
+        for (int k = 0; k < kFlight; ++k)
+            if (q + k * NT < q1) {
+                pc[k].raw = __ldcs(reinterpret_cast<const uint4 *>(c + (q + k * NT) * kN - pad));
+                pu[k].raw = has ? __ldcs(reinterpret_cast<const uint4 *>(u + (q + k * NT) * kN - pad)) : pc[k].raw;
             }
-        }
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            const int q = q0 + k * NT, e = q * kN - pad;
-            if (q >= pieces) break;
-            float x[kN];
-            if (whole[k]) {
+        for (int k = 0; k < kFlight; ++k)
+            if (q + k * NT < q1) {
+                float x[kN];
 #pragma unroll
-                for (int i = 0; i < kN; ++i) x[i] = guided(pc[k].at(i), pu[k].at(i), has, scale, flags);
-            } else {
+                for (int i = 0; i < kN; ++i) {
+                    x[i] = guided(pc[k].at(i), pu[k].at(i), has, scale, flags);
+                    hi = fmaxf(hi, x[i]);
+                }
+                if (x[0] >= kLowest) lo = fminf(lo, x[0]);
 #pragma unroll
-                for (int i = 0; i < kN; ++i)
-                    x[i] = e + i >= 0 && e + i < n ? guided(to_f32(c[e + i]), to_f32(u[e + i]), has, scale, flags) : -CUDART_INF_F;
+                for (int i = 0; i < kN; i += 4)
+                    *reinterpret_cast<float4 *>(vals + (q + k * NT) * kN + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
             }
-            take(q * kN, x);
-        }
+    }
+    // what is left at the ends (or all of it), one by one
+    const int done0 = q1 > q0 ? q0 * kN : 0, done1 = q1 > q0 ? q1 * kN : 0;
+    for (int j = threadIdx.x; j < m - (done1 - done0); j += NT) {
+        const int at = j < done0 ? j : j + (done1 - done0), e = at - pad;
+        float x = -CUDART_INF_F;
+        if (e >= 0 && e < n) x = guided(to_f32(c[e]), to_f32(u[e]), has, scale, flags);
+        hi = fmaxf(hi, x);
+        if (x >= kLowest) lo = fminf(lo, x);
+        vals[at] = x;
     }
     return pad;
 }
@@ -379,45 +410,59 @@ __device__ __forceinline__ float Row<T, NT>::mass_of_row()
     float mass = 0.f;
     for (int j = base; j < end; j += 128) {
         float l[4];
-        four(j, l);
+        four(j, end, l);
         mass += (hawk::fast_exp2((l[0] - mx) * octaves) + hawk::fast_exp2((l[1] - mx) * octaves)) +
                 (hawk::fast_exp2((l[2] - mx) * octaves) + hawk::fast_exp2((l[3] - mx) * octaves));
     }
     return hawk::warp_sum(mass);
 }
 
-// Four logits a thread, or all if there are no more, to the histogram of the sample.
+// One logit in `each` (of the block's P.slice), at most 4096 of them, in quads, to the histogram of the sample.
 template <typename T, int NT>
 __device__ __forceinline__ void Row<T, NT>::sample(const Steps &step)
 {
-    const int per = (P.slice + NT - 1) / NT, at = per > 4 ? static_cast<int>(threadIdx.x) * per & ~3 : 4 * static_cast<int>(threadIdx.x);
-    if (at < m) {
-        const float4 l = *reinterpret_cast<const float4 *>(vals + at);
-        if (l.x >= kLowest) atomicAdd(&sh.sample[place_of(step(l.x))], 1u);
-        if (l.y >= kLowest) atomicAdd(&sh.sample[place_of(step(l.y))], 1u);
-        if (l.z >= kLowest) atomicAdd(&sh.sample[place_of(step(l.z))], 1u);
-        if (l.w >= kLowest) atomicAdd(&sh.sample[place_of(step(l.w))], 1u);
+    for (int q = threadIdx.x; q < 1024; q += NT) {
+        const int at = 4 * each() * q;
+        if (at < m) {
+            const float4 l = *reinterpret_cast<const float4 *>(vals + at);
+            if (l.x >= kLowest) atomicAdd(&sh.sample[place_of(step(l.x))], 1u);
+            if (l.y >= kLowest) atomicAdd(&sh.sample[place_of(step(l.y))], 1u);
+            if (l.z >= kLowest) atomicAdd(&sh.sample[place_of(step(l.z))], 1u);
+            if (l.w >= kLowest) atomicAdd(&sh.sample[place_of(step(l.w))], 1u);
+        }
     }
     __syncwarp();
 }
 
-// Values between which the logit of rank `above` of the sample lies, by `margin` ranks on either side.  Every warp for itself (behind a barrier).
+// The lane's eight steps of a histogram, of all the row's blocks (eight loads in flight: one from another block takes some 700 cycles).
 template <typename T, int NT>
-__device__ __forceinline__ typename Row<T, NT>::Window Row<T, NT>::between_ranks(const Steps &step, float bottom, float above, float margin)
+template <typename N>
+__device__ __forceinline__ void Row<T, NT>::of_row(const uint32_t *hist, N (&part)[kBins / 32]) const
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < kBins / 32; ++i) part[i] = shared() ? 0 : hist[i * 32 + lane];
+    if (!shared()) return;
+    for (int r = 0; r < P.cluster; ++r) {
+        const uint32_t at = hawk::map_shared_to_cta(hist + lane, r);
+        uint32_t x[kBins / 32];
+#pragma unroll
+        for (int i = 0; i < kBins / 32; ++i) x[i] = hawk::ld_cluster_u32(at + 128 * i);
+#pragma unroll
+        for (int i = 0; i < kBins / 32; ++i) part[i] += x[i];
+    }
+}
+
+// Values between which the logit of rank `above` of the sample lies, by `margin` ranks on either side (one warp, behind a barrier).
+template <typename T, int NT>
+__device__ __forceinline__ void Row<T, NT>::between_ranks(float bottom, float above, float margin)
 {
     constexpr int kPer = kBins / 32;
     const int lane = threadIdx.x & 31;
     uint32_t part[kPer], sum = 0;
+    of_row(sh.sample, part);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        part[i] = 0;
-        if (shared()) {
-            for (int r = 0; r < P.cluster; ++r) part[i] += hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.sample[i * 32 + lane], r));
-        } else {
-            part[i] = sh.sample[i * 32 + lane];
-        }
-        sum += part[i];
-    }
+    for (int i = 0; i < kPer; ++i) sum += part[i];
     uint32_t run = warp_inclusive(sum) - sum;
     const float low = above - margin, high = above + margin;  // (a low of 1 or less: even the largest may be it)
     int b1 = low <= 1.f ? 0 : kBins, b2 = kBins;
@@ -429,275 +474,383 @@ __device__ __forceinline__ typename Row<T, NT>::Window Row<T, NT>::between_ranks
     }
     b1 = __reduce_min_sync(0xffffffffu, b1);
     b2 = __reduce_min_sync(0xffffffffu, b2);
-    const float wide = (mx - bottom) / kBins;
-    Window w;
-    w.hi = b1 > 0 && b1 < kBins ? mx - wide * b1 : CUDART_INF_F;
-    w.lo = b2 < kBins - 1 ? mx - wide * (b2 + 1) : kLowest;
-    return w;
+    if (lane == 0) {
+        const float wide = (mx - bottom) / kBins;
+        sh.window_hi = b1 > 0 && b1 < kBins ? mx - wide * b1 : CUDART_INF_F;
+        sh.window_lo = b2 < kBins - 1 ? mx - wide * (b2 + 1) : kLowest;
+    }
 }
 
 // Values between which the logits from `from` up to the threshold have the mass `below` together, as the sample has it, with a share `margin` of
-// it on either side.  Every warp for itself (behind a barrier).
+// it on either side, and margin_ranks(rank) of the sample's ranks (near the top, few of the sample have most of the mass).  One warp, behind a
+// barrier.
 template <typename T, int NT>
-__device__ __forceinline__ typename Row<T, NT>::Window Row<T, NT>::between_masses(const Steps &step, float bottom, float from, float below,
-                                                                                 float margin)
+__device__ __forceinline__ void Row<T, NT>::between_masses(const Steps &step, float bottom, float from, float below, float margin)
 {
     constexpr int kPer = kBins / 32;
     const int lane = threadIdx.x & 31, last = step(from);
     const float wide = (mx - bottom) / kBins, octaves = static_cast<float>(rate / kParts);
-    const int per = (P.slice + NT - 1) / NT;
-    const float each = per > 4 ? per * 0.25f : 1.f;
     float part[kPer], sum = 0.f;
+    uint32_t number[kPer], numbers = 0;
+    of_row(sh.sample, number);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int b = lane * kPer + i;
-        uint32_t count = 0;
-        if (shared()) {
-            for (int r = 0; r < P.cluster; ++r) count += hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.sample[i * 32 + lane], r));
-        } else {
-            count = sh.sample[i * 32 + lane];
-        }
-        part[i] = b <= last && count > 0 ? each * count * hawk::fast_exp2(-wide * octaves * (b + 0.5f)) : 0.f;
+        part[i] = b <= last && number[i] > 0 ? each() * number[i] * hawk::fast_exp2(-wide * octaves * (b + 0.5f)) : 0.f;
         sum += part[i];
+        numbers += number[i];
     }
     // (sums from the far end up: the near end's few large weights are what a sample knows least)
-    float tail = 0.f;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const float x = __shfl_down_sync(0xffffffffu, sum, o);
         if (lane + o < 32) sum += x;
     }
-    tail = __shfl_down_sync(0xffffffffu, sum, 1);
+    float tail = __shfl_down_sync(0xffffffffu, sum, 1);
     if (lane == 31) tail = 0.f;
-    int b1 = kBins, b2 = kBins;
+    int b1 = kBins, b2 = kBins, middle = kBins;
 #pragma unroll
     for (int i = kPer - 1; i >= 0; --i) {  // tail: what lies behind step lane * kPer + i
         if (tail <= below * (1.f + margin)) b1 = lane * kPer + i;
+        if (tail <= below) middle = lane * kPer + i;
         if (tail <= below * (1.f - margin)) b2 = lane * kPer + i;
         tail += part[i];
     }
     b1 = __reduce_min_sync(0xffffffffu, b1);
     b2 = __reduce_min_sync(0xffffffffu, b2);
-    Window w;
-    w.hi = b1 > 0 && b1 < kBins ? mx - wide * b1 : CUDART_INF_F;
-    w.lo = b2 < kBins - 1 ? mx - wide * (b2 + 1) : kLowest;
-    return w;
+    middle = __reduce_min_sync(0xffffffffu, middle);
+    uint32_t run = warp_inclusive(numbers) - numbers, rank = 0;
+    const uint32_t before = run;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        run += number[i];
+        if (lane * kPer + i == middle) rank = run;
+    }
+    rank = __reduce_max_sync(0xffffffffu, rank);
+    const float low = rank - margin_ranks(rank), high = rank + margin_ranks(rank);
+    int r1 = low <= 1.f ? 0 : kBins, r2 = kBins;
+    run = before;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        run += number[i];
+        if (run >= low) r1 = min(r1, lane * kPer + i);
+        if (run >= high) r2 = min(r2, lane * kPer + i);
+    }
+    b1 = min(b1, __reduce_min_sync(0xffffffffu, r1));
+    b2 = max(b2, __reduce_min_sync(0xffffffffu, r2));
+    if (lane == 0) {
+        sh.window_hi = b1 > 0 && b1 < kBins ? mx - wide * b1 : CUDART_INF_F;
+        sh.window_lo = b2 < kBins - 1 ? mx - wide * (b2 + 1) : kLowest;
+    }
 }
 
-// One pass over the weights of the logits from `from` on: the sums of the window, its members to the list; the warp's sum of what lies above it
-// stays in warp_a.  Barriers of the row lie in it.
+// One more of a step: its number, or its weight in three parts whose sums stay below 2^32.
 template <typename T, int NT>
-template <bool kBelow>
-__device__ __forceinline__ void Row<T, NT>::pass(Window &w, float from)
+template <bool kMass>
+__device__ __forceinline__ void Row<T, NT>::count(int at, u64 w)
+{
+    if (!kMass) {
+        atomicAdd(&sh.hist[0][at], 1u);
+    } else {
+        constexpr uint32_t kPart = (1u << 15) - 1;
+        atomicAdd(&sh.hist[0][at], static_cast<uint32_t>(w) & kPart);
+        atomicAdd(&sh.hist[1][at], static_cast<uint32_t>(w >> 15) & kPart);
+        atomicAdd(&sh.hist[2][at], static_cast<uint32_t>(w >> 30));
+    }
+}
+
+// One pass over the weights of the logits from `from` on: those from lo up to hi go to the list and, by their step, to the histogram; for the
+// others the warp's sums of what lies above (warp_a, and its number in warp_lo) and, for top-p, below (warp_b).  warp_d: the part of the sum above
+// that min-p leaves, which keeps what is not below `least`.
+template <typename T, int NT>
+template <bool kMass>
+__device__ __forceinline__ void Row<T, NT>::pass(const Steps &step, float lo, float hi, float from, float least)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    u64 above = 0, below = 0, between = 0;
-    u64 marks = 0;  // which of the lane's are members
-    int count = 0, at = 0;
-    for (int j = base; j < end; j += 128, at += 4) {
-        float l[4];
-        four(j, l);
+    double above = kWhole, below = kWhole, stays = kWhole;
+    const bool cuts = least > hi;
+    int up_count = 0;
+    listed = 0;
+    // 8 runs of 128 at a time, so that the marks of members fit 32 bits (a lane's sums take 256 weights: 40960 / 8 warps / 32 lanes are 160)
+    for (int j0 = base; j0 < end; j0 += 8 * 128) {
+        uint32_t marks = 0;
+        const int stop = min(end, j0 + 8 * 128);
+        for (int j = j0; j < stop; j += 128) {
+            float l[4];
+            four(j, end, l);
+            uint32_t in = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const u64 x = weight(l[k]);
-            const bool up = l[k] >= w.hi, low = l[k] < w.lo;
-            if (up) above += x;
-            if (up) ++count;
-            if (kBelow) {
-                if (low && l[k] >= from) below += x;
-                if (!up && !low && l[k] >= from) marks |= 1ull << (at + k);
-            } else {
-                if (!up && !low) marks |= 1ull << (at + k);
+            for (int k = 0; k < 4; ++k) {
+                const double x = raw_weight(l[k]);
+                const bool up = l[k] >= hi, member = !up && l[k] >= lo && (!kMass || l[k] >= from);
+                if (up) above += x;
+                if (cuts && l[k] >= least) stays += x;
+                if (!kMass && up) ++up_count;
+                if (kMass && !up && !member && l[k] >= from) below += x;
+                if (member) in |= 1u << k;
             }
+            marks |= in << ((j - j0) >> 5);
         }
-    }
-    const int mine = __popcll(marks), sum = warp_inclusive(mine);
-    listed = __shfl_sync(0xffffffffu, sum, 31);
-    for (int to = sum - mine; marks; marks &= marks - 1, ++to) {
-        const int i = __ffsll(marks) - 1;
-        const float l = vals[base + (i >> 2) * 128 + 4 * lane + (i & 3)];
-        const u64 x = weight(l);
-        between += x;
-        if (to < kShare) {
-            sh.list_v[warp * kShare + to] = l;
-            sh.list_w[warp * kShare + to] = x;
-        }
-    }
-    __syncwarp();
-    above = warp_sum(above);
-    between = warp_sum(between);
-    if (kBelow) below = warp_sum(below);
-    count = __reduce_add_sync(0xffffffffu, count);
-    __syncthreads();  // (the sums of the pass before have been read)
-    if (lane == 0) {
-        sh.warp_a[warp] = above;
-        sh.warp_b[warp] = below;
-        sh.warp_c[warp] = between;
-        sh.warp_lo[warp] = count;
-        sh.warp_hi[warp] = listed > kShare ? kTooMany : listed;  // (a sum that says that some did not fit)
-    }
-    for (int i = threadIdx.x; i < 3 * kBins; i += NT) sh.hist[0][i] = 0;
-    if (threadIdx.x == 0) {
-        sh.last = 0;
-        sh.tau_key = 0;
-    }
-    __syncthreads();
-    w.above = warp_sum(lane < NW ? sh.warp_a[lane] : 0ull);
-    w.below = kBelow ? warp_sum(lane < NW ? sh.warp_b[lane] : 0ull) : 0ull;
-    w.between = warp_sum(lane < NW ? sh.warp_c[lane] : 0ull);
-    w.count = __reduce_add_sync(0xffffffffu, lane < NW ? sh.warp_lo[lane] : 0u);
-    w.members = __reduce_add_sync(0xffffffffu, lane < NW ? sh.warp_hi[lane] : 0u);
-    if (shared()) {
-        if (threadIdx.x == 0) sh.swap[1] = {w.above, w.below, w.between, __int_as_float(w.count), 0.f, w.members};
-        meet();
-        w.above = w.below = w.between = 0;
-        w.count = w.members = 0;
-        for (int r = 0; r < P.cluster; ++r) {
-            const Swap s = of(1, r);
-            w.above += s.a;
-            w.below += s.b;
-            w.between += s.c;
-            w.count += __float_as_int(s.lo);
-            w.members += s.n;
-        }
-    }
-}
-
-// The largest value tau in [lo, hi] for which the logits from it to hi reach the target, their number or their mass; among the list (whose sums
-// have to reach it; false if its last step has too many members), or among the block's whole row (always found, in as many rounds as it
-// takes: a round leaves one value out at least).  The first round's steps start from `bottom`, the last of them takes what is below.  The same in all blocks of the row.  hist, last and tau_key are clear for the list.
-template <typename T, int NT>
-template <bool kMass, bool kFromList>
-__device__ __forceinline__ bool Row<T, NT>::search(float lo, float hi, float bottom, u64 target, float &tau)
-{
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int begin = kFromList ? warp * kShare : base, stop = kFromList ? begin + listed : end;
-    const float *from = kFromList ? sh.list_v : vals;
-    auto weigh = [&](int i, float l) -> u64 { return !kMass ? 1ull : kFromList ? sh.list_w[i] : weight(l); };
-    u64 above = 0;
-    while (lo < hi) {
-        const Steps step(fmaxf(lo, bottom), hi);
-        if (!kFromList) {
-            barrier();  // (everybody has read what the round before, or the search before, left in sh)
-            for (int i = tid; i < 3 * kBins; i += NT) sh.hist[0][i] = 0;
-            if (tid == 0) {
-                sh.last = 0;
-                sh.tau_key = 0;
-            }
-            __syncthreads();
-        }
-        for (int i = begin + lane; i < stop; i += 32) {
-            const float l = from[i];
-            if (l >= lo && l <= hi) {
-                const int at = place_of(step(l));
-                const u64 x = weigh(i, l);
-                if (!kMass) {
-                    atomicAdd(&sh.hist[0][at], 1u);
-                } else {
-                    constexpr uint32_t kPart = (1u << 15) - 1;
-                    atomicAdd(&sh.hist[0][at], static_cast<uint32_t>(x) & kPart);
-                    atomicAdd(&sh.hist[1][at], static_cast<uint32_t>(x >> 15) & kPart);
-                    atomicAdd(&sh.hist[2][at], static_cast<uint32_t>(x >> 30));
-                }
+        const int mine = __popc(marks), sum = warp_inclusive(mine);
+        for (int to = listed + sum - mine; marks; marks &= marks - 1, ++to) {
+            const int i = __ffs(marks) - 1;
+            const float l = vals[j0 + (i >> 2) * 128 + 4 * lane + (i & 3)];
+            const u64 x = weight(l);
+            count<kMass>(place_of(step(l)), x);
+            if (to < kShare) {
+                sh.list_v[warp * kShare + to] = l;
+                sh.list_w[warp * kShare + to] = x;
             }
         }
         __syncwarp();
-        barrier();
-        // the step that the target is reached in: every warp for itself
-        constexpr int kPer = kBins / 32;
-        u64 part[kPer], sum = 0;
+        listed += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    const u64 a = warp_sum(whole(above)), d = cuts ? warp_sum(whole(stays)) : a;
+    u64 b = 0;
+    if (kMass) b = warp_sum(whole(below));
+    if (!kMass) up_count = __reduce_add_sync(0xffffffffu, up_count);
+    if (lane == 0) {
+        sh.warp_a[warp] = a;
+        sh.warp_b[warp] = b;
+        sh.warp_d[warp] = d;
+        sh.warp_lo[warp] = up_count;
+        if (listed > kShare) sh.over = 1;
+    }
+}
+
+// The step of the histogram that the target is reached in (one warp, behind a barrier): bin, and the number or mass above it.  share >= 0: the target is
+// that share of above, the histogram and `rest`.
+template <typename T, int NT>
+template <bool kMass>
+__device__ __forceinline__ void Row<T, NT>::find_step(u64 above, u64 target, u64 rest, float share)
+{
+    constexpr int kPer = kBins / 32;
+    const int lane = threadIdx.x & 31;
+    u64 part[kPer], sum = 0;
+    of_row(sh.hist[0], part);
+    if (kMass) {
+        u64 more[kPer];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            part[i] = 0;
+        for (int k = 1; k < 3; ++k) {
+            of_row(sh.hist[k], more);
 #pragma unroll
-            for (int k = 0; k < (kMass ? 3 : 1); ++k) {
-                u64 x = 0;
-                if (shared()) {
-                    for (int r = 0; r < P.cluster; ++r) x += hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.hist[k][i * 32 + lane], r));
-                } else {
-                    x = sh.hist[k][i * 32 + lane];
-                }
-                part[i] += x << (15 * k);
-            }
-            sum += part[i];
+            for (int i = 0; i < kPer; ++i) part[i] += more[i] << (15 * k);
         }
-        u64 run = above + warp_inclusive(sum) - sum, at_run = 0;
-        int bin = kBins - 1;
-        bool here = false;
+    }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (run < target && run + part[i] >= target) {
-                bin = lane * kPer + i;
-                at_run = run;
-                here = true;
-            }
-            run += part[i];
+    for (int i = 0; i < kPer; ++i) sum += part[i];
+    u64 run = above + warp_inclusive(sum) - sum;
+    if (share >= 0.f) target = target_of(static_cast<double>(share), __shfl_sync(0xffffffffu, run + sum, 31) + rest);
+    int bin = -1;
+    u64 at_run = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (run < target && run + part[i] >= target) {
+            bin = lane * kPer + i;
+            at_run = run;
         }
-        const uint32_t who = __ballot_sync(0xffffffffu, here);
-        if (who == 0) return false;  // (the same in all warps and blocks)
-        bin = __shfl_sync(0xffffffffu, bin, __ffs(who) - 1);
-        above = __shfl_sync(0xffffffffu, at_run, __ffs(who) - 1);
-        // its members
-        float low = CUDART_INF_F, high = -CUDART_INF_F;
-        for (int i = begin + lane; i < stop; i += 32) {
-            const float l = from[i];
-            if (l >= lo && l <= hi && step(l) == bin) {
-                const int at = atomicAdd(&sh.last, 1);
-                if (at < kFinal) {
-                    sh.last_v[at] = l;
-                    sh.last_w[at] = weigh(i, l);
-                }
-                low = fminf(low, l);
-                high = fmaxf(high, l);
+        run += part[i];
+    }
+    const uint32_t who = __ballot_sync(0xffffffffu, bin >= 0);
+    if (lane == (who ? __ffs(who) - 1 : 0)) {
+        sh.bin = bin;
+        sh.bin_above = at_run;
+        sh.ok = who != 0;
+        sh.target = target;
+    }
+}
+
+// One more member of the last step.
+template <typename T, int NT>
+__device__ __forceinline__ void Row<T, NT>::push(float l, u64 w, uint32_t &low, uint32_t &high)
+{
+    const int at = atomicAdd(&sh.last, 1);
+    if (at < kFinal) {
+        sh.last_v[at] = l;
+        sh.last_w[at] = w;
+    }
+    low = min(low, key_of(l));
+    high = max(high, key_of(l));
+}
+
+// The lanes' smallest and largest members, to those of the block.
+template <typename T, int NT>
+__device__ __forceinline__ void Row<T, NT>::range(uint32_t low, uint32_t high)
+{
+    __syncwarp();
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    if ((threadIdx.x & 31) == 0 && low <= high) {
+        atomicMin(&sh.last_lo, low);
+        atomicMax(&sh.last_hi, high);
+    }
+}
+
+// The value at which the last step's members reach the target, to sh.tau (all threads; barriers lie in it); false if there are too many, of
+// values from low to high.
+template <typename T, int NT>
+__device__ __forceinline__ bool Row<T, NT>::finish(u64 target, float &low, float &high)
+{
+    const int tid = threadIdx.x, lane = tid & 31;
+    __syncthreads();
+    int members = sh.last;
+    const float *v = sh.last_v;
+    const u64 *w = sh.last_w;
+    low = value_of(sh.last_lo);  // (nonsense without members)
+    high = value_of(sh.last_hi);
+    if (shared()) {
+        if (tid == 0) {
+            sh.swap[2].n = members;
+            sh.swap[2].lo = members > 0 ? low : CUDART_INF_F;
+            sh.swap[2].hi = members > 0 ? high : -CUDART_INF_F;
+        }
+        meet();
+        int before[kMaxCluster + 1];
+        before[0] = 0;
+        low = CUDART_INF_F;
+        high = -CUDART_INF_F;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) {
+            before[r + 1] = before[r];
+            if (r < P.cluster) {
+                const Swap x = of(2, r);
+                before[r + 1] += x.n;
+                low = fminf(low, x.lo);
+                high = fmaxf(high, x.hi);
             }
         }
-        __syncthreads();
-        int members = sh.last;
-        const float *v = sh.last_v;
-        const u64 *w = sh.last_w;
-        if (shared()) {
-            if (tid == 0) sh.swap[2].n = members;
-            meet();
-            int before[kMaxCluster + 1];
-            before[0] = 0;
+        members = before[kMaxCluster];
+        if (members <= kFinal) {
 #pragma unroll
             for (int r = 0; r < kMaxCluster; ++r)
-                before[r + 1] = before[r] + (r < P.cluster ? static_cast<int>(hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.swap[2].n, r))) : 0);
-            members = before[kMaxCluster];
-            if (members <= kFinal) {
-#pragma unroll
-                for (int r = 0; r < kMaxCluster; ++r)
-                    for (int i = tid; i < before[r + 1] - before[r]; i += NT) {
-                        sh.all_v[before[r] + i] = __uint_as_float(hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.last_v[i], r)));
-                        sh.all_w[before[r] + i] = hawk::ld_cluster_u64(hawk::map_shared_to_cta(&sh.last_w[i], r));
-                    }
-                __syncthreads();
-                v = sh.all_v;
-                w = sh.all_w;
-            }
-        }
-        if (members <= kFinal) {
-            // against each other, 8 lanes a member
-            for (int i0 = 0; i0 < members; i0 += NT / 8) {  // (the same rounds for all lanes)
-                const int i = i0 + tid / 8;
-                const float mine = i < members ? v[i] : CUDART_INF_F;
-                u64 reach = 0;
-                for (int k = tid & 7; k < members; k += 8)
-                    if (v[k] >= mine) reach += w[k];
-                reach += __shfl_xor_sync(0xffffffffu, reach, 1);
-                reach += __shfl_xor_sync(0xffffffffu, reach, 2);
-                reach += __shfl_xor_sync(0xffffffffu, reach, 4);
-                if ((tid & 7) == 0 && i < members && above + reach >= target) atomicMax(&sh.tau_key, key_of(mine));
-            }
+                for (int i = tid; i < before[r + 1] - before[r]; i += NT) {
+                    sh.all_v[before[r] + i] = __uint_as_float(hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.last_v[i], r)));
+                    sh.all_w[before[r] + i] = hawk::ld_cluster_u64(hawk::map_shared_to_cta(&sh.last_w[i], r));
+                }
             __syncthreads();
-            tau = value_of(sh.tau_key);
+            v = sh.all_v;
+            w = sh.all_w;
+        }
+    }
+    if (low == high) {  // (16-bit logits are equal by the hundred)
+        if (tid == 0) sh.tau = low;
+    } else if (members > kFinal) {
+        return false;
+    } else if (tid < 32) {  // against each other, a member a lane
+        float best = -CUDART_INF_F;
+        const u64 above = sh.bin_above;
+        for (int i = lane; i < members; i += 32) {
+            const float mine = v[i];
+            u64 reach = above;
+            for (int k = 0; k < members; ++k)
+                if (v[k] >= mine) reach += w[k];
+            if (reach >= target) best = fmaxf(best, mine);
+        }
+        __syncwarp();
+        best = value_of(__reduce_max_sync(0xffffffffu, key_of(best)));
+        if (lane == 0) sh.tau = best;
+    }
+    __syncthreads();
+    return true;
+}
+
+// The threshold among the list that a pass has made of the logits from lo up to hi: the largest value from which on the logits reach `want`, or the
+// share of the mass (share >= 0), which becomes the target.  False if it is not among them.  complete: the list has them all.  The same in all
+// blocks of the row.
+template <typename T, int NT>
+template <bool kMass>
+__device__ __forceinline__ bool Row<T, NT>::from_list(const Steps &step, float lo, float hi, u64 want, float share, float &tau, u64 &target, bool &complete)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __syncthreads();
+    if (warp == 0 || shared()) {
+        u64 above = kMass ? warp_sum(lane < NW ? sh.warp_a[lane] : 0ull) : __reduce_add_sync(0xffffffffu, lane < NW ? sh.warp_lo[lane] : 0u);
+        u64 below = kMass ? warp_sum(lane < NW ? sh.warp_b[lane] : 0ull) : 0ull;
+        int over = sh.over;
+        if (shared()) {
+            if (threadIdx.x == 0) {
+                sh.swap[1].a = above;
+                sh.swap[1].b = below;
+                sh.swap[1].n = over;
+            }
+            meet();
+            above = below = 0;
+            over = 0;
+            if (warp == 0)
+                for (int r = 0; r < P.cluster; ++r) {
+                    const Swap s = of(1, r);
+                    above += s.a;
+                    below += s.b;
+                    over |= s.n;
+                }
+        }
+        if (warp == 0) {
+            find_step<kMass>(above, want, below, share);
+            if (lane == 0) sh.complete = !over;
+        }
+    }
+    __syncthreads();
+    target = sh.target;
+    complete = sh.complete != 0;
+    if (!sh.ok) return false;
+    const int bin = sh.bin;
+    uint32_t low = 0xffffffffu, high = 0;
+    if (complete) {
+        for (int i = lane; i < listed; i += 32) {
+            const float l = sh.list_v[warp * kShare + i];
+            if (l >= lo && step(l) == bin) push(l, kMass ? sh.list_w[warp * kShare + i] : 1, low, high);
+        }
+    } else {
+        for (int j = base + lane; j < end; j += 32) {
+            const float l = vals[j];
+            if (l >= lo && l < hi && step(l) == bin) push(l, kMass ? weight(l) : 1, low, high);
+        }
+    }
+    range(low, high);
+    float least, most;
+    if (!finish(target, least, most)) return false;
+    tau = sh.tau;
+    return true;
+}
+
+// The largest value tau in [lo, hi] for which the logits from it to hi reach the target, their number or their mass; false if all do not.  Any
+// distribution of values, as many rounds as it takes (a round leaves one value out at least).  The first round's steps start from
+// `bottom`, the last of them takes what is below.  The same in all blocks of the row.
+template <typename T, int NT>
+template <bool kMass>
+__device__ __forceinline__ bool Row<T, NT>::search(float lo, float hi, float bottom, u64 target, float &tau)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    u64 above = 0;
+    while (lo < hi) {
+        const Steps step(fmaxf(lo, bottom), hi);
+        barrier();  // (everybody has read what the round before, or the search before, left in sh)
+        clear();
+        __syncthreads();
+        for (int j = base + lane; j < end; j += 32) {
+            const float l = vals[j];
+            if (l >= lo && l <= hi) count<kMass>(place_of(step(l)), kMass ? weight(l) : 1);
+        }
+        __syncwarp();
+        barrier();
+        if (warp == 0) find_step<kMass>(above, target, 0, -1.f);
+        __syncthreads();
+        if (!sh.ok) return false;
+        const int bin = sh.bin;
+        above = sh.bin_above;
+        uint32_t low = 0xffffffffu, high = 0;
+        for (int j = base + lane; j < end; j += 32) {
+            const float l = vals[j];
+            if (l >= lo && l <= hi && step(l) == bin) push(l, kMass ? weight(l) : 1, low, high);
+        }
+        range(low, high);
+        float least, most;
+        if (finish(target, least, most)) {
+            tau = sh.tau;
             return true;
         }
-        if (kFromList) return false;
-        ends(low, high, 3);
-        lo = low;
-        hi = high;
-        bottom = low;
+        lo = bottom = least;
+        hi = most;
     }
     tau = hi;
     return true;
@@ -789,100 +942,129 @@ __device__ __forceinline__ void Row<T, NT>::run()
         const bool by_p = top_p < 1.f && !flat;
 
         // ---- thresholds of top-k and top-p
-        float tau_k = kLowest, tau_p = kLowest;
-        Window w = {kLowest, kLowest, 0, 0, 0, 0, 0};
-        bool summed = false;  // warp_a has the sums of what lies above w, the list what lies in it
+        float tau_k = kLowest, tau_p = kLowest, window_hi = CUDART_INF_F;
+        bool summed = false;  // warp_a has the sums of what lies above the window, the list what lies in it
         if (by_k || by_p) {
             const float bottom = by_k ? lo : fmaxf(lo, nothing);
             const Steps step(bottom, mx);
-            const int per = (P.slice + NT - 1) / NT;
-            const float each = per > 4 ? per * 0.25f : 1.f;  // logits that one of the sample stands for
             float mass = 0.f;
-            if (!by_k) mass = mass_of_row();
+            if (!by_k) {
+                mass = mass_of_row();
+                if (lane == 0) sh.warp_f[warp] = mass;
+            }
             sample(step);
-            if (lane == 0) sh.warp_f[warp] = mass;
+            __syncthreads();
             if (shared()) {
-                __syncthreads();
-                mass = hawk::warp_sum(lane < NW ? sh.warp_f[lane] : 0.f);
-                if (tid == 0) sh.swap[5].lo = mass;
+                if (warp == 0 && !by_k) {
+                    mass = hawk::warp_sum(lane < NW ? sh.warp_f[lane] : 0.f);
+                    if (lane == 0) sh.swap[5].lo = mass;
+                }
                 meet();
                 mass = 0.f;
-                for (int r = 0; r < P.cluster; ++r) mass += of(5, r).lo;
-            } else {
-                __syncthreads();
+                if (!by_k)
+                    for (int r = 0; r < P.cluster; ++r) mass += of(5, r).lo;
+            } else if (!by_k && warp == 0) {
                 mass = hawk::warp_sum(lane < NW ? sh.warp_f[lane] : 0.f);
             }
+            u64 target;
             if (by_k) {
-                const float s = top_k / each;
-                w = between_ranks(step, bottom, s, each > 1.f ? 4.f * sqrtf(s) + 8.f : 1.f);
-                pass<false>(w, kLowest);
-                const long long want = static_cast<long long>(top_k) - w.count;
-                summed = want > 0 && want <= w.members && w.members < kTooMany &&
-                         search<false, true>(w.lo, fminf(w.hi, mx), bottom, static_cast<u64>(want), tau_k);
-                if (!summed && !search<false, false>(kLowest, mx, bottom, static_cast<u64>(top_k), tau_k)) tau_k = kLowest;  // (fewer logits than top_k)
+                if (warp == 0) {
+                    const float s = static_cast<float>(top_k) / each();
+                    between_ranks(bottom, s, margin_ranks(s));
+                }
+                __syncthreads();
+                const float w_lo = sh.window_lo;
+                window_hi = top_k <= kList / 2 ? CUDART_INF_F : sh.window_hi;  // (few: all of them to the list, for top-p)
+                const Steps fine(fmaxf(w_lo, bottom), fminf(window_hi, mx));
+                pass<false>(fine, w_lo, window_hi, kLowest, tau_m);
+                const bool found = from_list<false>(fine, w_lo, window_hi, static_cast<u64>(top_k), -1.f, tau_k, target, summed);
+                summed &= found;
+                if (!found && !search<false>(kLowest, mx, bottom, static_cast<u64>(top_k), tau_k)) tau_k = kLowest;  // (fewer logits than top_k)
             }
             if (by_p && tau_k < mx) {
                 if (by_k) {  // the mass of what top-k left
-                    u64 mine = 0;
+                    double mine = kWhole;
+                    u64 all;
                     if (summed) {
-                        mine = lane == 0 ? sh.warp_a[warp] : 0;
+                        all = 0;
                         for (int i = lane; i < listed; i += 32)
-                            if (sh.list_v[warp * kShare + i] >= tau_k) mine += sh.list_w[warp * kShare + i];
+                            if (sh.list_v[warp * kShare + i] >= tau_k) all += sh.list_w[warp * kShare + i];
+                        if (lane == 0) all += sh.warp_a[warp];
                     } else {
                         for (int j = base; j < end; j += 128) {
                             float l[4];
-                            four(j, l);
+                            four(j, end, l);
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                const u64 x = weight(l[k]);
-                                mine += l[k] >= tau_k ? x : 0;
+                                const double x = raw_weight(l[k]);
+                                if (l[k] >= tau_k) mine += x;
                             }
                         }
+                        all = whole(mine);
                     }
                     __syncwarp();
-                    mine = warp_sum(mine);
-                    if (lane == 0) sh.warp_c[warp] = mine;
+                    all = warp_sum(all);
+                    if (lane == 0) sh.warp_c[warp] = all;
+                    barrier();
+                    clear();  // (the list's searches are done, in all blocks)
                     __syncthreads();
-                    mine = warp_sum(lane < NW ? sh.warp_c[lane] : 0ull);
+                    all = warp_sum(lane < NW ? sh.warp_c[lane] : 0ull);
                     if (shared()) {
-                        if (tid == 0) sh.swap[4].a = mine;
+                        if (tid == 0) sh.swap[4].a = all;
                         meet();
-                        mine = 0;
-                        for (int r = 0; r < P.cluster; ++r) mine += of(4, r).a;
+                        all = 0;
+                        for (int r = 0; r < P.cluster; ++r) all += of(4, r).a;
                     }
-                    mass = static_cast<float>(static_cast<double>(mine) / kOne);
+                    mass = static_cast<float>(static_cast<double>(all) / kOne);
                 }
                 const float from = fmaxf(tau_k, nothing);
-                w = between_masses(step, bottom, from, (1.f - top_p) * mass, each > 1.f ? 0.2f : 0.02f);
-                pass<true>(w, from);
-                const u64 target = target_of(top_p, w.above + w.between + w.below);
-                summed = target > w.above && target <= w.above + w.between && w.members < kTooMany &&
-                         search<true, true>(fmaxf(w.lo, from), fminf(w.hi, mx), bottom, target - w.above, tau_p);
-                if (!summed) (void)search<true, false>(from, mx, bottom, target, tau_p);
+                float w_lo = from;
+                if (summed && window_hi == CUDART_INF_F) {  // the list has all that top-k left
+                    const Steps fine(from, mx);
+                    for (int i = lane; i < listed; i += 32)
+                        if (sh.list_v[warp * kShare + i] >= from) count<true>(place_of(fine(sh.list_v[warp * kShare + i])), sh.list_w[warp * kShare + i]);
+                    if (lane == 0) sh.warp_b[warp] = 0;
+                    __syncwarp();
+                    const bool found = from_list<true>(fine, from, window_hi, 0, fmaxf(top_p, 0.f), tau_p, target, summed);
+                    summed &= found;
+                    if (!found) (void)search<true>(from, mx, bottom, target, tau_p);
+                } else {
+                    if (warp == 0) between_masses(step, bottom, from, (1.f - top_p) * mass, each() > 1 ? 0.12f : 0.02f);
+                    __syncthreads();
+                    w_lo = fmaxf(sh.window_lo, from);
+                    window_hi = sh.window_hi;
+                    const Steps fine(w_lo, fminf(window_hi, mx));
+                    pass<true>(fine, w_lo, window_hi, from, tau_m);
+                    const bool found = from_list<true>(fine, w_lo, window_hi, 0, fmaxf(top_p, 0.f), tau_p, target, summed);
+                    summed &= found;
+                    if (!found) (void)search<true>(from, mx, bottom, target, tau_p);
+                }
             }
         }
         tau = fmaxf(fmaxf(tau_k, tau_p), tau_m);
 
         // ---- what stays, for each warp
         u64 kept = 0;
-        if (summed && !(tau_m >= w.hi)) {
+        if (summed) {
             for (int i = lane; i < listed; i += 32)
                 if (sh.list_v[warp * kShare + i] >= tau) kept += sh.list_w[warp * kShare + i];
-            if (lane == 0) kept += sh.warp_a[warp];
+            if (lane == 0) kept += sh.warp_d[warp];
         } else {
+            double sum = kWhole;
             for (int j = base; j < end; j += 128) {
                 float l[4];
-                four(j, l);
-                if (!__any_sync(0xffffffffu, fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= tau)) continue;
+                four(j, end, l);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const u64 x = weight(l[k]);
-                    kept += l[k] >= tau ? x : 0;
+                    const double x = raw_weight(l[k]);
+                    if (l[k] >= tau) sum += x;
                 }
             }
+            kept = whole(sum);
         }
         __syncwarp();
         kept = warp_sum(kept);
+        __syncthreads();  // (warp_b has been read)
         if (lane == 0) sh.warp_b[warp] = kept;
         __syncthreads();
 
@@ -904,43 +1086,46 @@ __device__ __forceinline__ void Row<T, NT>::run()
         const u64 t = static_cast<u64>(static_cast<double>(u) * static_cast<double>(total));  // the running sum that has to be exceeded
         if (t >= before && t - before < mine) {
             const int at = __ffs(__ballot_sync(0xffffffffu, before + sums > t)) - 1;  // the stretch it falls on
-            const u64 low = __shfl_sync(0xffffffffu, sums, at > 0 ? at - 1 : 0);
-            if (warp == at) {
-                u64 run = before + (at > 0 ? low : 0);
-                for (int j = base; j < end; j += 128) {
-                    float l[4];
-                    four(j, l);
-                    u64 x[4];
+            const u64 low = __shfl_sync(0xffffffffu, sums, at > 0 ? at - 1 : 0), run = before + (at > 0 ? low : 0);
+            const int j0 = min(m, at * stretch), j1 = min(m, j0 + stretch), runs = (j1 - j0 + 127) / 128;  // 32 of them at most
+            auto weigh = [&](int j, float (&l)[4], u64 (&x)[4]) {
+                four(j, j1, l);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const u64 y = weight(l[k]);
-                        x[k] = l[k] >= tau ? y : 0;
-                    }
-                    const u64 sum = (x[0] + x[1]) + (x[2] + x[3]);
-                    const u64 inc = run + warp_inclusive(sum);
-                    const uint32_t past = __ballot_sync(0xffffffffu, inc > t);
-                    if (past) {
-                        if (lane == __ffs(past) - 1) {
-                            u64 here = inc - sum;
-                            int k = 0;
-                            float found = l[0];
+                for (int k = 0; k < 4; ++k) {
+                    const u64 y = weight(l[k]);
+                    x[k] = l[k] >= tau ? y : 0;
+                }
+                return (x[0] + x[1]) + (x[2] + x[3]);
+            };
+            float l[4];
+            u64 x[4];
+            for (int r = warp; r < runs; r += NW) {
+                const u64 sum = warp_sum(weigh(j0 + 128 * r, l, x));
+                if (lane == 0) sh.warp_c[r] = sum;
+            }
+            __syncthreads();
+            const u64 of_runs = run + warp_inclusive(lane < runs ? sh.warp_c[lane] : 0ull);
+            const int r = __ffs(__ballot_sync(0xffffffffu, of_runs > t)) - 1;  // the run
+            const u64 in_front = __shfl_sync(0xffffffffu, of_runs, r > 0 ? r - 1 : 0);
+            if (warp == r % NW) {
+                const u64 sum = weigh(j0 + 128 * r, l, x), inc = (r > 0 ? in_front : run) + warp_inclusive(sum);
+                if (lane == __ffs(__ballot_sync(0xffffffffu, inc > t)) - 1) {
+                    u64 here = inc - sum;
+                    int k = 0;
+                    float found = l[0];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if (here <= t) {
-                                    k = i;
-                                    found = l[i];
-                                }
-                                here += x[i];
-                            }
-                            const int e = first + j + 4 * lane + k - pad;
-                            if (HAWK_IN_BOUNDS(P.dev_status, e, P.n)) {
-                                P.token[row] = P.v_begin + e;
-                                if (P.token_prob) P.token_prob[row] = share(found, inv_total);
-                            }
+                    for (int i = 0; i < 4; ++i) {
+                        if (here <= t) {
+                            k = i;
+                            found = l[i];
                         }
-                        break;
+                        here += x[i];
                     }
-                    run = __shfl_sync(0xffffffffu, inc, 31);
+                    const int e = first + j0 + 128 * r + 4 * lane + k - pad;
+                    if (HAWK_IN_BOUNDS(P.dev_status, e, P.n)) {
+                        P.token[row] = P.v_begin + e;
+                        if (P.token_prob) P.token_prob[row] = share(found, inv_total);
+                    }
                 }
             }
         }
@@ -952,13 +1137,12 @@ __device__ __forceinline__ void Row<T, NT>::run()
     // ---- the distribution
     if (P.probs) {
         float *out = P.probs + row * P.probs_stride;
-        float *ids = out + P.v_begin + first - pad;  // of place 0 of vals
-        const bool whole = (reinterpret_cast<uintptr_t>(ids) & 15u) == 0;
+        const bool aligned = (reinterpret_cast<uintptr_t>(out + P.v_begin + first - pad) & 15u) == 0;  // of place 0 of vals
         const float factor = static_cast<float>(inv_total), octaves = fminf(static_cast<float>(rate / kParts), 1e30f);
         const float octaves_low = octaves < 1e30f ? static_cast<float>(rate / kParts - static_cast<double>(octaves)) : 0.f;
         for (int j = base; j < end; j += 128) {
             float l[4], p[4];
-            four(j, l);
+            four(j, end, l);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 // 2^((l - max) * octaves) in fp32: the product in two parts, its whole octaves apart
@@ -976,7 +1160,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
                     if (first + e + k == pick) p[k] = 1.f;
             }
             if (!HAWK_IN_BOUNDS(P.dev_status, static_cast<long long>(P.v_begin) + first + max(e, 0), P.V)) continue;
-            if (whole && e >= 0 && e + 4 <= n) {
+            if (aligned && e >= 0 && e + 4 <= n) {
                 *reinterpret_cast<float4 *>(out + P.v_begin + first + e) = make_float4(p[0], p[1], p[2], p[3]);
             } else {
 #pragma unroll
@@ -1041,7 +1225,7 @@ extern "C" hawk_status hawk_sample(const hawk_sample_args *a, int32_t *dev_statu
     if (a->uncond && !a->row_cfg_scale && !finite(a->cfg_scale)) return HAWK_ERR_PARAM;
     if (!a->logits || !a->u || !a->token) return HAWK_ERR_NULL;
     const int n = a->v_end - a->v_begin;
-    if (n < 1 || n > kMaxSlice * kMaxCluster) return HAWK_ERR_UNSUPPORTED;
+    if (n < 1 || n > kMaxIds) return HAWK_ERR_UNSUPPORTED;
     if (a->row_stride < 0 || (a->uncond && a->uncond_row_stride < 0) || (a->R > 1 && a->probs && a->probs_row_stride < a->V))
         return HAWK_ERR_SHAPE;
     const uintptr_t size = a->dtype == HAWK_F32 ? 4 : 2;
@@ -1076,14 +1260,21 @@ extern "C" hawk_status hawk_sample(const hawk_sample_args *a, int32_t *dev_statu
     P.token_prob = a->token_prob;
     P.probs = a->probs;
     P.dev_status = dev_status;
-    P.cluster = 1;
-    while ((n + P.cluster - 1) / P.cluster > kMaxSlice) P.cluster *= 2;
+    // Blocks of a row.  Few rows: about 4096 ids a block (one row of 16384 ids 13.9 us in one block of 512 threads, 12.3 in four; of 100003
+    // in bf16 23.7 in three, 18.9 in eight).  Up to two waves of blocks: 20480 ids (48 rows of 100003: 47 us in three, 40 in
+    // five).  Else as few as hold the row (200 rows of 100003: 129 us in three, 174 in five).  Below, calls of more rows than SMs: blocks
+    // of 256 threads, two on an SM (512 rows of 16384: 51 us, 61 with 512 threads; 148 rows: 18.7 and 14.4).
+    const auto blocks_of = [&](int ids) { return (n + ids - 1) / ids; };
+    P.cluster = blocks_of(kMaxSlice);
+    int more = 1;
+    if (a->R <= 16) more = n / 4096 < kMaxCluster ? n / 4096 : kMaxCluster;
+    else if (static_cast<long long>(a->R) * blocks_of(20480) <= 2 * 148) more = blocks_of(20480) < kMaxCluster ? blocks_of(20480) : kMaxCluster;
+    if (more > P.cluster) P.cluster = more;
     P.slice = ((n + P.cluster - 1) / P.cluster + 15) & ~15;  // (every block's rows then lie alike in 16-byte pieces)
     const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     auto pick = [&](auto type) {
         using T = decltype(type);
-        const bool many = static_cast<long long>(a->R) * P.cluster >= 2 * 148 && P.slice <= 16384 - 16;
-        return many ? launch<T, 256>(P, a->R, st) : launch<T, 1024>(P, a->R, st);
+        return P.cluster == 1 && P.slice <= 16384 && a->R > 148 ? launch<T, 256>(P, a->R, st) : launch<T, 512>(P, a->R, st);
     };
     return a->dtype == HAWK_F32 ? pick(float{}) : a->dtype == HAWK_BF16 ? pick(__nv_bfloat16{}) : pick(__half{});
 }
