@@ -54,7 +54,7 @@ struct SampleParams {
 };
 
 struct Swap {  // what the blocks of a row tell each other
-    u64 a, b, c;
+    u64 a, b;
     float lo, hi;
     int n;
 };
@@ -252,17 +252,20 @@ private:
         const double w = power(l, e);
         return static_cast<float>(__hiloint2double(__double2hiint(w) + e * (1 << 20), __double2loint(w)) * factor);
     }
-    __device__ __forceinline__ Swap of(int slot, int r) const
+    // What block r of the row has said in a slot, one number at a time (each is a load from another block).
+    __device__ __forceinline__ u64 a_of(int slot, int r) const { return hawk::ld_cluster_u64(hawk::map_shared_to_cta(&sh.swap[slot].a, r)); }
+    __device__ __forceinline__ u64 b_of(int slot, int r) const { return hawk::ld_cluster_u64(hawk::map_shared_to_cta(&sh.swap[slot].b, r)); }
+    __device__ __forceinline__ int n_of(int slot, int r) const
     {
-        const uint32_t at = hawk::map_shared_to_cta(&sh.swap[slot], r);
-        Swap s;
-        s.a = hawk::ld_cluster_u64(at);
-        s.b = hawk::ld_cluster_u64(at + 8);
-        s.c = hawk::ld_cluster_u64(at + 16);
-        s.lo = __uint_as_float(hawk::ld_cluster_u32(at + 24));
-        s.hi = __uint_as_float(hawk::ld_cluster_u32(at + 28));
-        s.n = static_cast<int>(hawk::ld_cluster_u32(at + 32));
-        return s;
+        return static_cast<int>(hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.swap[slot].n, r)));
+    }
+    __device__ __forceinline__ float lo_of(int slot, int r) const
+    {
+        return __uint_as_float(hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.swap[slot].lo, r)));
+    }
+    __device__ __forceinline__ float hi_of(int slot, int r) const
+    {
+        return __uint_as_float(hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.swap[slot].hi, r)));
     }
     // Lane's four logits of the run of 128 from place j on (-inf from `stop` on).
     __device__ __forceinline__ void four(int j, int stop, float (&l)[4]) const
@@ -395,9 +398,8 @@ __device__ __forceinline__ void Row<T, NT>::ends(float &lo, float &hi, int slot)
         }
         meet();
         for (int r = 0; r < P.cluster; ++r) {
-            const Swap s = of(slot, r);
-            lo = fminf(lo, s.lo);
-            hi = fmaxf(hi, s.hi);
+            lo = fminf(lo, lo_of(slot, r));
+            hi = fmaxf(hi, hi_of(slot, r));
         }
     }
 }
@@ -713,10 +715,9 @@ __device__ __forceinline__ bool Row<T, NT>::finish(u64 target, float &low, float
         for (int r = 0; r < kMaxCluster; ++r) {
             before[r + 1] = before[r];
             if (r < P.cluster) {
-                const Swap x = of(2, r);
-                before[r + 1] += x.n;
-                low = fminf(low, x.lo);
-                high = fmaxf(high, x.hi);
+                before[r + 1] += n_of(2, r);
+                low = fminf(low, lo_of(2, r));
+                high = fmaxf(high, hi_of(2, r));
             }
         }
         members = before[kMaxCluster];
@@ -778,10 +779,9 @@ __device__ __forceinline__ bool Row<T, NT>::from_list(const Steps &step, float l
             over = 0;
             if (warp == 0)
                 for (int r = 0; r < P.cluster; ++r) {
-                    const Swap s = of(1, r);
-                    above += s.a;
-                    below += s.b;
-                    over |= s.n;
+                    above += a_of(1, r);
+                    if (kMass) below += b_of(1, r);
+                    over |= n_of(1, r);
                 }
         }
         if (warp == 0) {
@@ -884,7 +884,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
         min_p = 0.f;
     }
     u = u > 0.f ? fminf(u, 1.f - 1.f / 16777216.f) : 0.f;
-    bool greedy = temperature == 0.f;
+    const bool greedy = temperature == 0.f;
     if (tid == 0) {  // (a row's own settings: fp64 division and logarithm by one lane)
         sh.rate = !P.temperatures ? P.rate : greedy ? 0.0 : rate_of(temperature);
         sh.least = !P.min_ps ? P.least : least_of(min_p);
@@ -892,6 +892,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
     }
     ends(lo, hi, 0);
     mx = hi;
+    lo = fminf(lo, hi);  // (none of some was a number)
     rate = sh.rate;
     nothing = fmaxf(fminf(static_cast<float>(static_cast<double>(mx) - 32.0 * static_cast<double>(temperature)), mx), kLowest);
     const bool some = mx > -CUDART_INF_F;
@@ -914,7 +915,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
         if (shared()) {
             if (tid == 0) sh.swap[4].n = pick;
             meet();
-            for (int r = 0; r < P.cluster; ++r) pick = min(pick, of(4, r).n);
+            for (int r = 0; r < P.cluster; ++r) pick = min(pick, n_of(4, r));
         }
         if (rank == 0 && tid == 0) {
             P.token[row] = P.v_begin + pick;
@@ -938,7 +939,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
         }
         const bool flat = nothing >= mx;  // a temperature so low that nothing but the maximum has a weight
         if (flat) tau_m = mx;
-        bool by_k = top_k > 0 && top_k < P.n && !flat;
+        const bool by_k = top_k > 0 && top_k < P.n && !flat;
         const bool by_p = top_p < 1.f && !flat;
 
         // ---- thresholds of top-k and top-p
@@ -961,8 +962,8 @@ __device__ __forceinline__ void Row<T, NT>::run()
                 }
                 meet();
                 mass = 0.f;
-                if (!by_k)
-                    for (int r = 0; r < P.cluster; ++r) mass += of(5, r).lo;
+                if (!by_k && warp == 0)
+                    for (int r = 0; r < P.cluster; ++r) mass += lo_of(5, r);
             } else if (!by_k && warp == 0) {
                 mass = hawk::warp_sum(lane < NW ? sh.warp_f[lane] : 0.f);
             }
@@ -1013,7 +1014,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
                         if (tid == 0) sh.swap[4].a = all;
                         meet();
                         all = 0;
-                        for (int r = 0; r < P.cluster; ++r) all += of(4, r).a;
+                        for (int r = 0; r < P.cluster; ++r) all += a_of(4, r);
                     }
                     mass = static_cast<float>(static_cast<double>(all) / kOne);
                 }
@@ -1077,7 +1078,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
             meet();
             total = 0;
             for (int r = 0; r < P.cluster; ++r) {
-                const u64 a = of(3, r).a;
+                const u64 a = a_of(3, r);
                 if (r < rank) before += a;
                 total += a;
             }
@@ -1138,18 +1139,20 @@ __device__ __forceinline__ void Row<T, NT>::run()
     if (P.probs) {
         float *out = P.probs + row * P.probs_stride;
         const bool aligned = (reinterpret_cast<uintptr_t>(out + P.v_begin + first - pad) & 15u) == 0;  // of place 0 of vals
-        const float factor = static_cast<float>(inv_total), octaves = fminf(static_cast<float>(rate / kParts), 1e30f);
-        const float octaves_low = octaves < 1e30f ? static_cast<float>(rate / kParts - static_cast<double>(octaves)) : 0.f;
+        const float factor = static_cast<float>(inv_total), octaves = static_cast<float>(rate / kParts);
+        const float octaves_low = static_cast<float>(rate / kParts - static_cast<double>(octaves));
+        const bool in_range = octaves < 1e37f;  // (of fp32: temperatures that are themselves next to nothing are not)
         for (int j = base; j < end; j += 128) {
             float l[4], p[4];
             four(j, end, l);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 // 2^((l - max) * octaves) in fp32: the product in two parts, its whole octaves apart
-                const float d = l[k] - mx, z = d * octaves;
+                const float d = fmaxf(l[k], nothing) - mx, z = d * octaves;
                 const float whole_z = rintf(z);
                 const float rest = (z - whole_z) + (fmaf(d, octaves, -z) + d * octaves_low);
-                const float x = hawk::fast_exp2(rest) * __int_as_float((static_cast<int>(whole_z) + 127) << 23) * factor;
+                float x = hawk::fast_exp2(rest) * __uint_as_float(static_cast<uint32_t>(static_cast<int>(whole_z) + 127) << 23) * factor;
+                if (!in_range) x = share(fmaxf(l[k], nothing), inv_total);
                 p[k] = greedy || !some || !(l[k] >= tau) || l[k] < nothing ? 0.f : x;
             }
             const int e = j + 4 * lane - pad;  // of the block's ids
