@@ -5,9 +5,15 @@
 //
 // The state is small (a few hundred KB at most) and every step of the bookkeeping needs the one before it: releases, then the free
 // pages, then who gets them.  So resize and compact are ONE launch of one cluster: 8 blocks that share the scan of the counts,
-// meet at cluster barriers (some 0.6 us each; another launch costs 1.5 to 2) and exchange one number a block through
+// meet at two cluster barriers (some 0.6 us each; another launch costs 1.5 to 2) and exchange one number a block through
 // distributed shared memory.  What a free page is called is found by prefix sums over bit masks in shared memory, not by atomics, so
-// results do not depend on the launch.  All of it is bound by latency: a launch, two or three barriers and as many dependent loads.
+// results do not depend on the launch.  All of it is bound by latency: a launch, the barriers, and chains of dependent loads (lengths,
+// table, counts) of some 0.7 us each.  256 streams that share pages, 131 of which need a copy: 12.7 us under ncu (26 when a thread handed out the
+// free pages of a word of the bit mask one after the other).
+// The copies are bound by HBM: 4096 pages of 82 KB (keys and values) in 68 us, 6.5 TB/s read and written, what a plain copy of as many
+// bytes takes.  Fork is one block a stream with four entries a thread in flight, its counts by atomics without a result (512 streams, 238
+// thousand entries: 6.5 us); keep moves rows through registers, eight a thread in flight (128 trees of 64 nodes, 4 layers: 7 us for 26 MB,
+// bound by the chain lengths -> table -> rows).
 #include <climits>
 
 #include "hawk_common.cuh"
@@ -22,6 +28,9 @@ constexpr int kBookWarps = kBookThreads / 32;
 constexpr int kMaxStreams = 4096;    // their prefix sums are held in shared memory
 constexpr int kMaxPages = 1 << 20;   // a block's share of them as bit masks too
 constexpr int kSlice = kMaxPages / kBookBlocks;
+// States up to here go to one block: 2 streams over 28 pages 8.1 us in a cluster, 7.4 in one block; 12 streams over 600 pages packed 12 and 8;
+// but 256 streams over 3922 pages 12.7 and 17, 128 over 12300 packed 14 and 28.
+constexpr int kSmallPages = 2048, kSmallEntries = 4096;
 
 struct Div {  // number of pages of `keys` keys
     hawk::FastDiv page;
@@ -68,10 +77,15 @@ __device__ __forceinline__ int block_sum(int v, int *sh)
 }
 
 // Barrier of the cluster (lanes that a branch parted come together first).
+template <int kBlocks>
 __device__ __forceinline__ void meet()
 {
-    __syncwarp();
-    hawk::cluster_sync_all();
+    if (kBlocks == 1) {
+        __syncthreads();
+    } else {
+        __syncwarp();
+        hawk::cluster_sync_all();
+    }
 }
 
 // Takes one reference of a page back; a count that is 0 already stays so.
@@ -91,9 +105,10 @@ __device__ __forceinline__ void report(int32_t *dev_status, int flags)
 }
 
 // A block's share of the pages, in whole runs of 128 (what a warp looks at in one go): [first, end).
+template <int kBlocks>
 __device__ __forceinline__ void slice_of(int n_pages, int rank, int &first, int &end)
 {
-    const int per = ((n_pages + kBookBlocks - 1) / kBookBlocks + 127) & ~127;
+    const int per = ((n_pages + kBlocks - 1) / kBlocks + 127) & ~127;
     first = min(n_pages, rank * per);
     end = min(n_pages, first + per);
 }
@@ -126,14 +141,21 @@ __device__ __forceinline__ int mark_pages(const int32_t *refs, int first, int en
     return count;
 }
 
-// The blocks' numbers `mine` (thread 0's): how many the blocks before this one have, and all.  A cluster barrier.
+// The blocks' numbers `mine`: how many the blocks before this one have, and all.  A cluster barrier.
+template <int kBlocks>
 __device__ __forceinline__ void exchange_counts(int mine, int *slot, int rank, int &before, int &total)
 {
+    before = 0;
+    total = mine;
+    if (kBlocks == 1) {
+        __syncthreads();
+        return;
+    }
     if (threadIdx.x == 0) *slot = mine;
-    meet();
-    before = total = 0;
+    meet<kBlocks>();
+    total = 0;
 #pragma unroll
-    for (int r = 0; r < kBookBlocks; ++r) {
+    for (int r = 0; r < kBlocks; ++r) {
         const int n = static_cast<int>(hawk::ld_cluster_u32(hawk::map_shared_to_cta(slot, r)));
         if (r < rank) before += n;
         total += n;
@@ -188,16 +210,17 @@ __device__ __forceinline__ int first_past(const int *ends, int n, int r)
 
 // Everything that the block reads of the state as it was on entry it reads before the first barrier of the cluster, and nobody writes the
 // state in place before it (but a block the counts of its own share of the pages).
+template <int kBlocks>
 __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(ResizeParams P)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     ResizeShared &sh = *reinterpret_cast<ResizeShared *>(smem_raw);
     hawk::allow_dependent_launch();
     hawk::grid_dependency_wait();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = static_cast<int>(hawk::cluster_cta_rank());
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = kBlocks == 1 ? 0 : static_cast<int>(hawk::cluster_cta_rank());
     const long long cap = static_cast<long long>(P.W) * P.div.page.d;
     int flags = 0, first, end;
-    slice_of(P.n_pages, rank, first, end);
+    slice_of<kBlocks>(P.n_pages, rank, first, end);
 
     // ---- lengths, pages that streams grow into; the share's counts to where they are kept
     if (P.out_refs != P.refs) {
@@ -241,7 +264,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(ResizeParams P)
         }
     }
     if (P.out_table != P.table) {
-        for (int s = rank * kBookWarps + warp; s < P.S; s += kBookBlocks * kBookWarps) {
+        for (int s = rank * kBookWarps + warp; s < P.S; s += kBlocks * kBookWarps) {
             const int old = sh.kv[s];
             if (old < 0) continue;
             const int stay = P.div.pages(min(old, sh.next[s]));
@@ -270,7 +293,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(ResizeParams P)
         at += __popc(sh.bits[w]);
         sh.before[w] = at;  // (with the word's own)
     }
-    exchange_counts(mine, &sh.slot, rank, free_before, total_free);
+    exchange_counts<kBlocks>(mine, &sh.slot, rank, free_before, total_free);
 
     // ---- what every stream needs: each block for itself
     constexpr int kPer = kMaxStreams / kBookThreads;
@@ -316,8 +339,8 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(ResizeParams P)
         P.out_table[static_cast<size_t>(s) * P.W + j] = page;
         P.out_refs[page] = 1;
     }
-    meet();  // (the counts of shared pages have been looked at by all; nobody's numbers are read any more)
-    for (int s = rank * kBookThreads + tid; s < P.S; s += kBookBlocks * kBookThreads) {
+    meet<kBlocks>();  // (the counts of shared pages have been looked at by all; nobody's numbers are read any more)
+    for (int s = rank * kBookThreads + tid; s < P.S; s += kBlocks * kBookThreads) {
         const int needs = sh.end[s] - (s > 0 ? sh.end[s - 1] : 0);
         const bool served = needs == 0 || sh.end[s] <= total_free;
         if (!served) flags |= HAWK_DEV_NO_PAGES;
@@ -441,16 +464,17 @@ struct CompactShared {
 
 // Packed, the pages in use end at `border`: those behind it have to move, and as many free ones lie in front of it.  Both lists are made
 // by rank; then every block knows all it needs, and the moves and the new ids are written without another barrier.
+template <int kBlocks>
 __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams P)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     CompactShared &sh = *reinterpret_cast<CompactShared *>(smem_raw);
     hawk::allow_dependent_launch();
     hawk::grid_dependency_wait();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = static_cast<int>(hawk::cluster_cta_rank());
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = kBlocks == 1 ? 0 : static_cast<int>(hawk::cluster_cta_rank());
     const long long cap = static_cast<long long>(P.W) * P.div.page.d;
     int flags = 0, first, end;
-    slice_of(P.n_pages, rank, first, end);
+    slice_of<kBlocks>(P.n_pages, rank, first, end);
     if (P.out_refs != P.refs) {
         for (int i = first / 4 + tid; i < end / 4; i += kBookThreads)
             reinterpret_cast<int4 *>(P.out_refs)[i] = reinterpret_cast<const int4 *>(P.refs)[i];
@@ -463,13 +487,17 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams 
     mine = block_sum(mine, sh.sums);
     const int eligible = max(0, end - max(first, from_page));
     if (tid == 0) sh.slot_free = eligible - mine;
-    exchange_counts(mine, &sh.slot_used, rank, used_before, used);
-    free_before = free_all = 0;
+    exchange_counts<kBlocks>(mine, &sh.slot_used, rank, used_before, used);
+    free_before = 0;
+    free_all = eligible - mine;
+    if (kBlocks > 1) {
+        free_all = 0;
 #pragma unroll
-    for (int r = 0; r < kBookBlocks; ++r) {
-        const int n = static_cast<int>(hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.slot_free, r)));
-        if (r < rank) free_before += n;
-        free_all += n;
+        for (int r = 0; r < kBlocks; ++r) {
+            const int n = static_cast<int>(hawk::ld_cluster_u32(hawk::map_shared_to_cta(&sh.slot_free, r)));
+            if (r < rank) free_before += n;
+            free_all += n;
+        }
     }
 
     // ---- the lowest free pages and the highest in use, by rank; a word a thread
@@ -501,16 +529,18 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams 
             if (i_f < lists && HAWK_IN_BOUNDS(P.dev_status, i_f, lists)) P.to[i_f] = p + __ffs(m) - 1;
     }
     behind = block_sum(behind, sh.sums);
-    if (tid == 0) P.counts[rank] = behind;
-    meet();
-    int moved = 0;
+    if (kBlocks > 1 && tid == 0) P.counts[rank] = behind;
+    meet<kBlocks>();
+    int moved = kBlocks > 1 ? 0 : behind;
+    if (kBlocks > 1) {
 #pragma unroll
-    for (int r = 0; r < kBookBlocks; ++r) moved += __ldcg(P.counts + r);
+        for (int r = 0; r < kBlocks; ++r) moved += __ldcg(P.counts + r);
+    }
     const int all_moves = moved;
     moved = min(moved, P.moves);
 
     // ---- moves
-    for (int i = rank * kBookThreads + tid; i < P.moves; i += kBookBlocks * kBookThreads) {
+    for (int i = rank * kBookThreads + tid; i < P.moves; i += kBlocks * kBookThreads) {
         int a = -1, b = -1;
         if (i < moved) {
             a = __ldcg(P.from + i);
@@ -531,7 +561,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams 
     }
     const int lowest = moved > 0 ? __ldcg(P.from + moved - 1) : INT_MAX;  // pages in use from here on move
     const int runs = P.S * static_cast<int>(P.div_runs.d);
-    for (int t = rank * kBookWarps + warp; t < runs; t += kBookBlocks * kBookWarps) {
+    for (int t = rank * kBookWarps + warp; t < runs; t += kBlocks * kBookWarps) {
         uint32_t part;
         const int s = static_cast<int>(P.div_runs.divmod(static_cast<uint32_t>(t), part)), j0 = static_cast<int>(part) * 128 + lane;
         const int kv = P.kv[s];
@@ -742,7 +772,7 @@ hawk_status done(cudaError_t e) { return e == cudaSuccess ? HAWK_OK : HAWK_ERR_C
 
 // Lets `kernel` use `bytes` of shared memory on the current device (asked once for each).
 template <class K>
-bool allow_smem(K *kernel, size_t bytes, unsigned long long (&seen))
+bool allow_smem(K *kernel, size_t bytes, unsigned long long &seen)
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return false;
@@ -751,6 +781,20 @@ bool allow_smem(K *kernel, size_t bytes, unsigned long long (&seen))
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess) return false;
     __atomic_fetch_or(&seen, bit, __ATOMIC_RELEASE);
     return true;
+}
+
+// The bookkeeping kernels: a cluster, or one block for small states, which then needs no barrier of a cluster.
+template <class P>
+hawk_status launch_book(void (*many)(P), void (*one)(P), unsigned long long &seen, unsigned long long &seen_one, size_t smem, const P &p,
+                        cudaStream_t st)
+{
+    const bool small = p.n_pages <= kSmallPages && static_cast<long long>(p.S) * p.W <= kSmallEntries;
+    if (small) {
+        if (!allow_smem(one, smem, seen_one)) return HAWK_ERR_CUDA;
+        return done(hawk_host::launch_dependent(one, dim3(1), dim3(kBookThreads), smem, st, p));
+    }
+    if (!allow_smem(many, smem, seen)) return HAWK_ERR_CUDA;
+    return done(hawk_host::launch_dependent_clusters(many, kBookBlocks, dim3(kBookBlocks), dim3(kBookThreads), smem, st, p));
 }
 
 hawk_status check_pages(const hawk_page_tensors &p)
@@ -799,12 +843,11 @@ extern "C" hawk_status hawk_pages_resize(const hawk_pages_resize_args *a, int32_
     if (a->n_pages > 0 && (!a->page_refs || !a->out_refs)) return HAWK_ERR_NULL;
     if (!aligned16(a->page_refs) || !aligned16(a->out_refs)) return HAWK_ERR_ALIGN;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
-    static unsigned long long seen = 0;
-    if (!allow_smem(resize_kernel, sizeof(ResizeShared), seen)) return HAWK_ERR_CUDA;
     ResizeParams P = {a->block_table, a->kv_len, a->new_len, a->page_refs, a->out_table, a->out_len, a->out_refs, a->copies,
                       a->S, a->table_width, a->n_pages, make_div(a->page_size), dev_status};
-    return done(hawk_host::launch_dependent_clusters(resize_kernel, kBookBlocks, dim3(kBookBlocks), dim3(kBookThreads),
-                                                     sizeof(ResizeShared), reinterpret_cast<cudaStream_t>(stream), P));
+    static unsigned long long seen = 0, seen_one = 0;
+    return launch_book(resize_kernel<kBookBlocks>, resize_kernel<1>, seen, seen_one, sizeof(ResizeShared), P,
+                       reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" hawk_status hawk_pages_fork(const hawk_pages_fork_args *a, int32_t *dev_status, hawk_stream_t stream)
@@ -858,8 +901,6 @@ extern "C" hawk_status hawk_pages_compact(const hawk_pages_compact_args *a, int3
     if (!a->workspace || a->workspace_bytes < hawk_pages_compact_workspace_bytes(a->n_pages, a->max_moves))
         return HAWK_ERR_WORKSPACE;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
-    static unsigned long long seen = 0;
-    if (!allow_smem(compact_kernel, sizeof(CompactShared), seen)) return HAWK_ERR_CUDA;
     CompactParams P = {};
     P.table = a->block_table;
     P.kv = a->kv_len;
@@ -881,8 +922,9 @@ extern "C" hawk_status hawk_pages_compact(const hawk_pages_compact_args *a, int3
     P.moves = a->max_moves;
     P.div = make_div(a->page_size);
     P.dev_status = dev_status;
-    return done(hawk_host::launch_dependent_clusters(compact_kernel, kBookBlocks, dim3(kBookBlocks), dim3(kBookThreads),
-                                                     sizeof(CompactShared), reinterpret_cast<cudaStream_t>(stream), P));
+    static unsigned long long seen = 0, seen_one = 0;
+    return launch_book(compact_kernel<kBookBlocks>, compact_kernel<1>, seen, seen_one, sizeof(CompactShared), P,
+                       reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" hawk_status hawk_pages_copy(const hawk_page_tensors *pages, const int32_t *copies, int n_copies, int32_t *dev_status,
