@@ -292,7 +292,7 @@ private:
     template <bool kMass>
     __device__ __forceinline__ void count(int at, u64 weight);
     template <bool kMass>
-    __device__ __forceinline__ void find_step(u64 above, u64 target, u64 count_above, float share);
+    __device__ __forceinline__ void find_step(u64 above, u64 target);
     __device__ __forceinline__ void push(float l, u64 weight, uint32_t &low, uint32_t &high);
     __device__ __forceinline__ void range(uint32_t low, uint32_t high);
     __device__ __forceinline__ bool finish(u64 target, float &low, float &high);
@@ -408,13 +408,13 @@ __device__ __forceinline__ void Row<T, NT>::ends(float &lo, float &hi, int slot)
 template <typename T, int NT>
 __device__ __forceinline__ float Row<T, NT>::mass_of_row()
 {
-    const float octaves = static_cast<float>(rate / kParts);
+    const float octaves = static_cast<float>(rate / kParts), top = mx * octaves;
     float mass = 0.f;
     for (int j = base; j < end; j += 128) {
         float l[4];
         four(j, end, l);
-        mass += (hawk::fast_exp2((l[0] - mx) * octaves) + hawk::fast_exp2((l[1] - mx) * octaves)) +
-                (hawk::fast_exp2((l[2] - mx) * octaves) + hawk::fast_exp2((l[3] - mx) * octaves));
+        mass += (hawk::fast_exp2(fmaf(l[0], octaves, -top)) + hawk::fast_exp2(fmaf(l[1], octaves, -top))) +
+                (hawk::fast_exp2(fmaf(l[2], octaves, -top)) + hawk::fast_exp2(fmaf(l[3], octaves, -top)));
     }
     return hawk::warp_sum(mass);
 }
@@ -561,15 +561,15 @@ __device__ __forceinline__ void Row<T, NT>::count(int at, u64 w)
     }
 }
 
-// One pass over the weights of the logits from `from` on: those from lo up to hi go to the list and, by their step, to the histogram; for the
-// others the warp's sums of what lies above (warp_a, and its number in warp_lo) and, for top-p, below (warp_b).  warp_d: the part of the sum above
-// that min-p leaves, which keeps what is not below `least`.
+// One pass over the weights of the logits from `from` on: those from lo (not below `from`) up to hi go to the list and, by their step, to the
+// histogram.  The warp's sums: of what lies above (warp_a, and its number in warp_lo); of everything, for top-p (warp_b); of the part above
+// that min-p leaves, which keeps what is not below `least` (warp_d).
 template <typename T, int NT>
 template <bool kMass>
 __device__ __forceinline__ void Row<T, NT>::pass(const Steps &step, float lo, float hi, float from, float least)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    double above = kWhole, below = kWhole, stays = kWhole;
+    double above = kWhole, all = kWhole, stays = kWhole;
     const bool cuts = least > hi;
     int up_count = 0;
     listed = 0;
@@ -584,12 +584,16 @@ __device__ __forceinline__ void Row<T, NT>::pass(const Steps &step, float lo, fl
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const double x = raw_weight(l[k]);
-                const bool up = l[k] >= hi, member = !up && l[k] >= lo && (!kMass || l[k] >= from);
+                const bool up = l[k] >= hi;
+                if (kMass && l[k] >= from) all += x;
                 if (up) above += x;
-                if (cuts && l[k] >= least) stays += x;
                 if (!kMass && up) ++up_count;
-                if (kMass && !up && !member && l[k] >= from) below += x;
-                if (member) in |= 1u << k;
+                if (!up && l[k] >= lo) in |= 1u << k;
+            }
+            if (cuts) {  // (rare: a second look is cheaper than a third sum in each of them)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (l[k] >= least) stays += raw_weight(l[k]);
             }
             marks |= in << ((j - j0) >> 5);
         }
@@ -609,7 +613,7 @@ __device__ __forceinline__ void Row<T, NT>::pass(const Steps &step, float lo, fl
     }
     const u64 a = warp_sum(whole(above)), d = cuts ? warp_sum(whole(stays)) : a;
     u64 b = 0;
-    if (kMass) b = warp_sum(whole(below));
+    if (kMass) b = warp_sum(whole(all));
     if (!kMass) up_count = __reduce_add_sync(0xffffffffu, up_count);
     if (lane == 0) {
         sh.warp_a[warp] = a;
@@ -620,11 +624,10 @@ __device__ __forceinline__ void Row<T, NT>::pass(const Steps &step, float lo, fl
     }
 }
 
-// The step of the histogram that the target is reached in (one warp, behind a barrier): bin, and the number or mass above it.  share >= 0: the target is
-// that share of above, the histogram and `rest`.
+// The step of the histogram that the target is reached in (one warp, behind a barrier): bin, and the number or mass above it.
 template <typename T, int NT>
 template <bool kMass>
-__device__ __forceinline__ void Row<T, NT>::find_step(u64 above, u64 target, u64 rest, float share)
+__device__ __forceinline__ void Row<T, NT>::find_step(u64 above, u64 target)
 {
     constexpr int kPer = kBins / 32;
     const int lane = threadIdx.x & 31;
@@ -642,7 +645,6 @@ __device__ __forceinline__ void Row<T, NT>::find_step(u64 above, u64 target, u64
 #pragma unroll
     for (int i = 0; i < kPer; ++i) sum += part[i];
     u64 run = above + warp_inclusive(sum) - sum;
-    if (share >= 0.f) target = target_of(static_cast<double>(share), __shfl_sync(0xffffffffu, run + sum, 31) + rest);
     int bin = -1;
     u64 at_run = 0;
 #pragma unroll
@@ -755,8 +757,8 @@ __device__ __forceinline__ bool Row<T, NT>::finish(u64 target, float &low, float
     return true;
 }
 
-// The threshold among the list that a pass has made of the logits from lo up to hi: the largest value from which on the logits reach `want`, or the
-// share of the mass (share >= 0), which becomes the target.  False if it is not among them.  complete: the list has them all.  The same in all
+// The threshold among the list that a pass has made of the logits from lo up to hi: the largest value from which on the logits reach the target:
+// `want` of them, or `share` of the mass.  False if it is not among them.  complete: the list has them all.  The same in all
 // blocks of the row.
 template <typename T, int NT>
 template <bool kMass>
@@ -766,26 +768,26 @@ __device__ __forceinline__ bool Row<T, NT>::from_list(const Steps &step, float l
     __syncthreads();
     if (warp == 0 || shared()) {
         u64 above = kMass ? warp_sum(lane < NW ? sh.warp_a[lane] : 0ull) : __reduce_add_sync(0xffffffffu, lane < NW ? sh.warp_lo[lane] : 0u);
-        u64 below = kMass ? warp_sum(lane < NW ? sh.warp_b[lane] : 0ull) : 0ull;
+        u64 all = kMass ? warp_sum(lane < NW ? sh.warp_b[lane] : 0ull) : 0ull;
         int over = sh.over;
         if (shared()) {
             if (threadIdx.x == 0) {
                 sh.swap[1].a = above;
-                sh.swap[1].b = below;
+                sh.swap[1].b = all;
                 sh.swap[1].n = over;
             }
             meet();
-            above = below = 0;
+            above = all = 0;
             over = 0;
             if (warp == 0)
                 for (int r = 0; r < P.cluster; ++r) {
                     above += a_of(1, r);
-                    if (kMass) below += b_of(1, r);
+                    if (kMass) all += b_of(1, r);
                     over |= n_of(1, r);
                 }
         }
         if (warp == 0) {
-            find_step<kMass>(above, want, below, share);
+            find_step<kMass>(above, kMass ? target_of(static_cast<double>(share), all) : want);
             if (lane == 0) sh.complete = !over;
         }
     }
@@ -833,7 +835,7 @@ __device__ __forceinline__ bool Row<T, NT>::search(float lo, float hi, float bot
         }
         __syncwarp();
         barrier();
-        if (warp == 0) find_step<kMass>(above, target, 0, -1.f);
+        if (warp == 0) find_step<kMass>(above, target);
         __syncthreads();
         if (!sh.ok) return false;
         const int bin = sh.bin;
@@ -978,7 +980,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
                 window_hi = top_k <= kList / 2 ? CUDART_INF_F : sh.window_hi;  // (few: all of them to the list, for top-p)
                 const Steps fine(fmaxf(w_lo, bottom), fminf(window_hi, mx));
                 pass<false>(fine, w_lo, window_hi, kLowest, tau_m);
-                const bool found = from_list<false>(fine, w_lo, window_hi, static_cast<u64>(top_k), -1.f, tau_k, target, summed);
+                const bool found = from_list<false>(fine, w_lo, window_hi, static_cast<u64>(top_k), 0.f, tau_k, target, summed);
                 summed &= found;
                 if (!found && !search<false>(kLowest, mx, bottom, static_cast<u64>(top_k), tau_k)) tau_k = kLowest;  // (fewer logits than top_k)
             }
@@ -1022,10 +1024,15 @@ __device__ __forceinline__ void Row<T, NT>::run()
                 float w_lo = from;
                 if (summed && window_hi == CUDART_INF_F) {  // the list has all that top-k left
                     const Steps fine(from, mx);
+                    u64 of_list = 0;
                     for (int i = lane; i < listed; i += 32)
-                        if (sh.list_v[warp * kShare + i] >= from) count<true>(place_of(fine(sh.list_v[warp * kShare + i])), sh.list_w[warp * kShare + i]);
-                    if (lane == 0) sh.warp_b[warp] = 0;
+                        if (sh.list_v[warp * kShare + i] >= from) {
+                            of_list += sh.list_w[warp * kShare + i];
+                            count<true>(place_of(fine(sh.list_v[warp * kShare + i])), sh.list_w[warp * kShare + i]);
+                        }
                     __syncwarp();
+                    of_list = warp_sum(of_list);
+                    if (lane == 0) sh.warp_b[warp] = of_list;
                     const bool found = from_list<true>(fine, from, window_hi, 0, fmaxf(top_p, 0.f), tau_p, target, summed);
                     summed &= found;
                     if (!found) (void)search<true>(from, mx, bottom, target, tau_p);
@@ -1147,11 +1154,10 @@ __device__ __forceinline__ void Row<T, NT>::run()
             four(j, end, l);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                // 2^((l - max) * octaves) in fp32: the product in two parts, its whole octaves apart
+                // 2^((l - max) * octaves) in fp32: the product in two parts, the second to first order
                 const float d = fmaxf(l[k], nothing) - mx, z = d * octaves;
-                const float whole_z = rintf(z);
-                const float rest = (z - whole_z) + (fmaf(d, octaves, -z) + d * octaves_low);
-                float x = hawk::fast_exp2(rest) * __uint_as_float(static_cast<uint32_t>(static_cast<int>(whole_z) + 127) << 23) * factor;
+                const float e = hawk::fast_exp2(z), low = fmaf(d, octaves, -z) + d * octaves_low;
+                float x = fmaf(e, low * 0.69314718f, e) * factor;
                 if (!in_range) x = share(fmaxf(l[k], nothing), inv_total);
                 p[k] = greedy || !some || !(l[k] >= tau) || l[k] < nothing ? 0.f : x;
             }
