@@ -19,6 +19,12 @@
 //
 // A block holds 40960 ids at most; longer rows, and rows of calls with few of them, are shared by a cluster, whose blocks exchange
 // histograms, members and sums through distributed shared memory.
+//
+// What bounds it: instructions and latency, not memory.  512 rows of 16384 ids with their distributions are 67 MB, 10 us, and take 67: some 130
+// warp instructions for each 32 ids (the pass 45 of them, loading 12, the fp32 mass 8, the distribution 14), 0.4 of the issue slots used by
+// two blocks an SM.  A row alone takes 12.4 to 15 us, a chain of some ten barriers with a warp's work between them.  Measured and not kept:
+// sorting out the ids below an estimated cut first (a pass to pack costs what it saves, 118 us); every warp summing up the histograms
+// for itself (7 thousand cycles of 32); 64-bit atomics in shared memory (loops, ten times the three 32-bit ones where ids share a step).
 #include <climits>
 
 #include <math_constants.h>
@@ -1269,10 +1275,10 @@ extern "C" hawk_status hawk_sample(const hawk_sample_args *a, int32_t *dev_statu
     P.token_prob = a->token_prob;
     P.probs = a->probs;
     P.dev_status = dev_status;
-    // Blocks of a row.  Few rows: about 4096 ids a block (one row of 16384 ids 13.9 us in one block of 512 threads, 12.3 in four; of 100003
-    // in bf16 23.7 in three, 18.9 in eight).  Up to two waves of blocks: 20480 ids (48 rows of 100003: 47 us in three, 40 in
-    // five).  Else as few as hold the row (200 rows of 100003: 129 us in three, 174 in five).  Below, calls of more rows than SMs: blocks
-    // of 256 threads, two on an SM (512 rows of 16384: 51 us, 61 with 512 threads; 148 rows: 18.7 and 14.4).
+    // Blocks of a row.  Few rows: about 4096 ids a block (one row of 16384 ids, top-k 2000: 13.4 us in one block of 512 threads, 12.4 in
+    // four; of 100003 in bf16 23.0 in three, 18.7 in eight).  Up to two waves of blocks: 20480 ids (48 rows of 100003: 45.6 us in three, 38.8
+    // in five).  Else as few as hold the row (200 rows of 100003: 125 us in three, 162 in five).  Below, calls of more rows than SMs: blocks
+    // of 256 threads, two on an SM (512 rows of 16384: 48.6 us, 59.2 with 512 threads; 148 rows: 18.0 and 14.0).
     const auto blocks_of = [&](int ids) { return (n + ids - 1) / ids; };
     P.cluster = blocks_of(kMaxSlice);
     int more = 1;
