@@ -347,7 +347,7 @@ __device__ __forceinline__ int Row<T, NT>::load(long long row, int first, int n,
     // whole pieces, where those of both rows lie alike
     const bool alike = ((reinterpret_cast<uintptr_t>(c) ^ reinterpret_cast<uintptr_t>(u)) & 15u) == 0;
     const int q0 = pad > 0 ? 1 : 0, q1 = alike ? (pad + n) / kN : q0;
-    constexpr int kFlight = (sizeof(T) == 4 ? 4 : 2) * (NT <= 256 ? 2 : 1);
+    constexpr int kFlight = sizeof(T) == 4 ? 4 : 2;
     for (int q = q0 + threadIdx.x; q < q1; q += NT * kFlight) {
         Piece<T> pc[kFlight], pu[kFlight];
 #pragma unroll
@@ -1192,8 +1192,8 @@ __device__ __forceinline__ void Row<T, NT>::run()
 
 constexpr size_t kValsAt = (sizeof(SampleShared) + 15) / 16 * 16;
 
-template <typename T, int NT>
-__global__ void __launch_bounds__(NT, 1) sample_kernel(const __grid_constant__ SampleParams P)
+template <typename T, int NT, int kOnSm>
+__global__ void __launch_bounds__(NT, kOnSm) sample_kernel(const __grid_constant__ SampleParams P)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     hawk::allow_dependent_launch();
@@ -1203,7 +1203,7 @@ __global__ void __launch_bounds__(NT, 1) sample_kernel(const __grid_constant__ S
     row.run();
 }
 
-template <typename T, int NT>
+template <typename T, int NT, int kOnSm>
 hawk_status launch(const SampleParams &P, int R, cudaStream_t st)
 {
     static unsigned long long seen = 0;  // devices on which the kernel may use the shared memory of its largest slice
@@ -1212,15 +1212,15 @@ hawk_status launch(const SampleParams &P, int R, cudaStream_t st)
     if (cudaGetDevice(&dev) != cudaSuccess) return HAWK_ERR_CUDA;
     const unsigned long long bit = 1ull << (dev & 63);
     if (!(__atomic_load_n(&seen, __ATOMIC_ACQUIRE) & bit) || dev >= 64) {
-        if (cudaFuncSetAttribute(sample_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)) != cudaSuccess)
+        if (cudaFuncSetAttribute(sample_kernel<T, NT, kOnSm>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)) != cudaSuccess)
             return HAWK_ERR_CUDA;
         __atomic_fetch_or(&seen, bit, __ATOMIC_RELEASE);
     }
     const size_t smem = kValsAt + sizeof(float) * (static_cast<size_t>(P.slice) + 16);
     const dim3 grid(static_cast<unsigned>(R) * P.cluster);
     const cudaError_t e = P.cluster > 1
-                              ? hawk_host::launch_dependent_clusters(sample_kernel<T, NT>, P.cluster, grid, dim3(NT), smem, st, P)
-                              : hawk_host::launch_dependent(sample_kernel<T, NT>, grid, dim3(NT), smem, st, P);
+                              ? hawk_host::launch_dependent_clusters(sample_kernel<T, NT, kOnSm>, P.cluster, grid, dim3(NT), smem, st, P)
+                              : hawk_host::launch_dependent(sample_kernel<T, NT, kOnSm>, grid, dim3(NT), smem, st, P);
     return e == cudaSuccess ? HAWK_OK : HAWK_ERR_CUDA;
 }
 
@@ -1277,8 +1277,7 @@ extern "C" hawk_status hawk_sample(const hawk_sample_args *a, int32_t *dev_statu
     P.dev_status = dev_status;
     // Blocks of a row.  Few rows: about 4096 ids a block (one row of 16384 ids, top-k 2000: 13.4 us in one block of 512 threads, 12.4 in
     // four; of 100003 in bf16 23.0 in three, 18.7 in eight).  Up to two waves of blocks: 20480 ids (48 rows of 100003: 45.6 us in three, 38.8
-    // in five).  Else as few as hold the row (200 rows of 100003: 125 us in three, 162 in five).  Below, calls of more rows than SMs: blocks
-    // of 256 threads, two on an SM (512 rows of 16384: 48.6 us, 59.2 with 512 threads; 148 rows: 18.0 and 14.0).
+    // in five).  Else as few as hold the row (200 rows of 100003: 125 us in three, 162 in five).
     const auto blocks_of = [&](int ids) { return (n + ids - 1) / ids; };
     P.cluster = blocks_of(kMaxSlice);
     int more = 1;
@@ -1289,7 +1288,10 @@ extern "C" hawk_status hawk_sample(const hawk_sample_args *a, int32_t *dev_statu
     const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     auto pick = [&](auto type) {
         using T = decltype(type);
-        return P.cluster == 1 && P.slice <= 16384 && a->R > 148 ? launch<T, 256>(P, a->R, st) : launch<T, 512>(P, a->R, st);
+        // Calls of more rows than SMs: two blocks of 512 threads on an SM (512 rows of 16384 ids 40 us, 59 with one; 100 rows 19.5 and 14.0,
+        // because two blocks go to an SM while others have none), four of 256 for short rows (2000 rows of 4096 ids 58 us, 73 with 512).
+        if (P.cluster > 1 || P.slice > 16384 || a->R <= 148) return launch<T, 512, 1>(P, a->R, st);
+        return P.slice > 8192 ? launch<T, 512, 2>(P, a->R, st) : launch<T, 256, 4>(P, a->R, st);
     };
     return a->dtype == HAWK_F32 ? pick(float{}) : a->dtype == HAWK_BF16 ? pick(__nv_bfloat16{}) : pick(__half{});
 }
