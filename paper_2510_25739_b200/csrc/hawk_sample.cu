@@ -1275,15 +1275,23 @@ extern "C" hawk_status hawk_sample(const hawk_sample_args *a, int32_t *dev_statu
     P.token_prob = a->token_prob;
     P.probs = a->probs;
     P.dev_status = dev_status;
-    // Blocks of a row.  Few rows: about 4096 ids a block (one row of 16384 ids, top-k 2000: 13.4 us in one block of 512 threads, 12.4 in
-    // four; of 100003 in bf16 23.0 in three, 18.7 in eight).  Up to two waves of blocks: 20480 ids (48 rows of 100003: 45.6 us in three, 38.8
+    // Blocks of a row.  Where all blocks run at once (132 in clusters, which do not reach every SM): as many as keep it so, of 4096 ids for
+    // a few rows (one row of 16384 ids, top-k 2000: 13.4 us in one block, 12.4 in four; of 100003 in bf16 23.0 in three, 18.7 in
+    // eight), of 8192 for more (32 rows of 50257: 21.8 us in two, 17.4 in four; 64 rows: 21.9 in two, 38 in three); rows of 16384 and
+    // less then stay in one (64 rows: 13.9 us, 14.7 in two).  Up to two waves of blocks: 20480 ids (48 rows of 100003: 45.8 us in three, 38.8
     // in five).  Else as few as hold the row (200 rows of 100003: 125 us in three, 162 in five).
     const auto blocks_of = [&](int ids) { return (n + ids - 1) / ids; };
-    P.cluster = blocks_of(kMaxSlice);
-    int more = 1;
-    if (a->R <= 16) more = n / 4096 < kMaxCluster ? n / 4096 : kMaxCluster;
-    else if (static_cast<long long>(a->R) * blocks_of(20480) <= 2 * 148) more = blocks_of(20480) < kMaxCluster ? blocks_of(20480) : kMaxCluster;
-    if (more > P.cluster) P.cluster = more;
+    const long long rows = a->R;
+    const int least = blocks_of(kMaxSlice);
+    int blocks = 1;
+    if (rows * least <= (least > 1 ? 132 : 148)) {
+        blocks = rows <= 16 ? n / 4096 : n > 16384 ? n / 8192 : 1;
+        if (rows * blocks > 132) blocks = static_cast<int>(132 / rows);
+    } else if (rows * blocks_of(20480) <= 2 * 148) {
+        blocks = blocks_of(20480);
+    }
+    if (blocks > kMaxCluster) blocks = kMaxCluster;
+    P.cluster = blocks > least ? blocks : least;
     P.slice = ((n + P.cluster - 1) / P.cluster + 15) & ~15;  // (every block's rows then lie alike in 16-byte pieces)
     const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     auto pick = [&](auto type) {

@@ -263,3 +263,17 @@ def test_refusals_with_tensors():
     with pytest.raises(binding.HawkError):
         hawk.sample(x, u, v_begin=5, v_end=101)
     assert hawk.sample(x[:0], u[:0]).shape == (0,)
+
+
+@pytest.mark.parametrize("rows, V", [(16, 8192), (17, 20000), (32, 50257), (33, 50257), (100, 32000), (150, 32000), (149, 8193), (150, 16384),
+                                     (40, 100003)])
+def test_launch_shapes(rows, V):
+    """Every way that a call's rows are dealt out to blocks gives the tokens of each row alone."""
+    logits, u = _logits(rows, V, "bf16", seed=rows)
+    kw = dict(top_k=1500, top_p=0.95)
+    probs, one = torch.full((rows, V), NAN, device="cuda"), torch.full((1, V), NAN, device="cuda")
+    got = hawk.sample(logits, u, probs=probs, **kw)
+    for r in (0, rows // 2, rows - 1):
+        assert int(hawk.sample(logits[r:r + 1], u[r:r + 1], probs=one, **kw)) == int(got[r])
+        assert torch.equal(one[0], probs[r])
+    assert _check(logits[:8], u[:8], **kw) == 0
