@@ -20,9 +20,9 @@
 // A block holds 40960 ids at most; longer rows, and rows of calls with few of them, are shared by a cluster, whose blocks exchange
 // histograms, members and sums through distributed shared memory.
 //
-// What bounds it: instructions and latency, not memory.  512 rows of 16384 ids with their distributions are 67 MB, 10 us, and take 67: some 130
-// warp instructions for each 32 ids (the pass 45 of them, loading 12, the fp32 mass 8, the distribution 14), 0.4 of the issue slots used by
-// two blocks an SM.  A row alone takes 12.4 to 15 us, a chain of some ten barriers with a warp's work between them.  Measured and not kept:
+// What bounds it: instructions and latency, not memory.  512 rows of 16384 ids with their distributions are 67 MB, 10 us, and take 56.5: some 130
+// warp instructions for each 32 ids (the pass 45 of them, loading 12, the fp32 mass 8, the distribution 14), 0.53 of the issue slots used by
+// two blocks an SM over 1.7 waves.  A row alone takes 12.4 to 15 us, a chain of some ten barriers with a warp's work between them.  Measured and not kept:
 // sorting out the ids below an estimated cut first (a pass to pack costs what it saves, 118 us); every warp summing up the histograms
 // for itself (7 thousand cycles of 32); 64-bit atomics in shared memory (loops, ten times the three 32-bit ones where ids share a step).
 #include <climits>
