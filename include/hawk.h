@@ -700,7 +700,7 @@ hawk_status hawk_pages_fork(const hawk_pages_fork_args *args, int32_t *dev_statu
  *   top        int32 [1] or NULL: all pages from this id on are free then (at least first_page, which is at most n_pages)
  *   workspace  at least hawk_pages_compact_workspace_bytes(n_pages, max_moves) bytes, 16-byte aligned, no initialisation; calls that may
  *              overlap on the GPU need one each
- * A page that the caller holds by a count of its own moves like the others (copies tell where).
+ * A page that the caller holds by a count of its own moves like the others (copies tell where).  n_pages >= 1.
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, CUDA.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct hawk_pages_compact_args {
