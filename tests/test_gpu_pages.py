@@ -390,3 +390,24 @@ def test_refusals_with_tensors():
         hawk.pages_copy(k, v[0], sv.int32([[0, 1, 16]]))
     with pytest.raises(TypeError, match="k_pages"):
         hawk.pages_copy(k.float(), v, sv.int32([[0, 1, 16]]))
+
+
+@pytest.mark.parametrize("S, S_out, width, n_pages", [(1, 32, 128, 4096), (32, 1, 128, 4095), (32, 32, 129, 4096), (33, 2, 4, 50), (2, 33, 4, 50),
+                                                      (7, 9, 128, 4097), (3, 3, 5, 1), (0, 4, 3, 6), (5, 0, 3, 6)])
+def test_fork_sizes_of_one_block(S, S_out, width, n_pages):
+    """The sizes around which one block does it all: old streams with every page of the pool among them, some kept, some left."""
+    page, r = 4, np.random.RandomState(S + width)
+    lens = r.randint(0, width * page + 1, S)
+    lens[:1] = width * page
+    table = r.randint(0, n_pages, (S, width))
+    refs = np.zeros(n_pages, np.int64)
+    for s in range(S):
+        np.add.at(refs, table[s, :serving.pages(int(lens[s]), page)], 1)
+    parent, length = (r.randint(-1, S, S_out) if S else np.full(S_out, -1)), r.randint(0, width * page + 9, S_out)
+    want = serving.fork(table.tolist(), lens.tolist(), parent.tolist(), refs.tolist(), page, length.tolist())
+    args = [torch.from_numpy(np.ascontiguousarray(x)).to(torch.int32).cuda() for x in (table, lens, parent, refs, length)]
+    for in_place in (False, True):
+        out_refs, status = args[3] if in_place else torch.full_like(args[3], -5), _status()
+        got_table, got_len = hawk.pages_fork(args[0], args[1], args[2], args[3], page, length=args[4], out_refs=out_refs, dev_status=status)
+        assert int(status) == 0 and got_len.tolist() == want[1] and out_refs.tolist() == want[2]
+        assert sv.same_where_written(got_table, want[0])
