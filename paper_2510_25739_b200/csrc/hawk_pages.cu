@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(ForkParams P)
 }
 
 // Small states whose counts go to another tensor: one block, a warp a stream, the changes of the counts in shared memory, so that no launch
-// ahead has to copy them.  In a graph 2.0 -> 1.7 us for 2 streams over 64 pages and 2.5 -> 2.2 for 16 over 700, launched one by one 4.3 -> 3.0; but
+// ahead has to copy them.  In a graph 2.0 -> 1.7 us for 2 streams over 64 pages and 2.5 -> 2.0 for 16 over 700, launched one by one 4.3 -> 3.1; but
 // 2.6 and 3.2 for 16 streams of 256 entries, 2.6 and 3.8 for 64 of 64.
 constexpr int kForkStreams = kBookWarps, kForkWidth = 128, kForkPages = 4 * kBookThreads;
 
