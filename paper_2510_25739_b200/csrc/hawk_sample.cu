@@ -211,7 +211,7 @@ private:
     int m, rank, flags = 0;
     int base, end;      // the warp's stretch of ids
     int listed;         // its members of the list
-    float mx, nothing;  // the largest; from `nothing`, 32 temperatures below it, down a weight is 0
+    float mx, nothing;  // the largest; from `nothing`, 32 temperatures below it or more, down a weight is 0
     double rate;        // kParts / (temperature * ln 2)
 
     __device__ __forceinline__ bool shared() const { return P.cluster > 1; }
@@ -241,7 +241,8 @@ private:
         return fma(f, r * fma(r, fma(r, c3, c2), c1), f);
     }
     // ... as a multiple of 2^-44, not yet whole.  The last bit is set, so that no sum of it is a tie: added to a number between 2^52 and 2^53 it
-    // counts as the nearest whole multiple, whatever the sum so far.  (At `nothing` and below, -inf too, that is 0: e^-32 of them.)
+    // counts as the nearest whole multiple, whatever the sum so far.  (At `nothing` and below that is 0: e^-32 of them
+    // at most.  -inf takes the weight of `nothing`, which is more where that is the lowest number; no threshold lets -inf stay.)
     __device__ __forceinline__ double raw_weight(float l) const
     {
         int e;
@@ -902,7 +903,11 @@ __device__ __forceinline__ void Row<T, NT>::run()
     mx = hi;
     lo = fminf(lo, hi);  // (none of some was a number)
     rate = sh.rate;
-    nothing = fmaxf(fminf(static_cast<float>(static_cast<double>(mx) - 32.0 * static_cast<double>(temperature)), mx), kLowest);
+    // A temperature so low that nothing but the maximum has a weight: the next lower number lies 32 temperatures below it.  Else `nothing` is rounded
+    // downwards (to 96 temperatures below the maximum at most): nearer than 31.2 its own weight, which every lower id takes, would not be 0.
+    const double reach = 32.0 * static_cast<double>(temperature);
+    const bool flat = static_cast<double>(mx) - static_cast<double>(nextafterf(mx, -CUDART_INF_F)) >= reach;
+    nothing = flat ? mx : fmaxf(__double2float_rd(static_cast<double>(mx) - reach), kLowest);
     const bool some = mx > -CUDART_INF_F;
     const int stretch = ((m + NW - 1) / NW + 127) & ~127;  // whole runs of 4 a lane
     base = min(m, warp * stretch);
@@ -945,7 +950,6 @@ __device__ __forceinline__ void Row<T, NT>::run()
                 tau_m = fmaxf(kLowest, fminf(t, mx));
             }
         }
-        const bool flat = nothing >= mx;  // a temperature so low that nothing but the maximum has a weight
         if (flat) tau_m = mx;
         const bool by_k = top_k > 0 && top_k < P.n && !flat;
         const bool by_p = top_p < 1.f && !flat;

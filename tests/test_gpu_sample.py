@@ -277,3 +277,54 @@ def test_launch_shapes(rows, V):
         assert int(hawk.sample(logits[r:r + 1], u[r:r + 1], probs=one, **kw)) == int(got[r])
         assert torch.equal(one[0], probs[r])
     assert _check(logits[:8], u[:8], **kw) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(top_k=3), dict(top_p=0.999999), dict(min_p=1e-30), dict(top_k=2, top_p=0.5)], ids=str)
+@pytest.mark.parametrize("V", [6, 5000, 50257])
+@pytest.mark.parametrize("top, T", [(40, 1e-6), (300, 1e-5), (500, 1.4e-6), (100, 3.5e-7), (100, 1e-6), (-40, 1e-6), (64, 1e-6), (-2, 9e-9),
+                                    (1e30, 1e22), (7, 1e-20), (7, 1e-45), (0, 1e-45), (-3e38, 1e-6)])
+def test_temperatures_next_to_nothing_beside_the_maximum(top, T, V, kw):
+    """A step of fp32 at the maximum is some temperatures: no id but the maximum has a weight, wherever it stands and whatever the number."""
+    at, u = [0, V // 2, V - 1, 3], torch.tensor([0.0, -1.0, NAN, 1 - 2.0 ** -24, 0.5], device="cuda")
+    x = torch.full((len(at), V), -INF)
+    x[:, 1:] = min(0.0, 0.9 * top if top > 0 else 1.1 * top) if top else -1.0
+    x[:, 4] = torch.tensor(0.5 * top if top > 0 else 1.05 * top if top else -0.5)
+    for r, p in enumerate(at):
+        x[r, p] = top
+    x = x.cuda()
+    one = torch.zeros_like(x)
+    one[range(len(at)), at] = 1
+    for number in u:
+        prob, probs, status = torch.full((len(at),), NAN, device="cuda"), torch.full_like(x, NAN), torch.zeros(1, dtype=torch.int32, device="cuda")
+        token = hawk.sample(x, number.expand(len(at)).contiguous(), temperature=T, token_prob=prob, probs=probs, dev_status=status, **kw)
+        assert token.tolist() == at and (prob == 1).all() and torch.equal(probs, one) and int(status) == 0
+
+
+@pytest.mark.parametrize("top, T", [(40, 1e-6), (300, 1e-5), (100, 1e-6), (-40, 1e-6), (500, 1e-5), (-300, 2e-5)])
+def test_neighbours_of_the_maximum_at_low_temperatures(top, T):
+    """Ids some steps of fp32 below the maximum among others far below: those of a weight of 2^-45 and more are drawn, no others."""
+    V = 3000
+    r, top32, T32 = np.random.RandomState(abs(top)), np.float32(top), np.float64(np.float32(T))
+    x = np.full(V, np.float32(top - abs(top) / 2), np.float32)
+    below = [top32]
+    for _ in range(14):
+        below.append(np.nextafter(below[-1], np.float32(-np.inf)))
+    place = np.sort(r.choice(V, 15, replace=False))
+    x[place] = r.permutation(below)
+    w = np.exp((x.astype(np.float64) - np.float64(top32)) / T32)
+    assert (np.abs(w * 2.0 ** 45 - 1) > 1e-3).all()
+    w[w < 2.0 ** -45] = 0
+    run = np.cumsum(w)
+    u = [0.0, -2.0, NAN, 0.3, 0.9, 0.99]
+    want = [int(np.searchsorted(run, (n if n > 0 else 0.0) * run[-1], side="right")) for n in u]
+    bound = serving.weight_error(V, 1 / run[-1]) + 2.0 ** -24
+    for n in u[3:]:
+        assert np.abs(run / run[-1] - n).min() > bound
+    logits = torch.from_numpy(x).cuda().expand(len(u), V)
+    prob, probs = torch.full((len(u),), NAN, device="cuda"), torch.full((len(u), V), NAN, device="cuda")
+    token = hawk.sample(logits, torch.tensor(u, device="cuda"), temperature=T, token_prob=prob, probs=probs)
+    assert token.tolist() == want
+    z = np.clip((x.astype(np.float64) - np.float64(top32)) / T32, -1e4, 0)
+    p = w / run[-1]
+    assert (np.abs(probs.double().cpu().numpy() - p) <= sv.prob_bound(p, z)).all()
+    assert (np.abs(prob.double().cpu().numpy() - p[want]) <= sv.prob_bound(p[want], z[want])).all() and (prob > 0).all()
