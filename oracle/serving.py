@@ -82,7 +82,8 @@ def resize(table, kv, new, refs, page):
     S, W = len(table), len(table[0]) if len(table) else 0
     out = [[None] * W for _ in range(S)]
     refs, lens, copies = list(refs), list(kv), [(-1, -1, 0)] * S
-    ok = [0 <= a <= W * page and 0 <= b <= W * page for a, b in zip(kv, new)]
+    new = [b if 0 <= b <= W * page else a for a, b in zip(kv, new)]  # (out of range: the stream stays as it is)
+    ok = [0 <= a <= W * page for a in kv]
     for s in range(S):
         if ok[s] and new[s] < kv[s]:
             for j in range(pages(new[s], page), pages(kv[s], page)):

@@ -175,7 +175,7 @@ struct ResizeShared {
     uint32_t bits[kSlice / 32];  // the share's free pages
     int before[kSlice / 32];     // free pages of the share in front of each word
     int end[kMaxStreams];        // running sum of the pages that streams need
-    int kv[kMaxStreams], next[kMaxStreams];  // lengths; -1: out of range, the stream stays as it is
+    int kv[kMaxStreams], next[kMaxStreams];  // lengths, `next` the old one where the new one is out of range; -1: the old one is
     int last[kMaxStreams];       // the page that a stream grows into, -1: none
     int sums[kBookWarps];
     int slot;
@@ -229,11 +229,14 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(ResizeParams P)
         for (int i = max(first, end & ~3) + tid; i < end; i += kBookThreads) P.out_refs[i] = P.refs[i];
     }
     for (int s = tid; s < P.S; s += kBookThreads) {
-        const int old = P.kv[s], next = P.next[s];
-        const bool ok = old >= 0 && old <= cap && next >= 0 && next <= cap;
-        if (!ok) flags |= HAWK_DEV_BAD_PREFIX;
+        int old = P.kv[s], next = P.next[s];
+        const bool held = old >= 0 && old <= cap;
+        if (!held || next < 0 || next > cap) {  // the stream stays as it is
+            flags |= HAWK_DEV_BAD_PREFIX;
+            next = old = held ? old : -1;
+        }
         int last = -1;
-        if (ok && next > old) {
+        if (next > old) {
             uint32_t part;
             const int full = static_cast<int>(P.div.page.divmod(static_cast<uint32_t>(old), part));
             if (part != 0) {
@@ -244,8 +247,8 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(ResizeParams P)
                 }
             }
         }
-        sh.kv[s] = ok ? old : -1;
-        sh.next[s] = ok ? next : -1;
+        sh.kv[s] = old;
+        sh.next[s] = next;
         sh.last[s] = last;
     }
     __syncthreads();

@@ -411,3 +411,22 @@ def test_fork_sizes_of_one_block(S, S_out, width, n_pages):
         got_table, got_len = hawk.pages_fork(args[0], args[1], args[2], args[3], page, length=args[4], out_refs=out_refs, dev_status=status)
         assert int(status) == 0 and got_len.tolist() == want[1] and out_refs.tolist() == want[2]
         assert sv.same_where_written(got_table, want[0])
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("S, spare", [(7, 60), (700, 4000)])
+def test_streams_of_lengths_out_of_range_keep_their_entries(S, spare, in_place):
+    """A stream with a sound length and a new one out of range stays as it is, entries included; one whose own length is out of range
+    has none that could be told.  The others go on as if it were not asked."""
+    page = 8
+    st, r = _state(S, page, 90 + S, spare=spare)
+    most = len(st.table[0]) * page
+    new = [int(np.clip(n + r.randint(-20, 20), 0, most)) for n in st.lens]
+    for s, bad in zip(range(0, S, 3), [-1, most + 1, -(1 << 31), (1 << 31) - 1] * S):
+        new[s] = bad
+    st.lens[1] = -3  # (its pages keep their counts)
+    want_table, want_len, want_refs, want_copies, stayed = serving.resize(st.table, st.lens, new, st.refs, page)
+    assert not stayed and want_len[::3] == st.lens[::3] and want_table[0][0] == st.table[0][0]
+    table, lens, refs, copies, status = _resize(st, new, in_place)
+    assert status == binding.DEV_BAD_PREFIX and lens.tolist() == want_len and refs.tolist() == want_refs
+    assert [tuple(c) for c in copies.tolist()] == want_copies and sv.same_where_written(table, want_table)
