@@ -978,8 +978,10 @@ extern "C" hawk_status hawk_pages_copy(const hawk_page_tensors *pages, const int
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
     const PageParams P = page_params(*pages, dev_status);
     const long long all = static_cast<long long>(P.H) * P.page_size * P.pieces;
-    // 4096 pages of 40 KB: 72 us with a page in two blocks, 68 in one; 16 pages of 98 KB: 5.2 us in twice as many blocks, 6.0 else
-    const long long share = static_cast<long long>(n_copies) * 2 * pages->layers >= 4 * 148 ? 2 * kCopyPieces : kCopyPieces;
+    // 4096 pages of 40 KB: 72 us with a page in two blocks, 68 in one; 16 pages of 98 KB: 5.2 us in twice as many blocks, 6.0 else.  A grid has
+    // 65535 blocks along z at most: the largest pages (2^27 pieces) take the larger share in any call.
+    const bool many = static_cast<long long>(n_copies) * 2 * pages->layers >= 4 * 148 || all > 65535ll * kCopyPieces;
+    const long long share = many ? 2 * kCopyPieces : kCopyPieces;
     const dim3 grid(n_copies, 2 * pages->layers, static_cast<unsigned>((all + share - 1) / share));
     return done(hawk_host::launch_dependent(copy_kernel, grid, dim3(kCopyThreads), 0, reinterpret_cast<cudaStream_t>(stream), P, copies,
                                             static_cast<uint32_t>(share)));

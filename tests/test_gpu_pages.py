@@ -430,3 +430,15 @@ def test_streams_of_lengths_out_of_range_keep_their_entries(S, spare, in_place):
     table, lens, refs, copies, status = _resize(st, new, in_place)
     assert status == binding.DEV_BAD_PREFIX and lens.tolist() == want_len and refs.tolist() == want_refs
     assert [tuple(c) for c in copies.tolist()] == want_copies and sv.same_where_written(table, want_table)
+
+
+@pytest.mark.parametrize("H, page, D", [(65536, 128, 128), (1, 16384, 65536), (2, 65531, 8192), (2, 65535, 8192)])
+def test_copy_of_the_largest_pages(H, page, D):
+    """Pages of 2^30 elements and a little less, in calls of few copies: as many blocks a page as a grid has."""
+    k = torch.zeros((2, H, page, D), dtype=torch.bfloat16, device="cuda")
+    k[0, 0, 0] = 1.5
+    k[0, H - 1, page - 2] = 2.5
+    k[0, H // 2, page // 2, D // 2] = 3.5
+    k[0, H - 1, page - 1] = 4.5
+    hawk.pages_copy(k, k, sv.int32([(0, 1, page - 1)]))
+    assert torch.equal(k[1, :, :page - 1], k[0, :, :page - 1]) and (k[1, :, page - 1] == 0).all()
