@@ -658,6 +658,8 @@ hawk_status hawk_sample(const hawk_sample_args *args, int32_t *dev_status, hawk_
  *   2. A stream that grows takes ceil(new/page_size) - ceil(old/page_size) pages; and one more if its last page is partly filled and,
  *      after step 1, named by other entries too: it gets a copy of its own, copies[s] = (shared page, new page, old % page_size), and
  *      releases the shared one (all streams that grow into a shared page do, the last of them as well).
+ *      (A last page whose count is then 0 or less, which its entry contradicts, is flagged HAWK_DEV_BAD_PAGE; by its count it is free, and
+ *      may be given to a stream.)
  *      Pages are those that are free after step 1, lowest id first, to streams in ascending order, each stream's entries in ascending
  *      order (the copy's is the first).
  *   3. When the pages run out, the streams from there on that need any stay as they were, HAWK_DEV_NO_PAGES.

@@ -310,7 +310,11 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(ResizeParams P)
         const int old = sh.kv[s], next = sh.next[s];
         if (next <= old) continue;
         need[i] = P.div.pages(next) - P.div.pages(old);
-        if (sh.last[s] >= 0 && __ldcg(P.out_refs + sh.last[s]) > 1) ++need[i];
+        // A count of 0 contradicts the entry.  (The block whose share the page is in sees it for certain: only that one may hand the page out, behind
+        // this loop.)
+        const int count = sh.last[s] >= 0 ? __ldcg(P.out_refs + sh.last[s]) : 1;
+        if (count <= 0) flags |= HAWK_DEV_BAD_PAGE;
+        if (count > 1) ++need[i];
         else sh.last[s] = -1;  // (from here on: the page that is copied)
         sum += need[i];
     }

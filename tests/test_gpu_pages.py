@@ -442,3 +442,32 @@ def test_copy_of_the_largest_pages(H, page, D):
     k[0, H - 1, page - 1] = 4.5
     hawk.pages_copy(k, k, sv.int32([(0, 1, page - 1)]))
     assert torch.equal(k[1, :, :page - 1], k[0, :, :page - 1]) and (k[1, :, page - 1] == 0).all()
+
+
+@pytest.mark.parametrize("count", [0, -2])
+@pytest.mark.parametrize("S, spare", [(5, 60), (700, 4000)])
+def test_growing_into_a_page_without_a_count(S, spare, count):
+    """A stream grows into a page that the counts say is free: flagged in every launch, also where the call hands that page to a stream."""
+    page, width = 8, 16
+    lens = [21] + [16] * (S - 1)
+    n_pages = sum(serving.pages(n, page) for n in lens) + spare
+    for seed, grown in ((0, 22), (1, 25), (2, 24)):
+        st = sv.PageState(lens, page, width, n_pages, seed=seed)
+        last = st.table[0][2]
+        st.refs[last] = count
+        new = [grown] + [16 + 8 * 2] * (S // 3) + [16] * (S - 1 - S // 3)
+        want_table, want_len, want_refs, want_copies, stayed = serving.resize(st.table, st.lens, new, st.refs, page)
+        for _ in range(4):
+            table, got_len, refs, copies, status = _resize(st, new, False)
+            assert status == binding.DEV_BAD_PAGE | (binding.DEV_NO_PAGES if stayed else 0)
+            assert got_len.tolist() == want_len and refs.tolist() == want_refs and [tuple(c) for c in copies.tolist()] == want_copies
+            assert sv.same_where_written(table, want_table)
+    st = sv.PageState(lens, page, width, n_pages, seed=0)
+    st.refs[st.table[0][2]] = count
+    assert _resize(st, [21] + [16] * (S - 1), True)[4] == 0  # (who does not grow into it is not looked at)
+
+
+def test_a_page_released_by_one_stream_while_another_that_names_it_grows():
+    st = sv.PageState([21, 21], 8, 5, 30, share=2, seed=3, fresh=1.0)
+    st.refs[st.table[0][2]] = 1  # two entries name it
+    assert _resize(st, [0, 22], True)[4] == binding.DEV_BAD_PAGE
