@@ -594,11 +594,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(CompactParams 
     }
     if (P.top && rank == 0 && tid == 0) *P.top = moved == all_moves ? border : __ldcg(P.from + moved) + 1;
 
-    // ---- the new ids into the table: runs of 128 entries a warp
-    if (moved == 0 && P.out_table == P.table) {
-        report(P.dev_status, flags);
-        return;
-    }
+    // ---- the new ids into the table: runs of 128 entries a warp (in place with nothing to move too, for what is to be flagged)
     const int lowest = moved > 0 ? __ldcg(P.from + moved - 1) : INT_MAX;  // pages in use from here on move
     const int runs = P.S * static_cast<int>(P.div_runs.d);
     for (int t = rank * kBookWarps + warp; t < runs; t += kBlocks * kBookWarps) {

@@ -471,3 +471,26 @@ def test_a_page_released_by_one_stream_while_another_that_names_it_grows():
     st = sv.PageState([21, 21], 8, 5, 30, share=2, seed=3, fresh=1.0)
     st.refs[st.table[0][2]] = 1  # two entries name it
     assert _resize(st, [0, 22], True)[4] == binding.DEV_BAD_PAGE
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("moves", [0, 5])
+@pytest.mark.parametrize("S, n_pages", [(4, 16), (300, 4096)])
+def test_compact_with_nothing_to_move_looks_at_lengths_and_ids(S, n_pages, moves, in_place):
+    """A full pool: lengths and ids out of range are flagged as where pages move, and nothing changes."""
+    st = sv.PageState([8 * (n_pages // S)] * S, 8, n_pages // S + 2, n_pages, seed=S)
+    st.refs = [max(1, c) for c in st.refs]
+    for what in ("length", "id", "both", "none"):
+        table, lens, refs = st.cuda()
+        want = 0
+        if what in ("length", "both"):
+            lens[S - 1], want = -1, want | binding.DEV_BAD_PREFIX
+        if what in ("id", "both"):
+            table[1, 2], want = n_pages, want | binding.DEV_BAD_PAGE
+        out = {} if in_place else dict(out_table=torch.full_like(table, -9), out_refs=torch.zeros_like(refs))
+        status, before = _status(), table.clone()
+        copies = hawk.pages_compact(table, lens, refs, 8, moves, dev_status=status, **out)
+        assert int(status) == want and (copies == torch.tensor([-1, -1, 0], device="cuda")).all()
+        assert torch.equal(table, before) and out.get("out_refs", refs).tolist() == st.refs
+        used = n_pages // S
+        assert torch.equal(out.get("out_table", table)[:S - 1, :used], before[:S - 1, :used])
