@@ -691,6 +691,9 @@ bool encode_16bit_4d_sw128(CUtensorMap *map, const void *base, bool bf16, const 
 bool is_sm100(int *sm_count);
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Bases of 32-bit elements.
+template <class... T>
+inline bool aligned4(const T *...p) { return ((reinterpret_cast<uintptr_t>(p) | ... | 0u) & 3u) == 0; }
 
 // The host-side argument checks of the three stage calls, without the device query and without any CUDA call:
 // HAWK_OK means the stage would go on to look at the device and launch.  The stage calls run them first; the

@@ -21,6 +21,7 @@
 namespace {
 
 using hawk_host::aligned16;
+using hawk_host::aligned4;
 
 constexpr int kBookBlocks = 8;       // of the cluster (the largest that every device runs)
 constexpr int kBookThreads = 1024;
@@ -878,6 +879,7 @@ extern "C" hawk_status hawk_pages_resize(const hawk_pages_resize_args *a, int32_
     if (a->S > 0 && (!a->block_table || !a->kv_len || !a->new_len || !a->out_table || !a->out_len || !a->copies)) return HAWK_ERR_NULL;
     if (a->n_pages > 0 && (!a->page_refs || !a->out_refs)) return HAWK_ERR_NULL;
     if (!aligned16(a->page_refs) || !aligned16(a->out_refs)) return HAWK_ERR_ALIGN;
+    if (!aligned4(a->block_table, a->kv_len, a->new_len, a->out_table, a->out_len, a->copies)) return HAWK_ERR_ALIGN;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
     ResizeParams P = {a->block_table, a->kv_len, a->new_len, a->page_refs, a->out_table, a->out_len, a->out_refs, a->copies,
                       a->S, a->table_width, a->n_pages, make_div(a->page_size), dev_status};
@@ -899,6 +901,7 @@ extern "C" hawk_status hawk_pages_fork(const hawk_pages_fork_args *a, int32_t *d
     if (a->S_out > 0 && (!a->parent || !a->out_table || !a->out_len)) return HAWK_ERR_NULL;
     if (a->n_pages > 0 && (!a->page_refs || !a->out_refs)) return HAWK_ERR_NULL;
     if (!aligned16(a->page_refs) || !aligned16(a->out_refs)) return HAWK_ERR_ALIGN;
+    if (!aligned4(a->block_table, a->kv_len, a->parent, a->length, a->out_table, a->out_len)) return HAWK_ERR_ALIGN;
     if ((a->S_out > 0 && a->S > 0) && (a->out_table == a->block_table || a->out_len == a->kv_len)) return HAWK_ERR_PARAM;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
     const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -936,6 +939,7 @@ extern "C" hawk_status hawk_pages_compact(const hawk_pages_compact_args *a, int3
     if (!a->page_refs || !a->out_refs) return HAWK_ERR_NULL;
     if (a->max_moves > 0 && !a->copies) return HAWK_ERR_NULL;
     if (!aligned16(a->page_refs) || !aligned16(a->out_refs) || !aligned16(a->workspace)) return HAWK_ERR_ALIGN;
+    if (!aligned4(a->block_table, a->kv_len, a->out_table, a->copies, a->top)) return HAWK_ERR_ALIGN;
     if (!a->workspace || a->workspace_bytes < hawk_pages_compact_workspace_bytes(a->n_pages, a->max_moves))
         return HAWK_ERR_WORKSPACE;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
@@ -975,6 +979,7 @@ extern "C" hawk_status hawk_pages_copy(const hawk_page_tensors *pages, const int
     const hawk_status chk = check_pages(*pages);
     if (chk != HAWK_OK) return chk;
     if (!copies) return HAWK_ERR_NULL;
+    if (!aligned4(copies)) return HAWK_ERR_ALIGN;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
     const PageParams P = page_params(*pages, dev_status);
     const long long all = static_cast<long long>(P.H) * P.page_size * P.pieces;
@@ -996,12 +1001,14 @@ extern "C" hawk_status hawk_pages_keep(const hawk_pages_keep_args *a, int32_t *d
     if (a->B < 1 || a->S % a->B != 0) return HAWK_ERR_SHAPE;
     if (!a->row_begin || !a->kv_len || !a->accept_len || !a->out_len) return HAWK_ERR_NULL;
     if (a->out_len == a->kv_len) return HAWK_ERR_PARAM;
+    if (!aligned4(a->row_begin, a->kv_len, a->accept_len, a->path, a->out_len)) return HAWK_ERR_ALIGN;
     KeepParams P = {};
     int layers = 1;
     if (a->path) {
         const hawk_status chk = check_pages(a->pages);
         if (chk != HAWK_OK) return chk;
         if (!a->block_table) return HAWK_ERR_NULL;
+        if (!aligned4(a->block_table)) return HAWK_ERR_ALIGN;
         if (static_cast<long long>(a->S) * a->table_width >= (1ll << 31) ||
             static_cast<long long>(a->table_width) * a->pages.page_size >= (1ll << 31) - 65536)
             return HAWK_ERR_UNSUPPORTED;

@@ -1249,7 +1249,8 @@ extern "C" hawk_status hawk_sample(const hawk_sample_args *a, int32_t *dev_statu
         return HAWK_ERR_SHAPE;
     const uintptr_t size = a->dtype == HAWK_F32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(a->logits) % size || reinterpret_cast<uintptr_t>(a->uncond) % size ||
-        reinterpret_cast<uintptr_t>(a->probs) % 4)
+        !hawk_host::aligned4(a->u, a->token, a->token_prob, a->probs, a->row_temperature, a->row_top_k, a->row_top_p, a->row_min_p,
+                             a->row_cfg_scale))
         return HAWK_ERR_ALIGN;
     if (static_cast<long long>(a->R) * kMaxCluster >= (1ll << 31)) return HAWK_ERR_UNSUPPORTED;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;

@@ -250,3 +250,41 @@ def test_plain_keep():
     lens, moves = serving.keep([0, 5, 5, 10], [20, 7, 30], [[2, 4], [-1, -1], [1, 3]], [2, 0, 1], 1)
     assert lens == [15 + 3, 7, 25 + 2] and moves == [(0, 17, 16), (0, 19, 17), (2, 26, 26)]
     assert serving.keep([0, 4], [10], None, [4], 1)[0] == [10]  # the last draft's row was never brought
+
+
+# ---- bases that 32-bit elements cannot have (followed, they would fault)
+@pytest.mark.parametrize("name", ["u", "token", "token_prob", "probs", "row_temperature", "row_top_k", "row_top_p", "row_min_p", "row_cfg_scale"])
+def test_sample_refuses_misaligned_bases(lib, name):
+    for off in (1, 2, 3):
+        a = _filled(sv.SampleArgs, ("logits", "u", "token"), dtype=2, R=3, V=100, v_begin=0, v_end=100, temperature=1.0, top_p=1.0, cfg_scale=1.0,
+                    row_stride=100, probs_row_stride=100, **{name: P + off})
+        assert lib.hawk_sample(ctypes.byref(a), None, None) == E_ALIGN
+
+
+def test_page_calls_refuse_misaligned_bases(lib):
+    def fork(**kw):
+        names = ("block_table", "kv_len", "page_refs", "parent", "length", "out_refs")
+        base = dict(S=2, S_out=3, table_width=4, n_pages=9, page_size=16, out_table=Q, out_len=Q)
+        return lib.hawk_pages_fork(ctypes.byref(_filled(sv.ForkArgs, names, **{**base, **kw})), None, None)
+
+    def compact(**kw):
+        names = ("block_table", "kv_len", "page_refs", "out_table", "out_refs", "copies", "top", "workspace")
+        base = dict(S=2, table_width=4, n_pages=9, page_size=16, first_page=0, max_moves=3, workspace_bytes=1 << 30)
+        return lib.hawk_pages_compact(ctypes.byref(_filled(sv.CompactArgs, names, **{**base, **kw})), None, None)
+
+    def keep(**kw):
+        names = ("block_table", "row_begin", "kv_len", "path", "accept_len")
+        a = _filled(sv.KeepArgs, names, **{**dict(S=4, B=2, table_width=4, path_width=3, first=1, out_len=Q), **kw})
+        a.pages = _tensors()
+        return lib.hawk_pages_keep(ctypes.byref(a), None, None)
+
+    for off in (1, 2, 3):
+        for name in ("block_table", "kv_len", "new_len", "out_table", "out_len", "copies"):
+            assert lib.hawk_pages_resize(ctypes.byref(_resize(**{name: P + off})), None, None) == E_ALIGN
+        for name in ("block_table", "kv_len", "parent", "length", "out_table", "out_len"):
+            assert fork(**{name: P + off}) == E_ALIGN
+        for name in ("block_table", "kv_len", "out_table", "copies", "top"):
+            assert compact(**{name: P + off}) == E_ALIGN
+        assert lib.hawk_pages_copy(ctypes.byref(_tensors()), P + off, 3, None, None) == E_ALIGN
+        for name in ("block_table", "row_begin", "kv_len", "path", "accept_len", "out_len"):
+            assert keep(**{name: P + off}) == E_ALIGN
