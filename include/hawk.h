@@ -650,7 +650,8 @@ hawk_status hawk_sample(const hawk_sample_args *args, int32_t *dev_status, hawk_
  * Lengths outside [0, table_width * page_size] are flagged HAWK_DEV_BAD_PREFIX and their streams stay as they are; a page id outside
  * [0, n_pages) is flagged HAWK_DEV_BAD_PAGE and nothing is counted for it.
  * Supported: S <= 4096, n_pages <= 2^20, page_size <= 65536, S * table_width and table_width * page_size + 65536 below 2^31.
- * page_refs, out_refs, workspaces and pages are 16-byte aligned, the other tensors as their type is.
+ * page_refs, out_refs, workspaces and pages are 16-byte aligned, the other tensors as their type is.  A tensor without elements (a table
+ * of no width, no layers) may be NULL, but for hawk_pages_keep's path, whose NULL says that there is none.
  *
  * hawk_pages_resize: stream s goes from kv_len[s] to new_len[s] keys.
  *   1. Streams that shrink release the entries they need no more (to 0: the stream is freed).  A count that is 0 already stays 0,

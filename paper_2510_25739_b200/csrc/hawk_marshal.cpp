@@ -659,6 +659,7 @@ PyObject *pages_keep(PyObject *, PyObject *const *args, Py_ssize_t n)
             dims(*path, "path", 2);
             const int64_t shape[2] = {B, path->size(1)};
             a.path = ints(args[6], "path", shape, index);
+            if (!a.path) a.path = a.accept_len;  // (a path without columns has no address, and none of it is read; NULL would be a chain)
             a.path_width = as_int(path->size(1), "path");
             int pages_index;
             a.pages = page_tensors(args[1], args[2], pages_index);

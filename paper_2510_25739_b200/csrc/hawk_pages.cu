@@ -840,7 +840,7 @@ hawk_status check_pages(const hawk_page_tensors &p)
     if (p.H_kv < 1 || p.page_size < 1 || p.D < 1 || p.n_pages < 1) return HAWK_ERR_SHAPE;
     if (p.D % 8 != 0 || p.D > 65536 || p.page_size > 65536 || p.layers > 32767) return HAWK_ERR_UNSUPPORTED;
     if (p.H_kv > 65536 || static_cast<long long>(p.H_kv) * p.page_size > (1ll << 30) / p.D) return HAWK_ERR_UNSUPPORTED;
-    if (!p.k_pages || !p.v_pages) return HAWK_ERR_NULL;
+    if (p.layers > 0 && (!p.k_pages || !p.v_pages)) return HAWK_ERR_NULL;
     if (!aligned16(p.k_pages) || !aligned16(p.v_pages)) return HAWK_ERR_ALIGN;
     const long long strides[] = {p.k_layer_stride, p.k_page_stride, p.k_head_stride, p.k_row_stride,
                                  p.v_layer_stride, p.v_page_stride, p.v_head_stride, p.v_row_stride};
@@ -876,7 +876,8 @@ extern "C" hawk_status hawk_pages_resize(const hawk_pages_resize_args *a, int32_
     const hawk_status chk = check_state(a->S, a->table_width, a->n_pages, a->page_size);
     if (chk != HAWK_OK) return chk;
     if (a->S == 0 && (a->n_pages == 0 || a->page_refs == a->out_refs)) return HAWK_OK;
-    if (a->S > 0 && (!a->block_table || !a->kv_len || !a->new_len || !a->out_table || !a->out_len || !a->copies)) return HAWK_ERR_NULL;
+    if (a->S > 0 && (!a->kv_len || !a->new_len || !a->out_len || !a->copies)) return HAWK_ERR_NULL;
+    if (a->S > 0 && a->table_width > 0 && (!a->block_table || !a->out_table)) return HAWK_ERR_NULL;
     if (a->n_pages > 0 && (!a->page_refs || !a->out_refs)) return HAWK_ERR_NULL;
     if (!aligned16(a->page_refs) || !aligned16(a->out_refs)) return HAWK_ERR_ALIGN;
     if (!aligned4(a->block_table, a->kv_len, a->new_len, a->out_table, a->out_len, a->copies)) return HAWK_ERR_ALIGN;
@@ -897,12 +898,13 @@ extern "C" hawk_status hawk_pages_fork(const hawk_pages_fork_args *a, int32_t *d
     if (chk != HAWK_OK) return chk;
     const bool move = a->n_pages > 0 && a->page_refs != a->out_refs;
     if (a->S == 0 && a->S_out == 0 && !move) return HAWK_OK;
-    if (a->S > 0 && (!a->block_table || !a->kv_len)) return HAWK_ERR_NULL;
-    if (a->S_out > 0 && (!a->parent || !a->out_table || !a->out_len)) return HAWK_ERR_NULL;
+    const bool wide = a->table_width > 0;
+    if (a->S > 0 && ((wide && !a->block_table) || !a->kv_len)) return HAWK_ERR_NULL;
+    if (a->S_out > 0 && (!a->parent || (wide && !a->out_table) || !a->out_len)) return HAWK_ERR_NULL;
     if (a->n_pages > 0 && (!a->page_refs || !a->out_refs)) return HAWK_ERR_NULL;
     if (!aligned16(a->page_refs) || !aligned16(a->out_refs)) return HAWK_ERR_ALIGN;
     if (!aligned4(a->block_table, a->kv_len, a->parent, a->length, a->out_table, a->out_len)) return HAWK_ERR_ALIGN;
-    if ((a->S_out > 0 && a->S > 0) && (a->out_table == a->block_table || a->out_len == a->kv_len)) return HAWK_ERR_PARAM;
+    if ((a->S_out > 0 && a->S > 0) && ((wide && a->out_table == a->block_table) || a->out_len == a->kv_len)) return HAWK_ERR_PARAM;
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
     const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int streams = a->S > a->S_out ? a->S : a->S_out;
@@ -935,7 +937,7 @@ extern "C" hawk_status hawk_pages_compact(const hawk_pages_compact_args *a, int3
     if (chk != HAWK_OK) return chk;
     if (a->n_pages < 1 || a->first_page < 0 || a->first_page > a->n_pages || a->max_moves < 0) return HAWK_ERR_SHAPE;
     if (a->max_moves > kMaxPages) return HAWK_ERR_UNSUPPORTED;
-    if (a->S > 0 && (!a->block_table || !a->kv_len || !a->out_table)) return HAWK_ERR_NULL;
+    if (a->S > 0 && (!a->kv_len || (a->table_width > 0 && (!a->block_table || !a->out_table)))) return HAWK_ERR_NULL;
     if (!a->page_refs || !a->out_refs) return HAWK_ERR_NULL;
     if (a->max_moves > 0 && !a->copies) return HAWK_ERR_NULL;
     if (!aligned16(a->page_refs) || !aligned16(a->out_refs) || !aligned16(a->workspace)) return HAWK_ERR_ALIGN;
@@ -1007,7 +1009,7 @@ extern "C" hawk_status hawk_pages_keep(const hawk_pages_keep_args *a, int32_t *d
     if (a->path) {
         const hawk_status chk = check_pages(a->pages);
         if (chk != HAWK_OK) return chk;
-        if (!a->block_table) return HAWK_ERR_NULL;
+        if (a->table_width > 0 && !a->block_table) return HAWK_ERR_NULL;
         if (!aligned4(a->block_table)) return HAWK_ERR_ALIGN;
         if (static_cast<long long>(a->S) * a->table_width >= (1ll << 31) ||
             static_cast<long long>(a->table_width) * a->pages.page_size >= (1ll << 31) - 65536)

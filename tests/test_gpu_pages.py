@@ -494,3 +494,33 @@ def test_compact_with_nothing_to_move_looks_at_lengths_and_ids(S, n_pages, moves
         assert torch.equal(table, before) and out.get("out_refs", refs).tolist() == st.refs
         used = n_pages // S
         assert torch.equal(out.get("out_table", table)[:S - 1, :used], before[:S - 1, :used])
+
+
+def test_tensors_without_elements():
+    """Tables of no width, pages of no layers and paths of no columns have no address, and are not taken for missing."""
+    none, zero = sv.int32(np.zeros((3, 0))), sv.int32([0, 0, 0])
+    refs, status = sv.int32([0, 1, 0, 2, 0]), _status()
+    for out in ({}, dict(out_table=sv.int32(np.zeros((3, 0))), out_len=sv.int32([5, 5, 5]), out_refs=sv.int32([9] * 5))):
+        lens = zero.clone()
+        copies = hawk.pages_resize(none, lens, sv.int32([0, 0, 1]), refs, 4, dev_status=status, **out)
+        assert int(status) == binding.DEV_BAD_PREFIX and out.get("out_len", lens).tolist() == [0, 0, 0]
+        assert out.get("out_refs", refs).tolist() == [0, 1, 0, 2, 0] and copies.tolist() == [[-1, -1, 0]] * 3
+        status.zero_()
+    for parents in ([2, -1], [0, 1, 2, 2]):
+        to = torch.full_like(refs, 9)
+        table, lens = hawk.pages_fork(none, zero, sv.int32(parents), refs, 4, out_refs=to, dev_status=status)
+        assert table.shape == (len(parents), 0) and not lens.any() and torch.equal(to, refs)
+    copies = hawk.pages_compact(none, zero, refs, 4, 2, dev_status=status)
+    assert refs.tolist() == [2, 1, 0, 0, 0] and copies.tolist() == [[3, 0, 4], [-1, -1, 0]] and int(status) == 0
+    # four streams of two sequences that brought three rows each; nothing was accepted, or so it should be
+    begin, kv = sv.int32([0, 3, 6, 9, 12]), sv.int32([5, 6, 7, 8])
+    k, v = sv.pages_tensor(2, 6, 2, 4, 8)
+    table = sv.int32([[0, 1], [2, 3], [4, 5], [0, 2]])
+    keep = k.clone()
+    got = hawk.pages_keep(k, v, table, begin, kv, sv.int32(np.zeros((2, 0))), sv.int32([0, 0]), dev_status=status)
+    assert got.tolist() == [3, 4, 5, 6] and int(status) == 0
+    got = hawk.pages_keep(k, v, table, begin, kv, sv.int32(np.zeros((2, 0))), sv.int32([1, 0]), dev_status=status)
+    assert got.tolist() == [5, 4, 7, 6] and int(status) == binding.DEV_BAD_TREE and torch.equal(k, keep)
+    status.zero_()
+    got = hawk.pages_keep(k[:0], v[:0], table, begin, kv, sv.int32([[2], [1]]), sv.int32([1, 0]), dev_status=status)
+    assert got.tolist() == [4, 4, 6, 6] and int(status) == 0

@@ -288,3 +288,15 @@ def test_page_calls_refuse_misaligned_bases(lib):
         assert lib.hawk_pages_copy(ctypes.byref(_tensors()), P + off, 3, None, None) == E_ALIGN
         for name in ("block_table", "row_begin", "kv_len", "path", "accept_len", "out_len"):
             assert keep(**{name: P + off}) == E_ALIGN
+
+
+def test_only_tensors_with_elements_have_to_be_there(lib):
+    """Without a GPU: a call that lacks a tensor without elements gets past the NULLs (here to the refusal of what comes behind them)."""
+    assert lib.hawk_pages_resize(ctypes.byref(_resize(table_width=0, block_table=None, out_table=None, page_refs=ODD)), None, None) == E_ALIGN
+    a = _filled(sv.ForkArgs, ("kv_len", "page_refs", "parent"), S=2, S_out=3, table_width=0, n_pages=9, page_size=16, out_len=Q, out_refs=ODD)
+    assert lib.hawk_pages_fork(ctypes.byref(a), None, None) == E_ALIGN
+    a = _filled(sv.CompactArgs, ("kv_len", "page_refs", "out_refs", "copies"), S=2, table_width=0, n_pages=9, page_size=16, max_moves=3)
+    assert lib.hawk_pages_compact(ctypes.byref(a), None, None) == E_WS
+    a = _filled(sv.KeepArgs, ("row_begin", "kv_len", "path", "accept_len"), S=4, B=2, table_width=0, path_width=3, first=1, out_len=Q)
+    a.pages = _tensors(layers=0, k_pages=None, v_pages=None, k_row_stride=4)
+    assert lib.hawk_pages_keep(ctypes.byref(a), None, None) == E_ALIGN
