@@ -524,3 +524,87 @@ def test_tensors_without_elements():
     status.zero_()
     got = hawk.pages_keep(k[:0], v[:0], table, begin, kv, sv.int32([[2], [1]]), sv.int32([1, 0]), dev_status=status)
     assert got.tolist() == [4, 4, 6, 6] and int(status) == 0
+
+
+# ------------------------------------------------------------------------------------------ what goes wrong in states of many pages
+def _large(seed, spare=3000, share=2):
+    """700 streams over more pages than one block takes."""
+    return _state(700, 8, seed, share=share, spare=spare)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("left", [0, 1, 77, 150, 333])
+def test_pages_run_out_in_the_middle_of_a_large_batch(left, in_place):
+    """All but `left` free pages, spread over the pool, are held by the caller: the first stream that finds too few lies somewhere in the
+    batch, and the last free page somewhere in a block's share."""
+    for seed in (1, 2):
+        st, r = _large(100 + seed)
+        free = [p for p, c in enumerate(st.refs) if c == 0]
+        for p in r.permutation(free)[left:]:
+            st.refs[p] = 1
+        most = len(st.table[0]) * 8
+        new = [int(np.clip(n + r.choice([0, 3, 9, 40, -9, -n]), 0, most)) for n in st.lens]
+        want = serving.resize(st.table, st.lens, new, st.refs, 8)
+        assert st.n_pages > 2048 and want[4]
+        _same_resize(st, new, in_place)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_page_ids_out_of_range_in_a_large_batch(in_place):
+    """Ids that are none, in entries that are released and in those that streams grow into: flagged by every block, counted by none."""
+    st, r = _large(110)
+    n, page = st.n_pages, 8
+    new, bad, expect = list(st.lens), [-1, n, 1 << 30, -(1 << 31)], list(st.refs)
+    cut = [s for s in range(700) if st.lens[s] > 16][::9]
+    grow = [s for s in range(700) if st.lens[s] % page and s not in cut][::7]
+    table = [list(row) for row in st.table]
+    for i, s in enumerate(cut):  # releases its last two entries, of which one is none
+        new[s] = (serving.pages(st.lens[s], page) - 2) * page
+        at = serving.pages(st.lens[s], page) - 1 - i % 2
+        table[s][at] = bad[i % 4]
+        expect[table[s][serving.pages(st.lens[s], page) - 2 + i % 2]] -= 1
+    for i, s in enumerate(grow):  # within its last page, which is none
+        if st.lens[s] % page == page - 1:
+            continue
+        new[s] = st.lens[s] + 1 if (st.lens[s] + 1) % page else st.lens[s]
+        if new[s] > st.lens[s]:
+            table[s][st.lens[s] // page] = bad[i % 4]
+    dev_table, lens, refs = sv.int32(table), sv.int32(st.lens), sv.int32(st.refs)
+    status = _status()
+    out = {} if in_place else dict(out_table=torch.full_like(dev_table, -9), out_len=torch.zeros_like(lens), out_refs=torch.zeros_like(refs))
+    copies = hawk.pages_resize(dev_table, lens, sv.int32(new), refs, page, dev_status=status, **out)
+    assert int(status) == binding.DEV_BAD_PAGE and out.get("out_len", lens).tolist() == new
+    assert out.get("out_refs", refs).tolist() == expect and (copies[:, 0] == -1).all()
+    got = out.get("out_table", dev_table).tolist()
+    assert all(got[s][:serving.pages(new[s], page)] == table[s][:serving.pages(new[s], page)] for s in range(700))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_compact_of_a_large_table_that_names_free_pages(in_place):
+    """As for a small one: the entry stays and is flagged, whatever the workspace held before."""
+    st, _ = _large(120, share=1)
+    free = [p for p, c in enumerate(st.refs) if c == 0][::-1][:6]
+    where = [s for s in range(700) if st.lens[s] > 0][::130][:6]
+    table, refs = [list(row) for row in st.table], list(st.refs)
+    for s, p in zip(where, free):
+        refs[table[s][0]], table[s][0] = 0, p
+    for fill in (0, 1, 255):
+        for moves in (3, 900, st.n_pages):
+            want_table, want_refs, want_copies, want_top = serving.compact(table, st.lens, refs, 8, moves)
+            moved = [a for a, _, _ in want_copies if a >= 0]
+            ws = torch.full((hawk.pages_compact_workspace_bytes(st.n_pages, moves),), fill, dtype=torch.uint8, device="cuda")
+            dev_table, dev_refs, lens, status, top = sv.int32(table), sv.int32(refs), sv.int32(st.lens), _status(), _status()
+            out = {} if in_place else dict(out_table=torch.full_like(dev_table, -9), out_refs=torch.zeros_like(dev_refs))
+            copies = hawk.pages_compact(dev_table, lens, dev_refs, 8, moves, workspace=ws, top=top, dev_status=status, **out)
+            assert int(status) == (binding.DEV_BAD_PAGE if max(free) >= min(moved) else 0)
+            assert sv.same_where_written(out.get("out_table", dev_table), want_table)
+            assert out.get("out_refs", dev_refs).tolist() == want_refs and [tuple(c) for c in copies.tolist()] == want_copies
+            assert int(top) == want_top
+
+
+def test_no_index_leaves_its_array_in_a_large_batch():
+    lib = build.build_debug_variant()
+    with binding.alternate_library(lib):
+        test_pages_run_out_in_the_middle_of_a_large_batch(333, False)
+        test_page_ids_out_of_range_in_a_large_batch(False)
+        test_compact_of_a_large_table_that_names_free_pages(False)

@@ -328,3 +328,30 @@ def test_neighbours_of_the_maximum_at_low_temperatures(top, T):
     p = w / run[-1]
     assert (np.abs(probs.double().cpu().numpy() - p) <= sv.prob_bound(p, z)).all()
     assert (np.abs(prob.double().cpu().numpy() - p[want]) <= sv.prob_bound(p[want], z[want])).all() and (prob > 0).all()
+
+
+def test_rows_past_2_31_elements():
+    """Logits and distributions whose offsets pass 32 bits."""
+    stride, V = 1 << 30, 1001
+    x, u = _logits(4, V, "bf16", seed=20)
+    far = torch.empty(3 * stride + V, dtype=torch.bfloat16, device="cuda").as_strided((4, V), (stride, 1))
+    far.copy_(x)
+    out = torch.empty(3 * stride + V, dtype=torch.float32, device="cuda").as_strided((4, V), (stride, 1))
+    probs, kw = torch.full((4, V), NAN, device="cuda"), dict(top_k=300, top_p=0.9)
+    assert torch.equal(hawk.sample(far, u, probs=out, **kw), hawk.sample(x, u, probs=probs, **kw)) and torch.equal(out, probs)
+    assert torch.equal(hawk.sample(far, u[:2], cfg_scale=3.0), hawk.sample(x, u[:2], cfg_scale=3.0))
+
+
+@pytest.mark.parametrize("rows", [6, 160])
+def test_guided_drafts_of_an_image_vocabulary(rows):
+    """Drafts as this framework verifies them: guidance, top-k 2000, distributions over the image's ids inside a wider vocabulary."""
+    V, begin, end = 65536, 4, 8196
+    x, u = _logits(rows, V, "bf16", seed=21)
+    logits = torch.cat([x, (0.9 * x.float() + 0.1 * x.roll(1, 0).float()).bfloat16()])
+    probs = torch.full((rows, V), NAN, device="cuda")
+    kw = dict(cfg_scale=3.0, top_k=2000, v_begin=begin, v_end=end)
+    got = hawk.sample(logits, u, probs=probs, **kw)
+    assert (probs[:, :begin] == 0).all() and (probs[:, end:] == 0).all()
+    few = list(range(0, rows, max(1, rows // 6)))
+    pair = torch.cat([logits[few], logits[[rows + r for r in few]]])
+    assert _check(pair, u[few], **kw) == 0 and torch.equal(hawk.sample(pair, u[few], **kw), got[few])
