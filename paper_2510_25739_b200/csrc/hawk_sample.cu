@@ -903,11 +903,9 @@ __device__ __forceinline__ void Row<T, NT>::run()
     mx = hi;
     lo = fminf(lo, hi);  // (none of some was a number)
     rate = sh.rate;
-    // A temperature so low that nothing but the maximum has a weight: the next lower number lies 32 temperatures below it.  Else `nothing` is rounded
-    // downwards (to 96 temperatures below the maximum at most): nearer than 31.2 its own weight, which every lower id takes, would not be 0.
-    const double reach = 32.0 * static_cast<double>(temperature);
-    const bool flat = static_cast<double>(mx) - static_cast<double>(nextafterf(mx, -CUDART_INF_F)) >= reach;
-    nothing = flat ? mx : fmaxf(__double2float_rd(static_cast<double>(mx) - reach), kLowest);
+    // `nothing` is rounded downwards (to 96 temperatures below the maximum at most): nearer than 31.2 its own weight, which every lower id takes, would
+    // not be 0.  Where the next lower number lies 32 temperatures below the maximum it is the maximum itself.  (That difference is exact.)
+    nothing = mx - value_of(key_of(mx) - 1) >= 32.f * temperature ? mx : fmaxf(__fmaf_rd(-32.f, temperature, mx), kLowest);
     const bool some = mx > -CUDART_INF_F;
     const int stretch = ((m + NW - 1) / NW + 127) & ~127;  // whole runs of 4 a lane
     base = min(m, warp * stretch);
@@ -950,6 +948,7 @@ __device__ __forceinline__ void Row<T, NT>::run()
                 tau_m = fmaxf(kLowest, fminf(t, mx));
             }
         }
+        const bool flat = nothing >= mx;  // a temperature so low that nothing but the maximum has a weight
         if (flat) tau_m = mx;
         const bool by_k = top_k > 0 && top_k < P.n && !flat;
         const bool by_p = top_p < 1.f && !flat;
