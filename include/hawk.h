@@ -600,7 +600,8 @@ hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t *dev_statu
  *   5. token = the smallest id whose running sum of w (ascending id) exceeds u * sum(w); p = w / sum(w).
  * temperature 0: the lowest id of the maximum, with p = 1; steps 2 to 5 have no say.  A row without a finite logit: token -1, p = 0.
  * Exponentials are taken in fp64 and held as whole multiples of 2^-44 of the largest, sums of them in 64-bit integers: no order
- * changes a sum, so equal inputs give equal tokens whatever the launch (a w below 2^-45 counts as 0).
+ * changes a sum, so equal inputs give equal tokens whatever the launch (a w below 2^-45 counts as 0 and is never drawn, though
+ * probs may show its p).
  *
  *   dtype        HAWK_F32, HAWK_BF16 or HAWK_F16: the logits' type
  *   logits       [R][V] at row_stride (elements, not negative; 0: all rows draw from one; any alignment that the type needs)
@@ -608,14 +609,14 @@ hawk_status hawk_paged_attn(const hawk_paged_attn_args *args, int32_t *dev_statu
  *   temperature, top_k, top_p, min_p, cfg_scale      for all rows; top_k <= 0, top_p >= 1 and min_p <= 0 are off
  *   row_temperature, row_top_k, row_top_p, row_min_p, row_cfg_scale   device [R] or NULL: take the place of the number above.
  *                A row's NaN, or a temperature that is negative or infinite, is flagged HAWK_DEV_BAD_SETTING and taken as off
- *                (temperature 1).  row_cfg_scale is used as it is.
+ *                (temperature 1).  row_cfg_scale is used as it is (one that is not finite leaves its row without a finite logit).
  *   u            fp32 [R], uniforms in [0,1); others are clamped into it
  *   token        int32 [R] (out)
  *   token_prob   fp32 [R] (out) or NULL: p of the token
  *   probs        fp32 [R][V] at probs_row_stride (out) or NULL: p, 0 outside the range
- * Supported: 1 <= v_end - v_begin <= 262144.  No workspace.
+ * Supported: 1 <= v_end - v_begin <= 262144, R < 2^28.  No workspace.
  * Errors: NULL, SHAPE (a range outside [0, V], a negative stride, rows of probs that overlap), ALIGN (a base that its type cannot have), UNSUPPORTED,
- * PARAM (dtype; a temperature that is negative or not finite, a NaN), CUDA.  R == 0 returns HAWK_OK without a launch.
+ * PARAM (dtype; a temperature that is negative or not finite, a cfg_scale that is not finite, a NaN), CUDA.  R == 0 returns HAWK_OK without a launch.
  * ---------------------------------------------------------------------------------------------- */
 #define HAWK_F32 2
 
@@ -647,7 +648,8 @@ hawk_status hawk_sample(const hawk_sample_args *args, int32_t *dev_status, hawk_
  * hawk_pages_copy does that for the pages of all layers, and hawk_pages_keep moves rows inside them.  Every out_* may be the tensor it
  * comes from (in place) unless the call says otherwise; tensors that overlap in part are not supported.  What is counted in this
  * section is whole numbers; results do not depend on the launch.
- * Lengths outside [0, table_width * page_size] are flagged HAWK_DEV_BAD_PREFIX and their streams stay as they are; a page id outside
+ * Lengths outside [0, table_width * page_size] are flagged HAWK_DEV_BAD_PREFIX and their streams stay as they are (without
+ * entries, where it is the stream's own length that is out of range); a page id outside
  * [0, n_pages) is flagged HAWK_DEV_BAD_PAGE and nothing is counted for it.
  * Supported: S <= 4096, n_pages <= 2^20, page_size <= 65536, S * table_width and table_width * page_size + 65536 below 2^31.
  * page_refs, out_refs, workspaces and pages are 16-byte aligned, the other tensors as their type is.  A tensor without elements (a table

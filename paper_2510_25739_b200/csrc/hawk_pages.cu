@@ -8,11 +8,11 @@
 // meet at two cluster barriers (some 0.6 us each; another launch costs 1.5 to 2) and exchange one number a block through
 // distributed shared memory.  What a free page is called is found by prefix sums over bit masks in shared memory, not by atomics, so
 // results do not depend on the launch.  All of it is bound by latency: a launch, the barriers, and chains of dependent loads (lengths,
-// table, counts) of some 0.7 us each.  256 streams that share pages, 131 of which need a copy: 12.7 us under ncu (26 when a thread handed out the
-// free pages of a word of the bit mask one after the other).
-// The copies are bound by HBM: 4096 pages of 82 KB (keys and values) in 68 us, 6.5 TB/s read and written, what a plain copy of as many
-// bytes takes.  Fork is one block a stream (one block for small states) with four entries a thread in flight, its counts by atomics without a result (512 streams,
-// 238 thousand entries: 6.5 us); keep moves rows through registers, eight a thread in flight (128 trees of 64 nodes, 4 layers: 7 us for 26 MB,
+// table, counts) of some 0.7 us each.  256 streams that share pages, 131 of which need a copy: 9.9 us in a graph of such calls, 14.8 under
+// ncu with cold caches (a thread that handed out the free pages of a word of the bit mask one after the other took 26 where this took 12.7).
+// The copies are bound by HBM: 2735 pages of 82 KB (keys and values) in 71 us, 6.3 TB/s read and written, 0.97 of what a plain copy
+// reaches.  Fork is one block a stream (one block for small states) with four entries a thread in flight, its counts by atomics without a result (512 streams,
+// 239 thousand entries: 6.1 us in a graph, 8.0 under ncu); keep moves rows through registers, eight a thread in flight (128 trees of 64 nodes, 4 layers: 7 us for 26 MB,
 // bound by the chain lengths -> table -> rows).
 #include <climits>
 
@@ -457,7 +457,8 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(ForkParams P)
 
 // Small states whose counts go to another tensor: one block, a warp a stream, the changes of the counts in shared memory, so that no launch
 // ahead has to copy them.  In a graph 2.0 -> 1.7 us for 2 streams over 64 pages and 2.5 -> 2.0 for 16 over 700, launched one by one 4.3 -> 3.1; but
-// 2.6 and 3.2 for 16 streams of 256 entries, 2.6 and 3.8 for 64 of 64.
+// 2.6 and 3.2 for 16 streams of 256 entries, 2.6 and 3.8 for 64 of 64.  At the bounds, 32 streams of 128 entries: over 64 pages 4.0 -> 2.5 in a graph, over
+// 700 3.0 -> 2.6, over 4096 2.7 -> 2.8, and one by one 5.0 -> 3.1 for each.
 constexpr int kForkStreams = kBookWarps, kForkWidth = 128, kForkPages = 4 * kBookThreads;
 
 __global__ void __launch_bounds__(kBookThreads) fork_small_kernel(ForkParams P)
@@ -985,7 +986,7 @@ extern "C" hawk_status hawk_pages_copy(const hawk_page_tensors *pages, const int
     if (!hawk_host::is_sm100(nullptr)) return HAWK_ERR_UNSUPPORTED;
     const PageParams P = page_params(*pages, dev_status);
     const long long all = static_cast<long long>(P.H) * P.page_size * P.pieces;
-    // 4096 pages of 40 KB: 72 us with a page in two blocks, 68 in one; 16 pages of 98 KB: 5.2 us in twice as many blocks, 6.0 else.  A grid has
+    // 2735 pages of 40 KB: 72 us with a page in two blocks, 68 in one; 16 pages of 98 KB: 5.2 us in twice as many blocks, 6.0 else.  A grid has
     // 65535 blocks along z at most: the largest pages (2^27 pieces) take the larger share in any call.
     const bool many = static_cast<long long>(n_copies) * 2 * pages->layers >= 4 * 148 || all > 65535ll * kCopyPieces;
     const long long share = many ? 2 * kCopyPieces : kCopyPieces;

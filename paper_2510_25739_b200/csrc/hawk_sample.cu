@@ -35,7 +35,7 @@ namespace {
 
 using u64 = unsigned long long;
 
-constexpr int kBins = 256;       // steps of a histogram: 8 a lane, so that each warp sums them up for itself
+constexpr int kBins = 256;       // steps of a histogram: 8 a lane of the warp that sums them up
 constexpr int kFinal = 256;      // members of a step that are ranked against each other
 constexpr int kList = 2048;      // ids that are looked at one by one, an equal share for each warp
 constexpr float kLowest = -3.402823466e38f;  // the lowest number: what is below is none
@@ -1301,7 +1301,10 @@ extern "C" hawk_status hawk_sample(const hawk_sample_args *a, int32_t *dev_statu
     auto pick = [&](auto type) {
         using T = decltype(type);
         // Calls of more rows than SMs: two blocks of 512 threads on an SM (512 rows of 16384 ids 40 us, 59 with one; 100 rows 19.5 and 14.0,
-        // because two blocks go to an SM while others have none), four of 256 for short rows (2000 rows of 4096 ids 58 us, 73 with 512).
+        // because two blocks go to an SM while others have none), blocks of 256 for short rows, of which four fit an SM up to some 4900 ids and three
+        // up to 8192.  fp32, top-p, 256 and 512 threads: 2000 rows of 1000 ids 38 and 63 us, of 4096 59 and 86, of 5500 81 and 99, of 8192 96 and 110; 300 rows
+        // of 8192 21 and 26; bf16 and
+        // other settings alike.  (149 rows, one more than SMs, of 8192 ids: 17 and 16.)
         if (P.cluster > 1 || P.slice > 16384 || a->R <= 148) return launch<T, 512, 1>(P, a->R, st);
         return P.slice > 8192 ? launch<T, 512, 2>(P, a->R, st) : launch<T, 256, 4>(P, a->R, st);
     };
